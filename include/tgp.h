@@ -430,10 +430,63 @@ int  tgp_k_attn_scratch_bytes(const tgp_model_cfg *cfg, uint64_t *bytes);
 #define TGP_STATIC_MAX_DEVICES   64
 int  tgp_k_attn_decode_static(const void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *ob,
                               const tgp_model_cfg *cfg, uint32_t B, uint32_t pos0, void *stream);
+/* ---- a KV cache in 4 bits ---------------------------------------------------------------------------------------
+ * (No counterpart in the paper: the same tiles in less than a third of the bytes that the link and HBM move.)
+ * A tile holds TK positions of cfg->B sequences and Hkv heads.  A page (one sequence, one head of it; pages lie [B, Hkv]) is TK rows of Dh / 2
+ * bytes of codes, two e2m1 numbers per byte with the lower dimension in the lower half, and behind them TK rows of Dh / 16 bytes of scales in
+ * e4m3, one for 16 neighbouring dimensions.  An element stands for code * scale * 2^exp: k_exp and v_exp belong to a layer's keys and values, lie in
+ * [-TGP_Q4_EXP_MAX, TGP_Q4_EXP_MAX] and are the same in every call on its tiles (a group is held well while its largest magnitude lies between
+ * 2^(exp - 3) and 2^(exp + 11)).  A scale that is NaN makes its group NaN, in every call.
+ * In the calls below Dh is 64 or 128, TK a multiple of 16, B <= cfg->B, pos0 + q_len <= cfg->max_len, at most 64 tiles; tiles and the other
+ * device arrays, but for pos_dev, begin on 16 bytes; tile arrays are host arrays, and tiles that hold none of the call's positions may be NULL.
+ * pos_dev, if not NULL, gives each sequence a position of its own and is for single tokens (q_len == 1): int32 [B] on the device, the
+ * position of sequence b's new token, at most pos0.  A sequence whose entry lies outside [0, pos0] is idle: nothing of it is read or
+ * appended, and its attention output is zero.  As pos_dev is read by the kernels, a captured step may be replayed with other positions. */
+#define TGP_Q4_EXP_MAX 32
+/* Bytes of one tile for cfg->B sequences: B * Hkv * TK * (Dh / 2 + Dh / 16). */
+int  tgp_k_kv_q4_tile_bytes(const tgp_model_cfg *cfg, uint64_t *bytes);
+/* tgp_k_rope_kv() for tiles in 4 bits.  The rotated values are rounded to bf16 from exact sums of the products (tgp_k_rope_kv() rounds between, so a value may
+ * differ from its in the last bit).  Of 16 dimensions of a key or value, as bf16, the scale is the largest magnitude * 2^-exp / 6 and a code the value *
+ * 2^-exp / scale, both rounded to the nearest (ties to even) and to the largest number where they are beyond it.  A group that
+ * holds an infinity or a NaN gets a scale that is NaN. */
+int  tgp_k_rope_kv_q4(const float *q32, const float *k32, const float *v32, void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles,
+                      const float *cos_dev, const float *sin_dev, const tgp_model_cfg *cfg, uint32_t B, uint32_t q_len, uint32_t pos0,
+                      int k_exp, int v_exp, const int32_t *pos_dev, void *stream);
+/* Positions pos0 ... pos0 + q_len - 1 of the tiles (with pos_dev: each sequence's one) as bf16: kb, vb [B, Hkv, q_len, Dh].  Exact. */
+int  tgp_k_kv_unpack_q4(void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *kb, void *vb, const tgp_model_cfg *cfg, uint32_t B,
+                        uint32_t q_len, uint32_t pos0, int k_exp, int v_exp, const int32_t *pos_dev, void *stream);
+/* tgp_k_attn() over tiles in 4 bits, on what they stand for.  scratch_dev: tgp_k_attn_q4_scratch_bytes() for this q_len, not shared with a
+ * call that may run at the same time.  Single tokens, and up to 64 query rows per KV head (q_len * Hq / Hkv), read the codes themselves; a
+ * NaN in a position that a query does not see leaves its output alone.  For more, keys and values are unpacked into the scratch
+ * first and the kernels of tgp_k_attn() run on them, with their limits (Hq / Hkv of any size). */
+int  tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *ob, const tgp_model_cfg *cfg, uint32_t B,
+                   uint32_t q_len, uint32_t pos0, int k_exp, int v_exp, const int32_t *pos_dev, void *scratch_dev, void *stream);
+int  tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64_t *bytes);
+/* Sequences copied, forked, compacted and freed inside the KV tiles: place dst[i] of every tile becomes what place src[i] was before the call,
+ * or zeros where src[i] is -1.  All sources count as read before any destination is written, so the pairs may be any map (a
+ * permutation, one source for many).  src and dst are HOST arrays of n <= B places in [0, B), read before the call returns;
+ * a destination may appear once.  Only the first len positions move; what the places hold behind them stays.  form: TGP_KV_BF16 for
+ * tiles [B, Hkv, TK, Dh] in bf16 (Dh a multiple of 8), TGP_KV_Q4 for tiles in 4 bits as above.  Tiles begin on 16 bytes; those past
+ * len may be NULL, and no two may be the same. */
+#define TGP_KV_BF16 0u
+#define TGP_KV_Q4   1u
+int  tgp_k_kv_move(void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, const int32_t *src, const int32_t *dst, uint32_t n,
+                   const tgp_model_cfg *cfg, uint32_t form, uint32_t B, uint32_t len, void *stream);
 /* a = bf16(silu(g) * u), g/u fp32 [M, F]. */
 int  tgp_k_swiglu(const float *g32, const float *u32, void *ab, uint64_t n_elems, void *stream);
 /* out[b] = argmax_j logits[b, j], lowest index on ties. */
 int  tgp_k_argmax(const float *logits, int32_t *out, uint32_t B, uint32_t V, void *stream);
+/* out[b] = a token drawn from row b of logits [B, V] by the random number u_dev[b] in [0, 1).  Tokens are ordered by logit, the lower index
+ * first of equals, and weigh w = exp((logit - max) / temperature).  Kept are the first top_k; of these the shortest beginning whose weight is at
+ * least top_p of theirs (one token at least); of these the tokens with w >= min_p, the first token in any case.  The result is the lowest token, in the
+ * order of the indices, at which the sum of the kept weights exceeds u times the whole.  Weights are rounded to 2^-44.
+ * The settings are device arrays [B], each may be NULL: temperature (NULL: 1; a row's 0, negative or NaN: the first token, as tgp_k_argmax()),
+ * top_k (NULL, or 0 and less, or V and more: off), top_p (NULL, or 1 and more, or NaN: off; 0 and less: the first token), min_p (NULL, or
+ * 0 and less, or NaN: off).  Logits of -inf and NaN are never drawn; a row of nothing else gives token 0.  u below 0 or NaN counts as 0, 1
+ * and above as the largest number below 1.  V <= TGP_SAMPLE_MAX_V. */
+#define TGP_SAMPLE_MAX_V (1u << 19)
+int  tgp_k_sample(const float *logits, const float *u_dev, int32_t *out, uint32_t B, uint32_t V, const float *temperature_dev, const int32_t *top_k_dev,
+                  const float *top_p_dev, const float *min_p_dev, void *stream);
 
 #ifdef __cplusplus
 }

@@ -27,6 +27,8 @@ X_CLASSES, X_TENSORS, X_PINS, X_COMMANDS, X_TOTALS = range(5)
 X_TAIL = 0x100
 # tensor kinds (TGP_K_*)
 (K_EMBED, K_G1, K_WQ, K_WK, K_WV, K_WO, K_G2, K_WG, K_WU, K_WD, K_GF, K_LM, K_ROUTER, K_KTILE, K_VTILE) = range(15)
+KV_BF16, KV_Q4 = 0, 1
+SAMPLE_MAX_V = 1 << 19
 TAP_H, TAP_HF, TAP_Q, TAP_KTILE, TAP_VTILE, TAP_O, TAP_A = range(7)
 
 
@@ -130,6 +132,13 @@ _SIGS = {
     "tgp_k_attn_scratch_bytes": [C.POINTER(ModelCfg), C.POINTER(_U64)],
     "tgp_k_swiglu": [_P, _P, _P, _U64, _P],
     "tgp_k_argmax": [_P, _P, _U32, _U32, _P],
+    "tgp_k_kv_q4_tile_bytes": [C.POINTER(ModelCfg), C.POINTER(_U64)],
+    "tgp_k_rope_kv_q4": [_P, _P, _P, _P, C.POINTER(_P), C.POINTER(_P), _U32, _P, _P, C.POINTER(ModelCfg), _U32, _U32, _U32, C.c_int, C.c_int, _P, _P],
+    "tgp_k_kv_unpack_q4": [C.POINTER(_P), C.POINTER(_P), _U32, _P, _P, C.POINTER(ModelCfg), _U32, _U32, _U32, C.c_int, C.c_int, _P, _P],
+    "tgp_k_attn_q4": [_P, C.POINTER(_P), C.POINTER(_P), _U32, _P, C.POINTER(ModelCfg), _U32, _U32, _U32, C.c_int, C.c_int, _P, _P, _P],
+    "tgp_k_attn_q4_scratch_bytes": [C.POINTER(ModelCfg), _U32, C.POINTER(_U64)],
+    "tgp_k_kv_move": [C.POINTER(_P), C.POINTER(_P), _U32, C.POINTER(_I32), C.POINTER(_I32), _U32, C.POINTER(ModelCfg), _U32, _U32, _U32, _P],
+    "tgp_k_sample": [_P, _P, _P, _U32, _U32, _P, _P, _P, _P, _P],
 }
 
 
@@ -643,3 +652,46 @@ def k_argmax(logits, out, B, V, stream=None):
         rc = lib().tgp_k_argmax(_ptr(logits), _ptr(out), B, V, _ptr(stream))
     if rc:
         raise TgpError(rc, "tgp_k_argmax")
+
+
+def k_kv_q4_tile_bytes(cfg):
+    """Bytes of one KV tile in 4 bits, for cfg.B sequences."""
+    n = _U64()
+    _k(lib().tgp_k_kv_q4_tile_bytes(C.byref(cfg), C.byref(n)), "tgp_k_kv_q4_tile_bytes")
+    return n.value
+
+
+def k_rope_kv_q4(q32, k32, v32, qb, k_tiles, v_tiles, cos, sin, cfg, B, q_len, pos0, k_exp=0, v_exp=0, pos=None, stream=None):
+    ka, va, n = _tile_arrays(k_tiles, v_tiles)
+    _k(lib().tgp_k_rope_kv_q4(_ptr(q32), _ptr(k32), _ptr(v32), _ptr(qb), ka, va, n, _ptr(cos), _ptr(sin), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(stream)),
+       "tgp_k_rope_kv_q4")
+
+
+def k_kv_unpack_q4(k_tiles, v_tiles, kb, vb, cfg, B, q_len, pos0, k_exp=0, v_exp=0, pos=None, stream=None):
+    ka, va, n = _tile_arrays(k_tiles, v_tiles)
+    _k(lib().tgp_k_kv_unpack_q4(ka, va, n, _ptr(kb), _ptr(vb), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(stream)), "tgp_k_kv_unpack_q4")
+
+
+def k_attn_q4(qb, k_tiles, v_tiles, ob, cfg, B, q_len, pos0, k_exp=0, v_exp=0, pos=None, scratch=None, stream=None):
+    """scratch: k_attn_q4_scratch_bytes(cfg, q_len) of device memory, needed by every call."""
+    ka, va, n = _tile_arrays(k_tiles, v_tiles)
+    _k(lib().tgp_k_attn_q4(_ptr(qb), ka, va, n, _ptr(ob), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(scratch), _ptr(stream)), "tgp_k_attn_q4")
+
+
+def k_attn_q4_scratch_bytes(cfg, q_len):
+    n = _U64()
+    _k(lib().tgp_k_attn_q4_scratch_bytes(C.byref(cfg), q_len, C.byref(n)), "tgp_k_attn_q4_scratch_bytes")
+    return n.value
+
+
+def k_kv_move(k_tiles, v_tiles, src, dst, cfg, form, B, length, stream=None):
+    """Place dst[i] of the batch becomes what src[i] was (zeros where src[i] is -1), in every tile; form KV_BF16 or KV_Q4.  src, dst: sequences of ints."""
+    n = len(src)
+    if len(dst) != n:
+        raise ValueError(f"{n} sources and {len(dst)} destinations")
+    ka, va, tiles = _tile_arrays(k_tiles, v_tiles)
+    _k(lib().tgp_k_kv_move(ka, va, tiles, (_I32 * max(1, n))(*src), (_I32 * max(1, n))(*dst), n, C.byref(cfg), form, B, length, _ptr(stream)), "tgp_k_kv_move")
+
+
+def k_sample(logits, u, out, B, V, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    _k(lib().tgp_k_sample(_ptr(logits), _ptr(u), _ptr(out), B, V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(stream)), "tgp_k_sample")

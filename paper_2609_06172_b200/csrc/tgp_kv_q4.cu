@@ -1,0 +1,619 @@
+// A KV cache in 4 bits: append (with the rotation), read back, and the attention that reads it.
+//
+// A page - one sequence and KV head of a tile - is TK rows of DH / 2 bytes of codes, two e2m1 numbers per byte with the lower dimension in the
+// lower half, and behind them TK rows of DH / 16 bytes of scales in e4m3, one for 16 dimensions.  An element stands for code * scale * 2^exp.
+// A code has two significant bits and a scale four, so code * scale is exact in fp16 and bf16, and what the kernels multiply is what the cache
+// stands for, without a rounding of its own: the only ones are the two when a position is appended, and those of the softmax weights.
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <cstdint>
+#include "tgp.h"
+#include "tgp_kernels.h"
+#include "tgp_launch.cuh"
+
+namespace {
+
+using namespace tgp_launch;
+typedef __nv_bfloat16 bf16;
+constexpr uint32_t KEYS = 16;                    // positions of a chunk, the unit of work of a warp; a tile holds whole chunks
+constexpr uint32_t E4M3_NAN = 0x7f;
+
+__device__ __host__ constexpr uint32_t row_codes(uint32_t Dh) { return Dh / 2; }
+__device__ __host__ constexpr uint32_t row_scales(uint32_t Dh) { return Dh / 16; }
+__device__ __host__ constexpr uint64_t page_bytes(uint32_t Dh, uint32_t TK) { return (uint64_t)TK * (row_codes(Dh) + row_scales(Dh)); }
+
+// The position of sequence b's first new token, -1 if the sequence is idle: positions on the device are not trusted beyond the bound that
+// the call was checked with.
+__device__ __forceinline__ int position_of(const int32_t *pos, uint32_t b, uint32_t pos0) {
+    if (!pos) return (int)pos0;
+    const int p = pos[b];
+    return p < 0 || (uint32_t)p > pos0 ? -1 : p;
+}
+
+// ---- conversions (each two values; the lower half is the first) ----
+template <int BYTE> __device__ __forceinline__ uint32_t e2m1_f16x2(uint32_t w) {
+    uint32_t d;
+    if (BYTE == 0) asm("{.reg .b8 p, q, r, s; mov.b32 {p, q, r, s}, %1; cvt.rn.f16x2.e2m1x2 %0, p;}" : "=r"(d) : "r"(w));
+    else if (BYTE == 1) asm("{.reg .b8 p, q, r, s; mov.b32 {p, q, r, s}, %1; cvt.rn.f16x2.e2m1x2 %0, q;}" : "=r"(d) : "r"(w));
+    else if (BYTE == 2) asm("{.reg .b8 p, q, r, s; mov.b32 {p, q, r, s}, %1; cvt.rn.f16x2.e2m1x2 %0, r;}" : "=r"(d) : "r"(w));
+    else asm("{.reg .b8 p, q, r, s; mov.b32 {p, q, r, s}, %1; cvt.rn.f16x2.e2m1x2 %0, s;}" : "=r"(d) : "r"(w));
+    return d;
+}
+__device__ __forceinline__ uint16_t e2m1_of(float x0, float x1, float x2, float x3) {       // four codes, the first the lowest
+    uint16_t d;
+    asm("{.reg .b8 p, q; cvt.rn.satfinite.e2m1x2.f32 p, %2, %1; cvt.rn.satfinite.e2m1x2.f32 q, %4, %3; mov.b16 %0, {p, q};}" : "=h"(d) : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+    return d;
+}
+__device__ __forceinline__ uint32_t e4m3_f16x2(uint32_t two) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)two));
+    return d;
+}
+__device__ __forceinline__ uint32_t e4m3_of(float x) {                           // largest magnitude where x is beyond it
+    uint16_t d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %2, %1;" : "=h"(d) : "f"(x), "f"(0.f));
+    return d & 0xffu;
+}
+__device__ __forceinline__ float half_lo(uint32_t h) { return __low2float(*reinterpret_cast<const __half2 *>(&h)); }
+__device__ __forceinline__ float half_hi(uint32_t h) { return __high2float(*reinterpret_cast<const __half2 *>(&h)); }
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) { const __half2 h = __floats2half2_rn(lo, hi); return *reinterpret_cast<const uint32_t *>(&h); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) { const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi); return *reinterpret_cast<const uint32_t *>(&h); }
+__device__ __forceinline__ uint32_t mul2(uint32_t x, uint32_t y) { uint32_t d; asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(x), "r"(y)); return d; }
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// ---- append ---------------------------------------------------------------------------------------------------------------------
+
+// x * c + y * s, rounded once: the products' own roundings are found by fused multiply-adds and the sum's by the difference of what it should be, and
+// added back.  The cache's values then do not depend on the order of a multiplication and an addition, at a border of two 4-bit codes least of all.
+__device__ __forceinline__ float two_products(float x, float c, float y, float s) {
+    const float p = __fmul_rn(x, c), q = __fmul_rn(y, s), sum = __fadd_rn(p, q);
+    const float t = __fsub_rn(sum, p), lost = __fadd_rn(__fsub_rn(p, __fsub_rn(sum, t)), __fsub_rn(q, t));
+    const float rest = __fadd_rn(lost, __fadd_rn(__fmaf_rn(x, c, -p), __fmaf_rn(y, s, -q)));
+    const float r = __fadd_rn(sum, rest);
+    return fabsf(sum) < INFINITY ? r : sum;                    // (an infinity's rest is NaN)
+}
+
+// Codes and scale of a group of 16 dimensions of which this thread and its three neighbours hold four each, bf16 values; the codes are 16 bits.
+// The quotient is never near a border without being on it (a border times the scale has seven bits, the value eight), so both roundings
+// are those of the exact quotients.
+__device__ __forceinline__ uint32_t quantise(const float (&x)[4], float down, uint32_t quad, uint32_t &scale) {
+    uint32_t top = 0;                                            // the largest magnitude as its bits: ordered like the numbers, infinity and NaN above all of them
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+    top = max(top, __shfl_xor_sync(quad, top, 1));
+    top = max(top, __shfl_xor_sync(quad, top, 2));
+    if (top >= 0x7f800000u) { scale = E4M3_NAN; return 0; }      // the group stands for NaN
+    scale = e4m3_of(__fdiv_rn(__uint_as_float(top) * down, 6.f));
+    const float s = half_lo(e4m3_f16x2(scale));
+    if (s == 0.f) return 0;
+    return e2m1_of(__fdiv_rn(x[0] * down, s), __fdiv_rn(x[1] * down, s), __fdiv_rn(x[2] * down, s), __fdiv_rn(x[3] * down, s));
+}
+
+struct AppendArgs {
+    const float *q32, *k32, *v32; bf16 *qb; const float *cos_t, *sin_t; const int32_t *pos;
+    uint32_t Hq, Hkv, TK, q_len, pos0;
+    float k_down, v_down;                                        // 2^-exp
+    TgpTilePtrs tiles;
+};
+
+// A thread takes four neighbouring dimensions of a head and their partners half a head away, as in tgp_rope_kv_vec_kernel: 16-byte loads, and the
+// four threads of a group of 16 dimensions are neighbours.
+template <int DH>
+__global__ void __launch_bounds__(256) tgp_rope_kv_q4_kernel(const AppendArgs a) {
+    pdl_enter();
+    constexpr uint32_t HALF = DH / 2, V = HALF / 4;
+    const uint32_t m = blockIdx.x, b = m / a.q_len, quad = 0xfu << (threadIdx.x & 28u);
+    const int first = position_of(a.pos, b, a.pos0);
+    if (first < 0) return;
+    const uint32_t pos = (uint32_t)first + (m - b * a.q_len), tile = pos / a.TK, slot = pos - tile * a.TK;
+    for (uint32_t idx = blockIdx.y * blockDim.x + threadIdx.x; idx < (a.Hq + 2 * a.Hkv) * V; idx += gridDim.y * blockDim.x) {
+        const uint32_t h = idx / V, i = idx % V * 4;
+        const bool rot = h < a.Hq + a.Hkv;
+        const uint32_t hk = h < a.Hq ? h : rot ? h - a.Hq : h - a.Hq - a.Hkv;
+        const float *s = (h < a.Hq ? a.q32 + (size_t)m * a.Hq * DH : (rot ? a.k32 : a.v32) + (size_t)m * a.Hkv * DH) + hk * DH + i;
+        const float4 y0 = *reinterpret_cast<const float4 *>(s), y1 = *reinterpret_cast<const float4 *>(s + HALF);
+        float x0[4] = {y0.x, y0.y, y0.z, y0.w}, x1[4] = {y1.x, y1.y, y1.z, y1.w};
+        if (rot) {
+            const float4 c4 = *reinterpret_cast<const float4 *>(a.cos_t + (size_t)pos * HALF + i), s4 = *reinterpret_cast<const float4 *>(a.sin_t + (size_t)pos * HALF + i);
+            const float c[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float lo = x0[e], hi = x1[e];
+                x0[e] = two_products(lo, c[e], -hi, sn[e]);
+                x1[e] = two_products(hi, c[e], lo, sn[e]);
+            }
+        }
+        const uint2 p0 = make_uint2(pack_bf16(x0[0], x0[1]), pack_bf16(x0[2], x0[3])), p1 = make_uint2(pack_bf16(x1[0], x1[1]), pack_bf16(x1[2], x1[3]));
+        if (h < a.Hq) {
+            bf16 *o = a.qb + (size_t)m * a.Hq * DH + hk * DH + i;
+            *reinterpret_cast<uint2 *>(o) = p0;
+            *reinterpret_cast<uint2 *>(o + HALF) = p1;
+            continue;
+        }
+        uint8_t *page = reinterpret_cast<uint8_t *>(rot ? a.tiles.k[tile] : a.tiles.v[tile]) + ((size_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
+        uint8_t *codes = page + slot * row_codes(DH) + i / 2, *scales = page + a.TK * row_codes(DH) + slot * row_scales(DH) + i / 16;
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const uint2 p = part ? p1 : p0;
+            const float x[4] = {__uint_as_float(p.x << 16), __uint_as_float(p.x & 0xffff0000u), __uint_as_float(p.y << 16), __uint_as_float(p.y & 0xffff0000u)};
+            uint32_t scale;
+            const uint32_t code = quantise(x, rot ? a.k_down : a.v_down, quad, scale);
+            *reinterpret_cast<uint16_t *>(codes + part * (HALF / 2)) = (uint16_t)code;
+            if ((i & 15u) == 0) scales[part * (HALF / 16)] = (uint8_t)scale;
+        }
+    }
+}
+
+// ---- read back -------------------------------------------------------------------------------------------------------------------
+
+struct UnpackArgs {
+    bf16 *kb, *vb; const int32_t *pos;
+    uint32_t Hkv, TK, count, pos0, ld;                           // rows of a head in kb and vb are ld apart from head to head
+    float k_up, v_up;                                            // 2^exp
+    TgpTilePtrs tiles;
+};
+
+// A thread takes a group of 16 dimensions: 8 bytes of codes and a scale, 32 bytes of bf16.
+template <int DH>
+__global__ void __launch_bounds__(256) tgp_kv_unpack_q4_kernel(const UnpackArgs a) {
+    pdl_enter();
+    constexpr uint32_t GROUPS = DH / 16;
+    const uint32_t hk = blockIdx.y % a.Hkv, b = blockIdx.y / a.Hkv, is_v = blockIdx.z;
+    const int first = position_of(a.pos, b, a.pos0);
+    if (first < 0) return;
+    const float up = is_v ? a.v_up : a.k_up;
+    bf16 *out = (is_v ? a.vb : a.kb) + (size_t)blockIdx.y * a.ld * DH;
+    for (uint32_t idx = blockIdx.x * blockDim.x + threadIdx.x; idx < a.count * GROUPS; idx += gridDim.x * blockDim.x) {
+        const uint32_t t = idx / GROUPS, g = idx % GROUPS, pos = (uint32_t)first + t, tile = pos / a.TK, slot = pos - tile * a.TK;
+        const uint8_t *page = reinterpret_cast<const uint8_t *>(is_v ? a.tiles.v[tile] : a.tiles.k[tile]) + ((size_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
+        const uint2 w = *reinterpret_cast<const uint2 *>(page + slot * row_codes(DH) + g * 8);
+        const float s = half_lo(e4m3_f16x2(page[a.TK * row_codes(DH) + slot * row_scales(DH) + g])) * up;
+        const uint32_t h[8] = {e2m1_f16x2<0>(w.x), e2m1_f16x2<1>(w.x), e2m1_f16x2<2>(w.x), e2m1_f16x2<3>(w.x),
+                               e2m1_f16x2<0>(w.y), e2m1_f16x2<1>(w.y), e2m1_f16x2<2>(w.y), e2m1_f16x2<3>(w.y)};
+        uint32_t o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = pack_bf16(half_lo(h[i]) * s, half_hi(h[i]) * s);
+        uint4 *dst = reinterpret_cast<uint4 *>(out + (size_t)t * DH + g * 16);
+        dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+}
+
+// ---- attention of a few query rows ------------------------------------------------------------------------------------------------
+// The rows that share a KV head - the G query heads of the group, at each of the call's positions - are the eight columns of an mma.sync m16n8k16 tile, 16
+// keys its rows.  Both products take the cache as the 16-row operand, so a step of eight rows costs half the MMAs that rows of their own would:
+//   S [16 keys x 8 rows]      = K Q^T       DH / 16 MMAs, the sum runs over dimensions;
+//   O^T [DH dimensions x 8 rows] += V^T P^T DH / 16 MMAs of 16 dimensions each, the sum runs over the keys.
+// The order of a sum is free, and of the rows of a tile too, as long as both operands keep to it.  So a lane (r = lane / 4, c = lane % 4) takes whatever
+// is contiguous in memory, straight from global memory to the registers the MMA reads, without shared memory between:
+//   K: of the keys that rows r and r + 8 stand for, dimensions [c DH / 4, (c + 1) DH / 4) - one load of 16 bytes each (8 at DH = 64);
+//   V: of its four keys, dimensions [r DH / 8, (r + 1) DH / 8) - four loads of 8 bytes (4 at DH = 64).
+// Row r of a chunk stands for key (r % 2) * 4 + r / 2, and row r + 8 for the key 8 further on: the four keys of a lane's V are then
+// c, c + 4, c + 8, c + 12, and each of those loads reads four neighbouring rows.
+// S leaves the MMA with a key per lane row, P enters the next with a key per register pair: two 8 x 8 transposes (movmatrix) of P in fp16.
+struct AttnQ4Args {
+    const bf16 *qb; bf16 *ob; float *scratch; const int32_t *pos;
+    uint32_t Hq, Hkv, G, TK, q_len, pos0, rows, row_blocks, parts, per_part;
+    float qk, v_up;                                              // score = q k * qk in units of log2; 2^v_exp
+    TgpTilePtrs tiles;
+};
+constexpr int WARPS = 4;
+
+template <int DH> struct Chunk;
+template <> struct Chunk<128> { uint4 k[2]; uint2 v[4]; uint32_t ks, vs; };
+template <> struct Chunk<64> { uint2 k[2]; uint32_t v[4]; uint32_t ks, vs; };
+
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(x));
+    return d;
+}
+
+template <int DH, int NT>
+__global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Args a) {
+    pdl_enter();
+    constexpr int KS = DH / 16;                                   // MMAs of either product
+    constexpr uint32_t RB = 8 * NT, LD = DH + 4, CODES = row_codes(DH), SCALES = row_scales(DH);
+    __shared__ float part_o[WARPS][RB][LD];
+    __shared__ float part_ml[WARPS][RB][2];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    const uint32_t part = blockIdx.x, hk = blockIdx.y / a.row_blocks, row0 = (blockIdx.y - hk * a.row_blocks) * RB, b = blockIdx.z;
+    const uint32_t nrows = min(RB, a.rows - row0);
+    auto out_row = [&](uint32_t row) {
+        const uint32_t t = (row0 + row) / a.G;
+        return ((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row0 + row - t * a.G)) * DH;
+    };
+    const int first = position_of(a.pos, b, a.pos0);
+    if (first < 0) {                                              // an idle sequence: its rows are zeros
+        if (part == 0) for (uint32_t e = threadIdx.x; e < nrows * DH; e += blockDim.x) a.ob[out_row(e / DH) + e % DH] = __float2bfloat16_rn(0.f);
+        return;
+    }
+    // keys that this block's rows see: the last row's; the first row's tells from where on a chunk has masked ones
+    const uint32_t lim_first = (uint32_t)first + row0 / a.G, kvlen = (uint32_t)first + (row0 + nrows - 1) / a.G + 1;
+    const uint32_t nchunks = (kvlen + KEYS - 1) / KEYS, q_lo = min(nchunks, part * a.per_part), q_hi = min(nchunks, q_lo + a.per_part);
+
+    // ---- the rows of Q: fp16 has fewer exponents than bf16, so each row is scaled to [1, 2) by a power of two, which its scores get back ----
+    uint32_t qf[NT][KS][2];
+    float fix[NT][2];                                             // of the rows 2c and 2c + 1, which this lane's scores belong to
+    uint32_t lim[NT][2];                                          // the last key that these rows see
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const uint32_t row = nt * 8 + r;
+        uint4 w[DH / 32];
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) w[i] = row < nrows ? reinterpret_cast<const uint4 *>(a.qb + out_row(row) + c * (DH / 4))[i] : make_uint4(0, 0, 0, 0);
+        const uint32_t *x = reinterpret_cast<const uint32_t *>(w);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i) top = max(top, max(x[i] << 16 & 0x7fff0000u, x[i] & 0x7fff0000u));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        uint32_t e = top >> 23;                                   // exponent of the largest; 0 (nothing but zeros and subnormals) and 255 (not finite) leave the row as it is
+        if (e == 0 || e == 255) e = 127;
+        // 2^(127 - e) in two factors: it has no fp32 of its own where e is at its ends
+        const uint32_t up = (254 - e) / 2, up2 = 254 - e - up;
+        const float f0 = __uint_as_float((up + 64) << 23), f1 = __uint_as_float((up2 + 63) << 23);
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i) {
+            const float lo = __uint_as_float(x[i] << 16) * f0 * f1, hi = __uint_as_float(x[i] & 0xffff0000u) * f0 * f1;
+            qf[nt][i / 2][i & 1] = pack_f16(lo, hi);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t ee = __shfl_sync(0xffffffffu, e, (2 * c + i) * 4);
+            fix[nt][i] = a.qk * __uint_as_float(ee << 23);
+            lim[nt][i] = (uint32_t)first + min(row0 + nt * 8 + 2 * c + i, a.rows - 1) / a.G;
+        }
+    }
+
+    // ---- chunks q_lo + warp, q_lo + warp + WARPS, ... ----
+    const uint64_t page = ((uint64_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
+    const uint32_t krow = (r & 1) * 4 + (r >> 1), scales_at = a.TK * CODES;
+    uint32_t next = q_lo + warp, tile = next * KEYS / a.TK, off = next * KEYS - tile * a.TK;          // the chunk that is loaded next
+    auto load = [&](Chunk<DH> &x) {
+        const uint8_t *kp = reinterpret_cast<const uint8_t *>(a.tiles.k[tile]) + page, *vp = reinterpret_cast<const uint8_t *>(a.tiles.v[tile]) + page;
+        const uint32_t kr = off + krow, vr = off + c;
+        if constexpr (DH == 128) {
+            x.k[0] = __ldcg(reinterpret_cast<const uint4 *>(kp + kr * CODES + c * 16));
+            x.k[1] = __ldcg(reinterpret_cast<const uint4 *>(kp + (kr + 8) * CODES + c * 16));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.v[i] = __ldcg(reinterpret_cast<const uint2 *>(vp + (vr + 4 * i) * CODES + r * 8));
+            x.ks = (uint32_t)__ldcg(reinterpret_cast<const uint16_t *>(kp + scales_at + kr * SCALES + 2 * c)) |
+                   (uint32_t)__ldcg(reinterpret_cast<const uint16_t *>(kp + scales_at + (kr + 8) * SCALES + 2 * c)) << 16;
+        } else {
+            x.k[0] = __ldcg(reinterpret_cast<const uint2 *>(kp + kr * CODES + c * 8));
+            x.k[1] = __ldcg(reinterpret_cast<const uint2 *>(kp + (kr + 8) * CODES + c * 8));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.v[i] = __ldcg(reinterpret_cast<const uint32_t *>(vp + (vr + 4 * i) * CODES + r * 4));
+            x.ks = (uint32_t)__ldcg(kp + scales_at + kr * SCALES + c) | (uint32_t)__ldcg(kp + scales_at + (kr + 8) * SCALES + c) << 16;
+        }
+        x.vs = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.vs |= (uint32_t)__ldcg(vp + scales_at + (vr + 4 * i) * SCALES + (DH == 128 ? r : r / 2)) << (8 * i);
+        next += WARPS;
+        off += WARPS * KEYS;
+        while (off >= a.TK) { off -= a.TK; ++tile; }
+    };
+    float o[NT][KS][4], m_ref[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int j = 0; j < KS; ++j) o[nt][j][0] = o[nt][j][1] = o[nt][j][2] = o[nt][j][3] = 0.f;
+        m_ref[nt][0] = m_ref[nt][1] = -FLT_MAX;                   // finite: keys of score -inf weigh nothing, wherever they lie
+        l[nt][0] = l[nt][1] = 0.f;
+    }
+    auto attend = [&](Chunk<DH> &x, uint32_t key0) {
+        const bool masked = key0 + KEYS - 1 > lim_first;          // some row does not see all of the chunk
+        // ---- S = K Q^T ----
+        float s[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+        uint32_t sc[2][2];                                        // scales of the two keys, of the first and the second half of the lane's dimensions
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t two = x.ks >> (16 * h);
+            if constexpr (DH == 128) {
+                const uint32_t f = e4m3_f16x2(two);
+                sc[h][0] = __byte_perm(f, f, 0x1010);
+                sc[h][1] = __byte_perm(f, f, 0x3232);
+            } else sc[h][0] = sc[h][1] = e4m3_f16x2(__byte_perm(two, 0, 0x4400));
+        }
+        const uint32_t *k0 = reinterpret_cast<const uint32_t *>(&x.k[0]), *k1 = reinterpret_cast<const uint32_t *>(&x.k[1]);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int half = DH == 128 ? ks / 4 : 0;
+            const uint32_t w0 = k0[ks / 2], w1 = k1[ks / 2];
+            const uint32_t a0 = mul2(ks & 1 ? e2m1_f16x2<2>(w0) : e2m1_f16x2<0>(w0), sc[0][half]), a1 = mul2(ks & 1 ? e2m1_f16x2<2>(w1) : e2m1_f16x2<0>(w1), sc[1][half]);
+            const uint32_t a2 = mul2(ks & 1 ? e2m1_f16x2<3>(w0) : e2m1_f16x2<1>(w0), sc[0][half]), a3 = mul2(ks & 1 ? e2m1_f16x2<3>(w1) : e2m1_f16x2<1>(w1), sc[1][half]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
+        }
+        // ---- softmax weights: the reference of a row moves when a score is more than 8 above it, so weights stay below 2^8, which fp16 holds ----
+        uint32_t pb[NT][2];
+        bool grown = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v = s[nt][i] * fix[nt][i & 1];
+                if (masked && key0 + krow + (i & 2) * 4 > lim[nt][i & 1]) v = -INFINITY;
+                s[nt][i] = v;
+                grown |= v > m_ref[nt][i & 1] + 8.f;
+            }
+        if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float mx = fmaxf(s[nt][i], s[nt][i + 2]);
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    const float m_new = fmaxf(m_ref[nt][i], mx), alpha = ex2(m_ref[nt][i] - m_new);
+                    m_ref[nt][i] = m_new;
+                    l[nt][i] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < KS; ++j) { o[nt][j][i] *= alpha; o[nt][j][i + 2] *= alpha; }
+                }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float p[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = ex2(s[nt][i] - m_ref[nt][i & 1]);
+            l[nt][0] += p[0] + p[2];
+            l[nt][1] += p[1] + p[3];
+            pb[nt][0] = transpose8(pack_f16(p[0], p[1]));
+            pb[nt][1] = transpose8(pack_f16(p[2], p[3]));
+        }
+        // ---- O^T += V^T P^T ----
+        uint32_t nans = 0;                                        // keys of the chunk whose group of this lane's dimensions stands for NaN
+        if (masked) {                                             // behind the sequence: whatever the tile holds there; a row that does not see a NaN must not multiply it by 0
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t key = 4 * i + c, byte = x.vs >> (8 * i) & 0xffu;
+                if (key0 + key < kvlen && (byte & 0x7fu) == E4M3_NAN) nans |= 1u << key;
+                if (key0 + key >= kvlen || (byte & 0x7fu) == E4M3_NAN) x.vs &= ~(0xffu << (8 * i));
+            }
+            nans |= __shfl_xor_sync(0xffffffffu, nans, 1);
+            nans |= __shfl_xor_sync(0xffffffffu, nans, 2);
+        }
+        const uint32_t s01 = e4m3_f16x2(x.vs & 0xffffu), s23 = e4m3_f16x2(x.vs >> 16);
+        const uint32_t *v0 = reinterpret_cast<const uint32_t *>(&x.v[0]), *v1 = reinterpret_cast<const uint32_t *>(&x.v[1]), *v2 = reinterpret_cast<const uint32_t *>(&x.v[2]),
+                       *v3 = reinterpret_cast<const uint32_t *>(&x.v[3]);
+#pragma unroll
+        for (int w = 0; w < KS / 4; ++w) {
+            // bytes that hold the same dimension of two keys, of even dimensions and of odd ones
+            constexpr uint32_t LO = 0x0f0f0f0fu;
+            const uint32_t e01 = (v0[w] & LO) | (v1[w] << 4 & ~LO), d01 = (v0[w] >> 4 & LO) | (v1[w] & ~LO);
+            const uint32_t e23 = (v2[w] & LO) | (v3[w] << 4 & ~LO), d23 = (v2[w] >> 4 & LO) | (v3[w] & ~LO);
+#define TGP_Q4_PV(I) do { \
+                const uint32_t a0 = mul2(e2m1_f16x2<I>(e01), s01), a1 = mul2(e2m1_f16x2<I>(d01), s01), a2 = mul2(e2m1_f16x2<I>(e23), s23), a3 = mul2(e2m1_f16x2<I>(d23), s23); \
+                _Pragma("unroll") for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + I], a0, a1, a2, a3, pb[nt][0], pb[nt][1]); } while (0)
+            TGP_Q4_PV(0); TGP_Q4_PV(1); TGP_Q4_PV(2); TGP_Q4_PV(3);
+#undef TGP_Q4_PV
+        }
+        if (masked && __any_sync(0xffffffffu, nans != 0)) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t seen = lim[nt][i] < key0 ? 0u : lim[nt][i] - key0 >= KEYS - 1 ? 0xffffu : (2u << (lim[nt][i] - key0)) - 1;
+                    if (nans & seen)
+#pragma unroll
+                        for (int j = 0; j < KS; ++j) o[nt][j][i] = o[nt][j][i + 2] = NAN;
+                }
+        }
+    };
+    if (next < q_hi) {
+        Chunk<DH> x, y;
+        uint32_t q = next;
+        load(x);
+        while (true) {
+            const bool second = next < q_hi;
+            if (second) load(y);
+            attend(x, q * KEYS);
+            if (!second) break;
+            q += WARPS;
+            const bool third = next < q_hi;
+            if (third) load(x);
+            attend(y, q * KEYS);
+            if (!third) break;
+            q += WARPS;
+        }
+    }
+
+    // ---- the warps' partial results meet ----
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float sum = l[nt][i];
+            sum += __shfl_xor_sync(0xffffffffu, sum, 4);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+            const uint32_t row = nt * 8 + 2 * c + i;
+            if (r == 0) { part_ml[warp][row][0] = m_ref[nt][i]; part_ml[warp][row][1] = sum; }
+#pragma unroll
+            for (int j = 0; j < KS; ++j) *reinterpret_cast<float2 *>(&part_o[warp][row][r * (DH / 8) + 2 * j]) = make_float2(o[nt][j][i], o[nt][j][i + 2]);
+        }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < nrows * DH; e += blockDim.x) {
+        const uint32_t row = e / DH, d = e % DH;
+        float M = -FLT_MAX, sum = 0.f, acc = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) M = fmaxf(M, part_ml[w][row][0]);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = ex2(part_ml[w][row][0] - M);
+            sum += f * part_ml[w][row][1];
+            acc += f * part_o[w][row][d];
+        }
+        if (a.parts == 1) a.ob[out_row(row) + d] = __float2bfloat16_rn(acc / sum * a.v_up);
+        else {
+            float *to = a.scratch + ((((size_t)b * a.Hkv + hk) * a.rows + row0 + row) * a.parts + part) * (DH + 2);
+            if (d == 0) { to[0] = M; to[1] = sum; }
+            to[2 + d] = acc;
+        }
+    }
+}
+
+// One CTA per row: the parts' partial results.
+template <int DH>
+__global__ void __launch_bounds__(DH) tgp_attn_q4_merge_kernel(const AttnQ4Args a) {
+    pdl_enter();
+    const uint32_t row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, d = threadIdx.x, t = row / a.G;
+    const int first = position_of(a.pos, b, a.pos0);
+    if (first < 0) return;                                        // (written by the kernel before)
+    const uint32_t nchunks = ((uint32_t)first + t + KEYS) / KEYS, parts = (nchunks + a.per_part - 1) / a.per_part;      // those that have a key of this row
+    const float *from = a.scratch + (((size_t)b * a.Hkv + hk) * a.rows + row) * a.parts * (DH + 2);
+    float M = -FLT_MAX, sum = 0.f, acc = 0.f;
+    for (uint32_t p = 0; p < parts; ++p) M = fmaxf(M, from[p * (DH + 2)]);
+    for (uint32_t p = 0; p < parts; ++p) {
+        const float f = ex2(from[p * (DH + 2)] - M);
+        sum += f * from[p * (DH + 2) + 1];
+        acc += f * from[p * (DH + 2) + 2 + d];
+    }
+    a.ob[((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row - t * a.G)) * DH + d] = __float2bfloat16_rn(acc / sum * a.v_up);
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------------------------
+
+constexpr uint32_t FEW_ROWS = 64;                                // query rows per KV head that the kernel above serves; of a single token any number
+constexpr uint32_t PARTS_MAX = 64, UNITS_MAX = 8192;             // parts of a context; parts of all sequences and KV heads
+
+bool q4_geometry(const tgp_model_cfg *c) {
+    return c && (c->Dh == 64 || c->Dh == 128) && c->Hkv && c->Hq && c->Hq % c->Hkv == 0 && c->TK && c->TK % KEYS == 0 && c->TK <= (1u << 20);
+}
+
+// positions [pos0, pos0 + q_len) of B sequences, in tiles that hold them
+bool q4_call(const tgp_model_cfg *c, uint32_t n_tiles, uint32_t B, uint32_t q_len, uint32_t pos0, const int32_t *pos, int k_exp, int v_exp) {
+    if (!q4_geometry(c) || B > c->B || (pos && q_len > 1) || k_exp < -TGP_Q4_EXP_MAX || k_exp > TGP_Q4_EXP_MAX || v_exp < -TGP_Q4_EXP_MAX || v_exp > TGP_Q4_EXP_MAX) return false;
+    return (uint64_t)pos0 + q_len <= c->max_len && (uint64_t)pos0 + q_len <= (uint64_t)n_tiles * c->TK;
+}
+
+// tiles first <= i < end are used; they begin on 16 bytes
+int q4_tiles(TgpTilePtrs &t, void *const *k, void *const *v, uint32_t n, uint32_t first, uint32_t end) {
+    if (n > TGP_MAX_TILES) return TGP_E_TOO_LARGE;
+    if (!k || !v) return TGP_E_INVAL;
+    t = TgpTilePtrs{};
+    for (uint32_t i = first; i < end && i < n; ++i) {
+        t.k[i] = k[i]; t.v[i] = v[i];
+        if (!k[i] || !v[i] || ((reinterpret_cast<uintptr_t>(k[i]) | reinterpret_cast<uintptr_t>(v[i])) & 15u)) return TGP_E_INVAL;
+    }
+    return TGP_OK;
+}
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+uint32_t parts_limit(const tgp_model_cfg *c, uint32_t B, uint32_t kvlen) {
+    return std::max(1u, std::min({PARTS_MAX, (kvlen + 127) / 128, UNITS_MAX / std::max(1u, B * c->Hkv)}));
+}
+
+template <int DH>
+int launch_attn(const AttnQ4Args &a, uint32_t B, cudaStream_t st) {
+    const dim3 grid(a.parts, a.Hkv * a.row_blocks, B);
+    int rc = a.rows <= 8 ? launch(tgp_attn_q4_kernel<DH, 1>, grid, dim3(WARPS * 32), 0, st, 1, a) : launch(tgp_attn_q4_kernel<DH, 2>, grid, dim3(WARPS * 32), 0, st, 1, a);
+    if (rc || a.parts == 1) return rc;
+    return launch(tgp_attn_q4_merge_kernel<DH>, dim3(a.rows, a.Hkv, B), dim3(DH), 0, st, 1, a);
+}
+
+uint32_t few_parts(const tgp_model_cfg *c, uint32_t B, uint32_t row_blocks, uint32_t kvlen, bool ragged) {
+    const uint32_t units = B * c->Hkv * row_blocks, slots = (uint32_t)tgpk_sms() * 4 * (ragged ? 3 : 1), nchunks = (kvlen + KEYS - 1) / KEYS;
+    const uint32_t want = std::max(1u, std::min(slots / units, (nchunks + 2 * WARPS - 1) / (2 * WARPS)));
+    return std::min(want, parts_limit(c, B, kvlen));
+}
+
+bool few(const tgp_model_cfg *c, uint32_t q_len) { return q_len == 1 || (uint64_t)q_len * (c->Hq / c->Hkv) <= FEW_ROWS; }
+
+uint64_t unpacked_rows(uint32_t kvlen) { return ((uint64_t)kvlen + 63) / 64 * 64; }
+
+int launch_unpack(const UnpackArgs &a, const tgp_model_cfg *c, uint32_t B, cudaStream_t st) {
+    const dim3 grid(std::min<uint64_t>(((uint64_t)a.count * (c->Dh / 16) + 255) / 256, 1u << 20), B * c->Hkv, 2);
+    return c->Dh == 64 ? launch(tgp_kv_unpack_q4_kernel<64>, grid, dim3(256), 0, st, 1, a) : launch(tgp_kv_unpack_q4_kernel<128>, grid, dim3(256), 0, st, 1, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tgp_k_kv_q4_tile_bytes(const tgp_model_cfg *cfg, uint64_t *bytes) {
+    if (!bytes || !q4_geometry(cfg)) return TGP_E_INVAL;
+    *bytes = (uint64_t)cfg->B * cfg->Hkv * page_bytes(cfg->Dh, cfg->TK);
+    return TGP_OK;
+}
+
+int tgp_k_rope_kv_q4(const float *q32, const float *k32, const float *v32, void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, const float *cos_dev,
+                     const float *sin_dev, const tgp_model_cfg *cfg, uint32_t B, uint32_t q_len, uint32_t pos0, int k_exp, int v_exp, const int32_t *pos_dev, void *stream) {
+    if (!q32 || !k32 || !v32 || !qb || !cos_dev || !sin_dev || !q4_call(cfg, n_tiles, B, q_len, pos0, pos_dev, k_exp, v_exp)) return TGP_E_INVAL;
+    if (!aligned16(q32) || !aligned16(k32) || !aligned16(v32) || !aligned16(qb) || !aligned16(cos_dev) || !aligned16(sin_dev)) return TGP_E_INVAL;
+    AppendArgs a{q32, k32, v32, (bf16 *)qb, cos_dev, sin_dev, pos_dev, cfg->Hq, cfg->Hkv, cfg->TK, q_len, pos0, ldexpf(1.f, -k_exp), ldexpf(1.f, -v_exp), {}};
+    const uint32_t end = B && q_len ? (pos0 + q_len - 1) / cfg->TK + 1 : 0;
+    if (int rc = q4_tiles(a.tiles, k_tiles, v_tiles, n_tiles, pos_dev ? 0 : pos0 / cfg->TK, end)) return rc;
+    if (!B || !q_len) return TGP_OK;
+    if ((uint64_t)B * q_len > 0x7fffffffu) return TGP_E_TOO_LARGE;
+    const uint32_t items = (cfg->Hq + 2 * cfg->Hkv) * (cfg->Dh / 8);
+    const uint32_t split = std::max(1u, std::min((items + 255) / 256, 4u * (uint32_t)tgpk_sms() / (B * q_len)));
+    const dim3 grid(B * q_len, split);
+    return cfg->Dh == 64 ? launch(tgp_rope_kv_q4_kernel<64>, grid, dim3(256), 0, (cudaStream_t)stream, 1, a) : launch(tgp_rope_kv_q4_kernel<128>, grid, dim3(256), 0, (cudaStream_t)stream, 1, a);
+}
+
+int tgp_k_kv_unpack_q4(void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *kb, void *vb, const tgp_model_cfg *cfg, uint32_t B, uint32_t q_len, uint32_t pos0,
+                       int k_exp, int v_exp, const int32_t *pos_dev, void *stream) {
+    if (!kb || !vb || !aligned16(kb) || !aligned16(vb) || !q4_call(cfg, n_tiles, B, q_len, pos0, pos_dev, k_exp, v_exp)) return TGP_E_INVAL;
+    UnpackArgs a{(bf16 *)kb, (bf16 *)vb, pos_dev, cfg->Hkv, cfg->TK, q_len, pos0, q_len, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), {}};
+    const uint32_t end = B && q_len ? (pos0 + q_len - 1) / cfg->TK + 1 : 0;
+    if (int rc = q4_tiles(a.tiles, k_tiles, v_tiles, n_tiles, pos_dev ? 0 : pos0 / cfg->TK, end)) return rc;
+    if (!B || !q_len) return TGP_OK;
+    if ((uint64_t)B * cfg->Hkv > 65535u) return TGP_E_TOO_LARGE;
+    return launch_unpack(a, cfg, B, (cudaStream_t)stream);
+}
+
+int tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64_t *bytes) {
+    if (!bytes || !q4_geometry(cfg) || !cfg->B || !q_len || q_len > cfg->max_len) return TGP_E_INVAL;
+    if (few(cfg, q_len)) {                                        // partial results; fewer sequences than cfg->B may have more parts each
+        const uint64_t rows = (uint64_t)q_len * (cfg->Hq / cfg->Hkv), units = (uint64_t)cfg->B * cfg->Hkv, longest = std::min<uint64_t>(PARTS_MAX, ((uint64_t)cfg->max_len + 127) / 128);
+        *bytes = std::min(units * longest, std::max<uint64_t>(units, UNITS_MAX)) * rows * (cfg->Dh + 2) * sizeof(float);
+    } else                                                        // keys and values as bf16
+        *bytes = 2 * (uint64_t)cfg->B * cfg->Hkv * unpacked_rows(cfg->max_len) * cfg->Dh * sizeof(bf16);
+    return TGP_OK;
+}
+
+int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *ob, const tgp_model_cfg *cfg, uint32_t B, uint32_t q_len, uint32_t pos0,
+                  int k_exp, int v_exp, const int32_t *pos_dev, void *scratch_dev, void *stream) {
+    if (!qb || !ob || !scratch_dev || !aligned16(qb) || !aligned16(ob) || !aligned16(scratch_dev) || !q4_call(cfg, n_tiles, B, q_len, pos0, pos_dev, k_exp, v_exp)) return TGP_E_INVAL;
+    const uint32_t kvlen = pos0 + q_len, G = cfg->Hq / cfg->Hkv;
+    TgpTilePtrs tiles;
+    if (int rc = q4_tiles(tiles, k_tiles, v_tiles, n_tiles, 0, B && q_len ? (kvlen - 1) / cfg->TK + 1 : 0)) return rc;
+    if (!B || !q_len) return TGP_OK;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (few(cfg, q_len)) {
+        const uint32_t rows = q_len * G, rb = rows <= 8 ? 8 : 16, row_blocks = (rows + rb - 1) / rb;
+        if ((uint64_t)cfg->Hkv * row_blocks > 65535u || rows > 65535u || B > 65535u) return TGP_E_TOO_LARGE;
+        const uint32_t nchunks = (kvlen + KEYS - 1) / KEYS, parts = few_parts(cfg, B, row_blocks, kvlen, pos_dev != nullptr), per = (nchunks + parts - 1) / parts;
+        AttnQ4Args a{(const bf16 *)qb, (bf16 *)ob, (float *)scratch_dev, pos_dev, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, rows, row_blocks, (nchunks + per - 1) / per, per,
+                     ldexpf(1.4426950408889634f / sqrtf((float)cfg->Dh), k_exp), ldexpf(1.f, v_exp), tiles};
+        return cfg->Dh == 64 ? launch_attn<64>(a, B, st) : launch_attn<128>(a, B, st);
+    }
+    // more rows: keys and values once as bf16, exactly what the cache stands for, and the attention over a bf16 cache of one tile
+    if ((uint64_t)B * cfg->Hkv > 65535u) return TGP_E_TOO_LARGE;
+    const uint64_t ld = unpacked_rows(kvlen);
+    bf16 *kb = (bf16 *)scratch_dev, *vb = kb + (uint64_t)B * cfg->Hkv * ld * cfg->Dh;
+    UnpackArgs u{kb, vb, nullptr, cfg->Hkv, cfg->TK, kvlen, 0, (uint32_t)ld, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), tiles};
+    if (int rc = launch_unpack(u, cfg, B, st)) return rc;
+    tgp_model_cfg one = *cfg;
+    one.TK = (uint32_t)ld;
+    TgpTilePtrs whole{};
+    whole.k[0] = kb; whole.v[0] = vb;
+    return tgpk_attn(qb, whole, 1, ob, &one, B, q_len, pos0, nullptr, st);
+}
+
+}  // extern "C"
