@@ -73,8 +73,7 @@ __device__ __forceinline__ float two_products(float x, float c, float y, float s
     const float p = __fmul_rn(x, c), q = __fmul_rn(y, s), sum = __fadd_rn(p, q);
     const float t = __fsub_rn(sum, p), lost = __fadd_rn(__fsub_rn(p, __fsub_rn(sum, t)), __fsub_rn(q, t));
     const float rest = __fadd_rn(lost, __fadd_rn(__fmaf_rn(x, c, -p), __fmaf_rn(y, s, -q)));
-    const float r = __fadd_rn(sum, rest);
-    return fabsf(sum) < INFINITY ? r : sum;                    // (an infinity's rest is NaN)
+    return rest != 0.f && fabsf(sum) < INFINITY ? __fadd_rn(sum, rest) : sum;       // (a zero keeps its sign; an infinity's rest is NaN)
 }
 
 // Codes and scale of a group of 16 dimensions of which this thread and its three neighbours hold four each, bf16 values; the codes are 16 bits.
@@ -202,6 +201,7 @@ struct AttnQ4Args {
     TgpTilePtrs tiles;
 };
 constexpr int WARPS = 4;
+constexpr float BELOW = 6.f, ABOVE = 14.f;
 
 template <int DH> struct Chunk;
 template <> struct Chunk<128> { uint4 k[2]; uint2 v[4]; uint32_t ks, vs; };
@@ -336,7 +336,8 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
         }
-        // ---- softmax weights: the reference of a row moves when a score is more than 8 above it, so weights stay below 2^8, which fp16 holds ----
+        // ---- softmax weights: the reference of a row lies BELOW under its largest score when it moves, and moves when a score is more than ABOVE over it.  Weights
+        // are below 2^ABOVE then, which fp16 holds, and what it rounds to multiples of 2^-24 is less than 2^-(BELOW + 14) of the largest ----
         uint32_t pb[NT][2];
         bool grown = false;
 #pragma unroll
@@ -346,7 +347,7 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
                 float v = s[nt][i] * fix[nt][i & 1];
                 if (masked && key0 + krow + (i & 2) * 4 > lim[nt][i & 1]) v = -INFINITY;
                 s[nt][i] = v;
-                grown |= v > m_ref[nt][i & 1] + 8.f;
+                grown |= v > m_ref[nt][i & 1] + ABOVE;
             }
         if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
@@ -357,7 +358,7 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float m_new = fmaxf(m_ref[nt][i], mx), alpha = ex2(m_ref[nt][i] - m_new);
+                    const float m_new = fmaxf(m_ref[nt][i], mx - BELOW), alpha = ex2(m_ref[nt][i] - m_new);
                     m_ref[nt][i] = m_new;
                     l[nt][i] *= alpha;
 #pragma unroll
