@@ -188,9 +188,10 @@ __global__ void __launch_bounds__(256) tgp_kv_unpack_q4_kernel(const UnpackArgs 
 //   S [16 keys x 8 rows]      = K Q^T       DH / 16 MMAs, the sum runs over dimensions;
 //   O^T [DH dimensions x 8 rows] += V^T P^T DH / 16 MMAs of 16 dimensions each, the sum runs over the keys.
 // The order of a sum is free, and of the rows of a tile too, as long as both operands keep to it.  So a lane (r = lane / 4, c = lane % 4) takes whatever
-// is contiguous in memory, straight from global memory to the registers the MMA reads, without shared memory between:
+// is contiguous in memory:
 //   K: of the keys that rows r and r + 8 stand for, dimensions [c DH / 4, (c + 1) DH / 4) - one load of 16 bytes each (8 at DH = 64);
 //   V: of its four keys, dimensions [r DH / 8, (r + 1) DH / 8) - four loads of 8 bytes (4 at DH = 64).
+// and converts it to the registers the MMA reads: two codes to two fp16 per instruction, and a multiplication of both by their scales.
 // Row r of a chunk stands for key (r % 2) * 4 + r / 2, and row r + 8 for the key 8 further on: the four keys of a lane's V are then
 // c, c + 4, c + 8, c + 12, and each of those loads reads four neighbouring rows.
 // S leaves the MMA with a key per lane row, P enters the next with a key per register pair: two 8 x 8 transposes (movmatrix) of P in fp16.
@@ -203,9 +204,22 @@ struct AttnQ4Args {
 constexpr int WARPS = 4;
 constexpr float BELOW = 6.f, ABOVE = 14.f;
 
-template <int DH> struct Chunk;
-template <> struct Chunk<128> { uint4 k[2]; uint2 v[4]; uint32_t ks, vs; };
-template <> struct Chunk<64> { uint2 k[2]; uint32_t v[4]; uint32_t ks, vs; };
+// A chunk in shared memory: codes of its keys, codes of its values, scales of both.  A 16-byte piece of a row lies where neither the copies in nor the loads of
+// eight lanes at a time meet another in a bank: K is read four pieces of rows q and q + 4 at a time, V two pieces of four neighbouring rows.
+template <int DH> struct Stage {
+    static constexpr uint32_t CODES = row_codes(DH), SCALES = row_scales(DH), V = KEYS * CODES, KS = 2 * V, VS = KS + KEYS * SCALES, BYTES = VS + KEYS * SCALES;
+    static __device__ __forceinline__ uint32_t at(uint32_t row, uint32_t piece) {
+        if constexpr (DH == 128) return (row >> 1) * 128 + (((row ^ row >> 2) & 1) * 4 + (piece ^ (row & 2))) * 16;
+        else return (row >> 2) * 128 + (((row & 3) * 2 + piece) ^ (row & 4)) * 16;
+    }
+};
+template <int DH> constexpr int STAGES = DH == 128 ? 5 : 6;
+template <int DH> constexpr uint32_t attn_smem(int NT) {
+    const uint32_t ring = WARPS * STAGES<DH> * Stage<DH>::BYTES, partial = WARPS * 8 * NT * (DH + 4 + 2) * 4;
+    return ring > partial ? ring : partial;
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -222,8 +236,10 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
     pdl_enter();
     constexpr int KS = DH / 16;                                   // MMAs of either product
     constexpr uint32_t RB = 8 * NT, LD = DH + 4, CODES = row_codes(DH), SCALES = row_scales(DH);
-    __shared__ float part_o[WARPS][RB][LD];
-    __shared__ float part_ml[WARPS][RB][2];
+    using St = Stage<DH>;
+    extern __shared__ __align__(128) uint8_t q4_sm[];
+    float (*part_o)[RB][LD] = reinterpret_cast<float (*)[RB][LD]>(q4_sm);                                  // (of the warps, when the chunks are done)
+    float (*part_ml)[RB][2] = reinterpret_cast<float (*)[RB][2]>(q4_sm + sizeof(float) * WARPS * RB * LD);
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     const uint32_t part = blockIdx.x, hk = blockIdx.y / a.row_blocks, row0 = (blockIdx.y - hk * a.row_blocks) * RB, b = blockIdx.z;
     const uint32_t nrows = min(RB, a.rows - row0);
@@ -276,31 +292,27 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
 
     // ---- chunks q_lo + warp, q_lo + warp + WARPS, ... ----
     const uint64_t page = ((uint64_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
-    const uint32_t krow = (r & 1) * 4 + (r >> 1), scales_at = a.TK * CODES;
-    uint32_t next = q_lo + warp, tile = next * KEYS / a.TK, off = next * KEYS - tile * a.TK;          // the chunk that is loaded next
-    auto load = [&](Chunk<DH> &x) {
-        const uint8_t *kp = reinterpret_cast<const uint8_t *>(a.tiles.k[tile]) + page, *vp = reinterpret_cast<const uint8_t *>(a.tiles.v[tile]) + page;
-        const uint32_t kr = off + krow, vr = off + c;
-        if constexpr (DH == 128) {
-            x.k[0] = __ldcg(reinterpret_cast<const uint4 *>(kp + kr * CODES + c * 16));
-            x.k[1] = __ldcg(reinterpret_cast<const uint4 *>(kp + (kr + 8) * CODES + c * 16));
+    const uint32_t krow = (r & 1) * 4 + (r >> 1), ring = (uint32_t)__cvta_generic_to_shared(q4_sm) + warp * STAGES<DH> * St::BYTES;
+    uint32_t next = q_lo + warp, tile = next * KEYS / a.TK, off = next * KEYS - tile * a.TK, fill = ring;      // the chunk that is requested next, and its stage
+    const uint32_t lane_at = St::at(lane / (CODES / 16), lane % (CODES / 16)), lane_scale = (lane % KEYS) * 16;
+    auto request = [&]() {
+        if (next < q_hi) {
+            const uint8_t *kp = reinterpret_cast<const uint8_t *>(a.tiles.k[tile]) + page, *vp = reinterpret_cast<const uint8_t *>(a.tiles.v[tile]) + page;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x.v[i] = __ldcg(reinterpret_cast<const uint2 *>(vp + (vr + 4 * i) * CODES + r * 8));
-            x.ks = (uint32_t)__ldcg(reinterpret_cast<const uint16_t *>(kp + scales_at + kr * SCALES + 2 * c)) |
-                   (uint32_t)__ldcg(reinterpret_cast<const uint16_t *>(kp + scales_at + (kr + 8) * SCALES + 2 * c)) << 16;
-        } else {
-            x.k[0] = __ldcg(reinterpret_cast<const uint2 *>(kp + kr * CODES + c * 8));
-            x.k[1] = __ldcg(reinterpret_cast<const uint2 *>(kp + (kr + 8) * CODES + c * 8));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.v[i] = __ldcg(reinterpret_cast<const uint32_t *>(vp + (vr + 4 * i) * CODES + r * 4));
-            x.ks = (uint32_t)__ldcg(kp + scales_at + kr * SCALES + c) | (uint32_t)__ldcg(kp + scales_at + (kr + 8) * SCALES + c) << 16;
+            for (uint32_t i = 0; i < KEYS * CODES / 512; ++i) {       // (eight rows further on in the swizzle is 8 * CODES bytes)
+                cp_async16(fill + lane_at + i * 512, kp + off * CODES + i * 512 + lane * 16);
+                cp_async16(fill + St::V + lane_at + i * 512, vp + off * CODES + i * 512 + lane * 16);
+            }
+            if (lane < 2 * SCALES) {
+                const uint8_t *from = lane < SCALES ? kp : vp;
+                cp_async16(fill + St::KS + lane_scale, from + a.TK * CODES + off * SCALES + (lane % SCALES) * 16);
+            }
+            next += WARPS;
+            off += WARPS * KEYS;
+            while (off >= a.TK) { off -= a.TK; ++tile; }
         }
-        x.vs = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x.vs |= (uint32_t)__ldcg(vp + scales_at + (vr + 4 * i) * SCALES + (DH == 128 ? r : r / 2)) << (8 * i);
-        next += WARPS;
-        off += WARPS * KEYS;
-        while (off >= a.TK) { off -= a.TK; ++tile; }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        fill = fill + St::BYTES == ring + STAGES<DH> * St::BYTES ? ring : fill + St::BYTES;
     };
     float o[NT][KS][4], m_ref[NT][2], l[NT][2];
 #pragma unroll
@@ -310,8 +322,16 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
         m_ref[nt][0] = m_ref[nt][1] = -FLT_MAX;                   // finite: keys of score -inf weigh nothing, wherever they lie
         l[nt][0] = l[nt][1] = 0.f;
     }
-    auto attend = [&](Chunk<DH> &x, uint32_t key0) {
+    auto attend = [&](uint32_t at, uint32_t key0) {
+        const uint8_t *st = q4_sm + (at - (uint32_t)__cvta_generic_to_shared(q4_sm));
         const bool masked = key0 + KEYS - 1 > lim_first;          // some row does not see all of the chunk
+        uint32_t kw[2][DH / 32], vw[4][DH / 64], vs01, vs23;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+            const uint8_t *from = st + h * 8 * CODES + (DH == 128 ? St::at(krow, c) : St::at(krow, c >> 1) + (c & 1) * 8);
+            if constexpr (DH == 128) { const uint4 w = *reinterpret_cast<const uint4 *>(from); kw[h][0] = w.x; kw[h][1] = w.y; kw[h][2] = w.z; kw[h][3] = w.w; }
+            else { const uint2 w = *reinterpret_cast<const uint2 *>(from); kw[h][0] = w.x; kw[h][1] = w.y; }
+        }
         // ---- S = K Q^T ----
         float s[NT][4];
 #pragma unroll
@@ -319,18 +339,17 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
         uint32_t sc[2][2];                                        // scales of the two keys, of the first and the second half of the lane's dimensions
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t two = x.ks >> (16 * h);
+            const uint8_t *from = st + St::KS + (h * 8 + krow) * SCALES;
             if constexpr (DH == 128) {
-                const uint32_t f = e4m3_f16x2(two);
+                const uint32_t f = e4m3_f16x2(*reinterpret_cast<const uint16_t *>(from + 2 * c));
                 sc[h][0] = __byte_perm(f, f, 0x1010);
                 sc[h][1] = __byte_perm(f, f, 0x3232);
-            } else sc[h][0] = sc[h][1] = e4m3_f16x2(__byte_perm(two, 0, 0x4400));
+            } else sc[h][0] = sc[h][1] = e4m3_f16x2(from[c] * 0x101u);
         }
-        const uint32_t *k0 = reinterpret_cast<const uint32_t *>(&x.k[0]), *k1 = reinterpret_cast<const uint32_t *>(&x.k[1]);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             const int half = DH == 128 ? ks / 4 : 0;
-            const uint32_t w0 = k0[ks / 2], w1 = k1[ks / 2];
+            const uint32_t w0 = kw[0][ks / 2], w1 = kw[1][ks / 2];
             const uint32_t a0 = mul2(ks & 1 ? e2m1_f16x2<2>(w0) : e2m1_f16x2<0>(w0), sc[0][half]), a1 = mul2(ks & 1 ? e2m1_f16x2<2>(w1) : e2m1_f16x2<0>(w1), sc[1][half]);
             const uint32_t a2 = mul2(ks & 1 ? e2m1_f16x2<3>(w0) : e2m1_f16x2<1>(w0), sc[0][half]), a3 = mul2(ks & 1 ? e2m1_f16x2<3>(w1) : e2m1_f16x2<1>(w1), sc[1][half]);
 #pragma unroll
@@ -376,28 +395,35 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
             pb[nt][1] = transpose8(pack_f16(p[2], p[3]));
         }
         // ---- O^T += V^T P^T ----
-        uint32_t nans = 0;                                        // keys of the chunk whose group of this lane's dimensions stands for NaN
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint8_t *from = st + St::V + (DH == 128 ? St::at(4 * i + c, r >> 1) + (r & 1) * 8 : St::at(4 * i + c, r >> 2) + (r & 3) * 4);
+            if constexpr (DH == 128) { const uint2 w = *reinterpret_cast<const uint2 *>(from); vw[i][0] = w.x; vw[i][1] = w.y; }
+            else vw[i][0] = *reinterpret_cast<const uint32_t *>(from);
+        }
+        uint32_t vs[4], nans = 0;                                 // nans: keys of the chunk whose group of this lane's dimensions stands for NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) vs[i] = st[St::VS + (4 * i + c) * SCALES + (DH == 128 ? r : r / 2)];
         if (masked) {                                             // behind the sequence: whatever the tile holds there; a row that does not see a NaN must not multiply it by 0
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t key = 4 * i + c, byte = x.vs >> (8 * i) & 0xffu;
-                if (key0 + key < kvlen && (byte & 0x7fu) == E4M3_NAN) nans |= 1u << key;
-                if (key0 + key >= kvlen || (byte & 0x7fu) == E4M3_NAN) x.vs &= ~(0xffu << (8 * i));
+                const uint32_t key = 4 * i + c;
+                const bool nan = (vs[i] & 0x7fu) == E4M3_NAN;
+                if (key0 + key < kvlen && nan) nans |= 1u << key;
+                if (key0 + key >= kvlen || nan) vs[i] = 0;
             }
             nans |= __shfl_xor_sync(0xffffffffu, nans, 1);
             nans |= __shfl_xor_sync(0xffffffffu, nans, 2);
         }
-        const uint32_t s01 = e4m3_f16x2(x.vs & 0xffffu), s23 = e4m3_f16x2(x.vs >> 16);
-        const uint32_t *v0 = reinterpret_cast<const uint32_t *>(&x.v[0]), *v1 = reinterpret_cast<const uint32_t *>(&x.v[1]), *v2 = reinterpret_cast<const uint32_t *>(&x.v[2]),
-                       *v3 = reinterpret_cast<const uint32_t *>(&x.v[3]);
+        vs01 = e4m3_f16x2(vs[0] | vs[1] << 8); vs23 = e4m3_f16x2(vs[2] | vs[3] << 8);
 #pragma unroll
         for (int w = 0; w < KS / 4; ++w) {
             // bytes that hold the same dimension of two keys, of even dimensions and of odd ones
             constexpr uint32_t LO = 0x0f0f0f0fu;
-            const uint32_t e01 = (v0[w] & LO) | (v1[w] << 4 & ~LO), d01 = (v0[w] >> 4 & LO) | (v1[w] & ~LO);
-            const uint32_t e23 = (v2[w] & LO) | (v3[w] << 4 & ~LO), d23 = (v2[w] >> 4 & LO) | (v3[w] & ~LO);
+            const uint32_t e01 = (vw[0][w] & LO) | (vw[1][w] << 4 & ~LO), d01 = (vw[0][w] >> 4 & LO) | (vw[1][w] & ~LO);
+            const uint32_t e23 = (vw[2][w] & LO) | (vw[3][w] << 4 & ~LO), d23 = (vw[2][w] >> 4 & LO) | (vw[3][w] & ~LO);
 #define TGP_Q4_PV(I) do { \
-                const uint32_t a0 = mul2(e2m1_f16x2<I>(e01), s01), a1 = mul2(e2m1_f16x2<I>(d01), s01), a2 = mul2(e2m1_f16x2<I>(e23), s23), a3 = mul2(e2m1_f16x2<I>(d23), s23); \
+                const uint32_t a0 = mul2(e2m1_f16x2<I>(e01), vs01), a1 = mul2(e2m1_f16x2<I>(d01), vs01), a2 = mul2(e2m1_f16x2<I>(e23), vs23), a3 = mul2(e2m1_f16x2<I>(d23), vs23); \
                 _Pragma("unroll") for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + I], a0, a1, a2, a3, pb[nt][0], pb[nt][1]); } while (0)
             TGP_Q4_PV(0); TGP_Q4_PV(1); TGP_Q4_PV(2); TGP_Q4_PV(3);
 #undef TGP_Q4_PV
@@ -414,23 +440,18 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
                 }
         }
     };
-    if (next < q_hi) {
-        Chunk<DH> x, y;
-        uint32_t q = next;
-        load(x);
-        while (true) {
-            const bool second = next < q_hi;
-            if (second) load(y);
-            attend(x, q * KEYS);
-            if (!second) break;
-            q += WARPS;
-            const bool third = next < q_hi;
-            if (third) load(x);
-            attend(y, q * KEYS);
-            if (!third) break;
-            q += WARPS;
-        }
+#pragma unroll
+    for (int i = 0; i < STAGES<DH> - 1; ++i) request();
+    uint32_t at = ring;
+    for (uint32_t q = q_lo + warp; q < q_hi; q += WARPS) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES<DH> - 2) : "memory");
+        __syncwarp();                                             // this chunk has landed, and every lane is done with the one before, whose stage is filled next
+        request();
+        attend(at, q * KEYS);
+        at = at + St::BYTES == ring + STAGES<DH> * St::BYTES ? ring : at + St::BYTES;
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
 
     // ---- the warps' partial results meet ----
 #pragma unroll
@@ -522,7 +543,14 @@ uint32_t parts_limit(const tgp_model_cfg *c, uint32_t B, uint32_t kvlen) {
 template <int DH>
 int launch_attn(const AttnQ4Args &a, uint32_t B, cudaStream_t st) {
     const dim3 grid(a.parts, a.Hkv * a.row_blocks, B);
-    int rc = a.rows <= 8 ? launch(tgp_attn_q4_kernel<DH, 1>, grid, dim3(WARPS * 32), 0, st, 1, a) : launch(tgp_attn_q4_kernel<DH, 2>, grid, dim3(WARPS * 32), 0, st, 1, a);
+    int rc;
+    if (a.rows <= 8) {
+        if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, 1>>(attn_smem<DH>(1), true)) return TGP_E_CUDA;
+        rc = launch(tgp_attn_q4_kernel<DH, 1>, grid, dim3(WARPS * 32), attn_smem<DH>(1), st, 1, a);
+    } else {
+        if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, 2>>(attn_smem<DH>(2), true)) return TGP_E_CUDA;
+        rc = launch(tgp_attn_q4_kernel<DH, 2>, grid, dim3(WARPS * 32), attn_smem<DH>(2), st, 1, a);
+    }
     if (rc || a.parts == 1) return rc;
     return launch(tgp_attn_q4_merge_kernel<DH>, dim3(a.rows, a.Hkv, B), dim3(DH), 0, st, 1, a);
 }
