@@ -19,7 +19,7 @@ namespace {
 
 using namespace tgp_launch;
 typedef __nv_bfloat16 bf16;
-constexpr uint32_t KEYS = 16;                    // positions of a chunk, the unit of work of a warp; a tile holds whole chunks
+constexpr uint32_t KEYS = 16;                    // positions that an MMA of the attention takes; a tile holds whole ones
 constexpr uint32_t E4M3_NAN = 0x7f;
 
 __device__ __host__ constexpr uint32_t row_codes(uint32_t Dh) { return Dh / 2; }
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(256) tgp_kv_unpack_q4_kernel(const UnpackArgs 
 // S leaves the MMA with a key per lane row, P enters the next with a key per register pair: two 8 x 8 transposes (movmatrix) of P in fp16.
 struct AttnQ4Args {
     const bf16 *qb; bf16 *ob; float *scratch; const int32_t *pos;
-    uint32_t Hq, Hkv, G, TK, q_len, pos0, rows, row_blocks, parts, per_part;
+    uint32_t Hq, Hkv, G, TK, q_len, pos0, rows, row_blocks, parts, per_part, chunk;      // chunk: keys of one, 16 or 32; per_part: chunks
     float qk, v_up;                                              // score = q k * qk in units of log2; 2^v_exp
     TgpTilePtrs tiles;
 };
@@ -206,16 +206,16 @@ constexpr float BELOW = 6.f, ABOVE = 14.f;
 
 // A chunk in shared memory: codes of its keys, codes of its values, scales of both.  A 16-byte piece of a row lies where neither the copies in nor the loads of
 // eight lanes at a time meet another in a bank: K is read four pieces of rows q and q + 4 at a time, V two pieces of four neighbouring rows.
-template <int DH> struct Stage {
-    static constexpr uint32_t CODES = row_codes(DH), SCALES = row_scales(DH), V = KEYS * CODES, KS = 2 * V, VS = KS + KEYS * SCALES, BYTES = VS + KEYS * SCALES;
+template <int DH, int U> struct Stage {
+    static constexpr uint32_t CODES = row_codes(DH), SCALES = row_scales(DH), V = U * KEYS * CODES, KS = 2 * V, VS = KS + U * KEYS * SCALES, BYTES = VS + U * KEYS * SCALES;
     static __device__ __forceinline__ uint32_t at(uint32_t row, uint32_t piece) {
         if constexpr (DH == 128) return (row >> 1) * 128 + (((row ^ row >> 2) & 1) * 4 + (piece ^ (row & 2))) * 16;
         else return (row >> 2) * 128 + (((row & 3) * 2 + piece) ^ (row & 4)) * 16;
     }
 };
-template <int DH> constexpr int STAGES = DH == 128 ? 5 : 6;
-template <int DH> constexpr uint32_t attn_smem(int NT) {
-    const uint32_t ring = WARPS * STAGES<DH> * Stage<DH>::BYTES, partial = WARPS * 8 * NT * (DH + 4 + 2) * 4;
+template <int DH, int U> constexpr int STAGES = U == 2 ? (DH == 128 ? 3 : 4) : DH == 128 ? 5 : 6;
+template <int DH, int NT, int U> constexpr uint32_t attn_smem() {
+    const uint32_t ring = WARPS * STAGES<DH, U> * Stage<DH, U>::BYTES, partial = WARPS * 8 * NT * (DH + 4 + 2) * 4;
     return ring > partial ? ring : partial;
 }
 
@@ -231,12 +231,13 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     return d;
 }
 
-template <int DH, int NT>
-__global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Args a) {
+template <int DH, int NT, int U>
+__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kernel(const AttnQ4Args a) {
     pdl_enter();
     constexpr int KS = DH / 16;                                   // MMAs of either product
-    constexpr uint32_t RB = 8 * NT, LD = DH + 4, CODES = row_codes(DH), SCALES = row_scales(DH);
-    using St = Stage<DH>;
+    constexpr uint32_t RB = 8 * NT, LD = DH + 4, CODES = row_codes(DH), SCALES = row_scales(DH), CHUNK = U * KEYS;
+    using St = Stage<DH, U>;
+    constexpr uint32_t RING = STAGES<DH, U> * St::BYTES;
     extern __shared__ __align__(128) uint8_t q4_sm[];
     float (*part_o)[RB][LD] = reinterpret_cast<float (*)[RB][LD]>(q4_sm);                                  // (of the warps, when the chunks are done)
     float (*part_ml)[RB][2] = reinterpret_cast<float (*)[RB][2]>(q4_sm + sizeof(float) * WARPS * RB * LD);
@@ -254,7 +255,8 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
     }
     // keys that this block's rows see: the last row's; the first row's tells from where on a chunk has masked ones
     const uint32_t lim_first = (uint32_t)first + row0 / a.G, kvlen = (uint32_t)first + (row0 + nrows - 1) / a.G + 1;
-    const uint32_t nchunks = (kvlen + KEYS - 1) / KEYS, q_lo = min(nchunks, part * a.per_part), q_hi = min(nchunks, q_lo + a.per_part);
+    const uint32_t nchunks = (kvlen + CHUNK - 1) / CHUNK, p_lo = min(nchunks, part * a.per_part), p_n = min(nchunks - p_lo, a.per_part);
+    const uint32_t q_lo = p_lo + p_n * warp / WARPS, q_hi = p_lo + p_n * (warp + 1) / WARPS;          // this warp's chunks
 
     // ---- the rows of Q: fp16 has fewer exponents than bf16, so each row is scaled to [1, 2) by a power of two, which its scores get back ----
     uint32_t qf[NT][KS][2];
@@ -285,34 +287,41 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const uint32_t ee = __shfl_sync(0xffffffffu, e, (2 * c + i) * 4);
-            fix[nt][i] = a.qk * __uint_as_float(ee << 23);
+            fix[nt][i] = fminf(fmaxf(a.qk * __uint_as_float(ee << 23), FLT_MIN), FLT_MAX);      // (neither 0 nor infinite: a masked score is -inf, a zero one 0)
             lim[nt][i] = (uint32_t)first + min(row0 + nt * 8 + 2 * c + i, a.rows - 1) / a.G;
         }
     }
 
-    // ---- chunks q_lo + warp, q_lo + warp + WARPS, ... ----
+    // ---- chunks of 16 or 32 keys (32 where a tile holds whole ones), requested STAGES - 1 ahead; the addresses of a lane's pieces run along a tile ----
     const uint64_t page = ((uint64_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
-    const uint32_t krow = (r & 1) * 4 + (r >> 1), ring = (uint32_t)__cvta_generic_to_shared(q4_sm) + warp * STAGES<DH> * St::BYTES;
-    uint32_t next = q_lo + warp, tile = next * KEYS / a.TK, off = next * KEYS - tile * a.TK, fill = ring;      // the chunk that is requested next, and its stage
-    const uint32_t lane_at = St::at(lane / (CODES / 16), lane % (CODES / 16)), lane_scale = (lane % KEYS) * 16;
+    const uint32_t krow = (r & 1) * 4 + (r >> 1), ring = (uint32_t)__cvta_generic_to_shared(q4_sm) + warp * RING;
+    constexpr uint32_t SC = U * SCALES;                          // 16-byte pieces of a chunk's scales, for the keys; as many lanes bring them, and as many those of the values
+    const uint32_t lane_at = St::at(lane / (CODES / 16), lane % (CODES / 16)), lane_scale = St::KS + lane * 16;
+    uint32_t left = q_hi - q_lo, tile = q_lo * CHUNK / a.TK, off = q_lo * CHUNK - tile * a.TK, fill = ring;
+    const uint8_t *kp = nullptr, *vp = nullptr, *sp = nullptr;
+    auto enter = [&]() {                                          // the lane's pieces of the chunk at `off` in `tile`
+        const uint8_t *k = reinterpret_cast<const uint8_t *>(a.tiles.k[tile]) + page, *v = reinterpret_cast<const uint8_t *>(a.tiles.v[tile]) + page;
+        kp = k + off * CODES + lane * 16;
+        vp = v + off * CODES + lane * 16;
+        sp = (lane < SC ? k : v) + a.TK * CODES + off * SCALES + (lane % SC) * 16;
+    };
+    if (left) enter();
     auto request = [&]() {
-        if (next < q_hi) {
-            const uint8_t *kp = reinterpret_cast<const uint8_t *>(a.tiles.k[tile]) + page, *vp = reinterpret_cast<const uint8_t *>(a.tiles.v[tile]) + page;
+        if (left) {
 #pragma unroll
-            for (uint32_t i = 0; i < KEYS * CODES / 512; ++i) {       // (eight rows further on in the swizzle is 8 * CODES bytes)
-                cp_async16(fill + lane_at + i * 512, kp + off * CODES + i * 512 + lane * 16);
-                cp_async16(fill + St::V + lane_at + i * 512, vp + off * CODES + i * 512 + lane * 16);
+            for (uint32_t i = 0; i < CHUNK * CODES / 512; ++i) {      // (512 bytes are a multiple of eight rows, which the swizzle does not look at)
+                cp_async16(fill + lane_at + i * 512, kp + i * 512);
+                cp_async16(fill + St::V + lane_at + i * 512, vp + i * 512);
             }
-            if (lane < 2 * SCALES) {
-                const uint8_t *from = lane < SCALES ? kp : vp;
-                cp_async16(fill + St::KS + lane_scale, from + a.TK * CODES + off * SCALES + (lane % SCALES) * 16);
+            if (lane < 2 * SC) cp_async16(fill + lane_scale, sp);
+            off += CHUNK;
+            if (--left) {
+                if (off < a.TK) { kp += CHUNK * CODES; vp += CHUNK * CODES; sp += CHUNK * SCALES; }
+                else { off = 0; ++tile; enter(); }
             }
-            next += WARPS;
-            off += WARPS * KEYS;
-            while (off >= a.TK) { off -= a.TK; ++tile; }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        fill = fill + St::BYTES == ring + STAGES<DH> * St::BYTES ? ring : fill + St::BYTES;
+        fill = fill + St::BYTES == ring + RING ? ring : fill + St::BYTES;
     };
     float o[NT][KS][4], m_ref[NT][2], l[NT][2];
 #pragma unroll
@@ -324,60 +333,67 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
     }
     auto attend = [&](uint32_t at, uint32_t key0) {
         const uint8_t *st = q4_sm + (at - (uint32_t)__cvta_generic_to_shared(q4_sm));
-        const bool masked = key0 + KEYS - 1 > lim_first;          // some row does not see all of the chunk
-        uint32_t kw[2][DH / 32], vw[4][DH / 64], vs01, vs23;
+        const bool masked = key0 + CHUNK - 1 > lim_first;         // some row does not see all of the chunk
+        float s[U][NT][4];
 #pragma unroll
-        for (uint32_t h = 0; h < 2; ++h) {
-            const uint8_t *from = st + h * 8 * CODES + (DH == 128 ? St::at(krow, c) : St::at(krow, c >> 1) + (c & 1) * 8);
-            if constexpr (DH == 128) { const uint4 w = *reinterpret_cast<const uint4 *>(from); kw[h][0] = w.x; kw[h][1] = w.y; kw[h][2] = w.z; kw[h][3] = w.w; }
-            else { const uint2 w = *reinterpret_cast<const uint2 *>(from); kw[h][0] = w.x; kw[h][1] = w.y; }
-        }
-        // ---- S = K Q^T ----
-        float s[NT][4];
+        for (int u = 0; u < U; ++u) {
+            // ---- S = K Q^T ----
+            uint32_t kw[2][DH / 32];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-        uint32_t sc[2][2];                                        // scales of the two keys, of the first and the second half of the lane's dimensions
+            for (uint32_t h = 0; h < 2; ++h) {
+                const uint8_t *from = st + (u * 2 + h) * 8 * CODES + (DH == 128 ? St::at(krow, c) : St::at(krow, c >> 1) + (c & 1) * 8);
+                if constexpr (DH == 128) { const uint4 w = *reinterpret_cast<const uint4 *>(from); kw[h][0] = w.x; kw[h][1] = w.y; kw[h][2] = w.z; kw[h][3] = w.w; }
+                else { const uint2 w = *reinterpret_cast<const uint2 *>(from); kw[h][0] = w.x; kw[h][1] = w.y; }
+            }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint8_t *from = st + St::KS + (h * 8 + krow) * SCALES;
-            if constexpr (DH == 128) {
-                const uint32_t f = e4m3_f16x2(*reinterpret_cast<const uint16_t *>(from + 2 * c));
-                sc[h][0] = __byte_perm(f, f, 0x1010);
-                sc[h][1] = __byte_perm(f, f, 0x3232);
-            } else sc[h][0] = sc[h][1] = e4m3_f16x2(from[c] * 0x101u);
-        }
+            for (int nt = 0; nt < NT; ++nt) s[u][nt][0] = s[u][nt][1] = s[u][nt][2] = s[u][nt][3] = 0.f;
+            uint32_t sc[2][2];                                    // scales of the two keys, of the first and the second half of the lane's dimensions
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int half = DH == 128 ? ks / 4 : 0;
-            const uint32_t w0 = kw[0][ks / 2], w1 = kw[1][ks / 2];
-            const uint32_t a0 = mul2(ks & 1 ? e2m1_f16x2<2>(w0) : e2m1_f16x2<0>(w0), sc[0][half]), a1 = mul2(ks & 1 ? e2m1_f16x2<2>(w1) : e2m1_f16x2<0>(w1), sc[1][half]);
-            const uint32_t a2 = mul2(ks & 1 ? e2m1_f16x2<3>(w0) : e2m1_f16x2<1>(w0), sc[0][half]), a3 = mul2(ks & 1 ? e2m1_f16x2<3>(w1) : e2m1_f16x2<1>(w1), sc[1][half]);
+            for (int h = 0; h < 2; ++h) {
+                const uint8_t *from = st + St::KS + ((u * 2 + h) * 8 + krow) * SCALES;
+                if constexpr (DH == 128) {
+                    const uint32_t f = e4m3_f16x2(*reinterpret_cast<const uint16_t *>(from + 2 * c));
+                    sc[h][0] = __byte_perm(f, f, 0x1010);
+                    sc[h][1] = __byte_perm(f, f, 0x3232);
+                } else sc[h][0] = sc[h][1] = e4m3_f16x2(from[c] * 0x101u);
+            }
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_f16(s[nt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
+            for (int ks = 0; ks < KS; ++ks) {
+                const int half = DH == 128 ? ks / 4 : 0;
+                const uint32_t w0 = kw[0][ks / 2], w1 = kw[1][ks / 2];
+                const uint32_t a0 = mul2(ks & 1 ? e2m1_f16x2<2>(w0) : e2m1_f16x2<0>(w0), sc[0][half]), a1 = mul2(ks & 1 ? e2m1_f16x2<2>(w1) : e2m1_f16x2<0>(w1), sc[1][half]);
+                const uint32_t a2 = mul2(ks & 1 ? e2m1_f16x2<3>(w0) : e2m1_f16x2<1>(w0), sc[0][half]), a3 = mul2(ks & 1 ? e2m1_f16x2<3>(w1) : e2m1_f16x2<1>(w1), sc[1][half]);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(s[u][nt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
+            }
+            if (masked) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) if (key0 + u * KEYS + krow + (i & 2) * 4 > lim[nt][i & 1]) s[u][nt][i] = -INFINITY;       // (fix > 0)
+            }
         }
         // ---- softmax weights: the reference of a row lies BELOW under its largest score when it moves, and moves when a score is more than ABOVE over it.  Weights
         // are below 2^ABOVE then, which fp16 holds, and what it rounds to multiples of 2^-24 is less than 2^-(BELOW + 14) of the largest ----
-        uint32_t pb[NT][2];
-        bool grown = false;
+        uint32_t pb[U][NT][2];
+        float top = -INFINITY;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v = s[nt][i] * fix[nt][i & 1];
-                if (masked && key0 + krow + (i & 2) * 4 > lim[nt][i & 1]) v = -INFINITY;
-                s[nt][i] = v;
-                grown |= v > m_ref[nt][i & 1] + ABOVE;
-            }
-        if (__any_sync(0xffffffffu, grown)) {
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaf(s[u][nt][i], fix[nt][i & 1], -m_ref[nt][i & 1]));
+        if (__any_sync(0xffffffffu, top > ABOVE)) {
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float mx = fmaxf(s[nt][i], s[nt][i + 2]);
+                    float mx = fmaxf(s[0][nt][i], s[0][nt][i + 2]);
+                    if constexpr (U == 2) mx = fmaxf(mx, fmaxf(s[U - 1][nt][i], s[U - 1][nt][i + 2]));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                     mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float m_new = fmaxf(m_ref[nt][i], mx - BELOW), alpha = ex2(m_ref[nt][i] - m_new);
+                    const float m_new = fmaxf(m_ref[nt][i], mx * fix[nt][i] - BELOW), alpha = ex2(m_ref[nt][i] - m_new);
                     m_ref[nt][i] = m_new;
                     l[nt][i] *= alpha;
 #pragma unroll
@@ -385,70 +401,75 @@ __global__ void __launch_bounds__(WARPS * 32) tgp_attn_q4_kernel(const AttnQ4Arg
                 }
         }
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float p[4];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = ex2(s[nt][i] - m_ref[nt][i & 1]);
-            l[nt][0] += p[0] + p[2];
-            l[nt][1] += p[1] + p[3];
-            pb[nt][0] = transpose8(pack_f16(p[0], p[1]));
-            pb[nt][1] = transpose8(pack_f16(p[2], p[3]));
-        }
+            for (int nt = 0; nt < NT; ++nt) {
+                float p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[i] = ex2(fmaf(s[u][nt][i], fix[nt][i & 1], -m_ref[nt][i & 1]));
+                l[nt][0] += p[0] + p[2];
+                l[nt][1] += p[1] + p[3];
+                pb[u][nt][0] = transpose8(pack_f16(p[0], p[1]));
+                pb[u][nt][1] = transpose8(pack_f16(p[2], p[3]));
+            }
         // ---- O^T += V^T P^T ----
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            const uint8_t *from = st + St::V + (DH == 128 ? St::at(4 * i + c, r >> 1) + (r & 1) * 8 : St::at(4 * i + c, r >> 2) + (r & 3) * 4);
-            if constexpr (DH == 128) { const uint2 w = *reinterpret_cast<const uint2 *>(from); vw[i][0] = w.x; vw[i][1] = w.y; }
-            else vw[i][0] = *reinterpret_cast<const uint32_t *>(from);
-        }
-        uint32_t vs[4], nans = 0;                                 // nans: keys of the chunk whose group of this lane's dimensions stands for NaN
+        for (int u = 0; u < U; ++u) {
+            uint32_t vw[4][DH / 64], vs[4], nans = 0;             // nans: keys whose group of this lane's dimensions stands for NaN
+            const uint32_t base = key0 + u * KEYS;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) vs[i] = st[St::VS + (4 * i + c) * SCALES + (DH == 128 ? r : r / 2)];
-        if (masked) {                                             // behind the sequence: whatever the tile holds there; a row that does not see a NaN must not multiply it by 0
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t key = 4 * i + c;
-                const bool nan = (vs[i] & 0x7fu) == E4M3_NAN;
-                if (key0 + key < kvlen && nan) nans |= 1u << key;
-                if (key0 + key >= kvlen || nan) vs[i] = 0;
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint8_t *from = st + St::V + u * KEYS * CODES + (DH == 128 ? St::at(4 * i + c, r >> 1) + (r & 1) * 8 : St::at(4 * i + c, r >> 2) + (r & 3) * 4);
+                if constexpr (DH == 128) { const uint2 w = *reinterpret_cast<const uint2 *>(from); vw[i][0] = w.x; vw[i][1] = w.y; }
+                else vw[i][0] = *reinterpret_cast<const uint32_t *>(from);
+                vs[i] = st[St::VS + (u * KEYS + 4 * i + c) * SCALES + (DH == 128 ? r : r / 2)];
             }
-            nans |= __shfl_xor_sync(0xffffffffu, nans, 1);
-            nans |= __shfl_xor_sync(0xffffffffu, nans, 2);
-        }
-        vs01 = e4m3_f16x2(vs[0] | vs[1] << 8); vs23 = e4m3_f16x2(vs[2] | vs[3] << 8);
+            if (masked) {                                         // behind the sequence: whatever the tile holds there; a row that does not see a NaN must not multiply it by 0
 #pragma unroll
-        for (int w = 0; w < KS / 4; ++w) {
-            // bytes that hold the same dimension of two keys, of even dimensions and of odd ones
-            constexpr uint32_t LO = 0x0f0f0f0fu;
-            const uint32_t e01 = (vw[0][w] & LO) | (vw[1][w] << 4 & ~LO), d01 = (vw[0][w] >> 4 & LO) | (vw[1][w] & ~LO);
-            const uint32_t e23 = (vw[2][w] & LO) | (vw[3][w] << 4 & ~LO), d23 = (vw[2][w] >> 4 & LO) | (vw[3][w] & ~LO);
-#define TGP_Q4_PV(I) do { \
-                const uint32_t a0 = mul2(e2m1_f16x2<I>(e01), vs01), a1 = mul2(e2m1_f16x2<I>(d01), vs01), a2 = mul2(e2m1_f16x2<I>(e23), vs23), a3 = mul2(e2m1_f16x2<I>(d23), vs23); \
-                _Pragma("unroll") for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + I], a0, a1, a2, a3, pb[nt][0], pb[nt][1]); } while (0)
-            TGP_Q4_PV(0); TGP_Q4_PV(1); TGP_Q4_PV(2); TGP_Q4_PV(3);
-#undef TGP_Q4_PV
-        }
-        if (masked && __any_sync(0xffffffffu, nans != 0)) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t seen = lim[nt][i] < key0 ? 0u : lim[nt][i] - key0 >= KEYS - 1 ? 0xffffu : (2u << (lim[nt][i] - key0)) - 1;
-                    if (nans & seen)
-#pragma unroll
-                        for (int j = 0; j < KS; ++j) o[nt][j][i] = o[nt][j][i + 2] = NAN;
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t key = 4 * i + c;
+                    const bool nan = (vs[i] & 0x7fu) == E4M3_NAN;
+                    if (base + key < kvlen && nan) nans |= 1u << key;
+                    if (base + key >= kvlen || nan) vs[i] = 0;
                 }
+                nans |= __shfl_xor_sync(0xffffffffu, nans, 1);
+                nans |= __shfl_xor_sync(0xffffffffu, nans, 2);
+            }
+            const uint32_t vs01 = e4m3_f16x2(vs[0] | vs[1] << 8), vs23 = e4m3_f16x2(vs[2] | vs[3] << 8);
+#pragma unroll
+            for (int w = 0; w < KS / 4; ++w) {
+                // bytes that hold the same dimension of two keys, of even dimensions and of odd ones
+                constexpr uint32_t LO = 0x0f0f0f0fu;
+                const uint32_t e01 = (vw[0][w] & LO) | (vw[1][w] << 4 & ~LO), d01 = (vw[0][w] >> 4 & LO) | (vw[1][w] & ~LO);
+                const uint32_t e23 = (vw[2][w] & LO) | (vw[3][w] << 4 & ~LO), d23 = (vw[2][w] >> 4 & LO) | (vw[3][w] & ~LO);
+#define TGP_Q4_PV(I) do { \
+                    const uint32_t a0 = mul2(e2m1_f16x2<I>(e01), vs01), a1 = mul2(e2m1_f16x2<I>(d01), vs01), a2 = mul2(e2m1_f16x2<I>(e23), vs23), a3 = mul2(e2m1_f16x2<I>(d23), vs23); \
+                    _Pragma("unroll") for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + I], a0, a1, a2, a3, pb[u][nt][0], pb[u][nt][1]); } while (0)
+                TGP_Q4_PV(0); TGP_Q4_PV(1); TGP_Q4_PV(2); TGP_Q4_PV(3);
+#undef TGP_Q4_PV
+            }
+            if (masked && __any_sync(0xffffffffu, nans != 0)) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t seen = lim[nt][i] < base ? 0u : lim[nt][i] - base >= KEYS - 1 ? 0xffffu : (2u << (lim[nt][i] - base)) - 1;
+                        if (nans & seen)
+#pragma unroll
+                            for (int j = 0; j < KS; ++j) o[nt][j][i] = o[nt][j][i + 2] = NAN;
+                    }
+            }
         }
     };
 #pragma unroll
-    for (int i = 0; i < STAGES<DH> - 1; ++i) request();
+    for (int i = 0; i < STAGES<DH, U> - 1; ++i) request();
     uint32_t at = ring;
-    for (uint32_t q = q_lo + warp; q < q_hi; q += WARPS) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES<DH> - 2) : "memory");
+    for (uint32_t q = q_lo; q < q_hi; ++q) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES<DH, U> - 2) : "memory");
         __syncwarp();                                             // this chunk has landed, and every lane is done with the one before, whose stage is filled next
         request();
-        attend(at, q * KEYS);
-        at = at + St::BYTES == ring + STAGES<DH> * St::BYTES ? ring : at + St::BYTES;
+        attend(at, q * CHUNK);
+        at = at + St::BYTES == ring + RING ? ring : at + St::BYTES;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();
@@ -495,7 +516,7 @@ __global__ void __launch_bounds__(DH) tgp_attn_q4_merge_kernel(const AttnQ4Args 
     const uint32_t row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, d = threadIdx.x, t = row / a.G;
     const int first = position_of(a.pos, b, a.pos0);
     if (first < 0) return;                                        // (written by the kernel before)
-    const uint32_t nchunks = ((uint32_t)first + t + KEYS) / KEYS, parts = (nchunks + a.per_part - 1) / a.per_part;      // those that have a key of this row
+    const uint32_t nchunks = ((uint32_t)first + t + a.chunk) / a.chunk, parts = (nchunks + a.per_part - 1) / a.per_part;      // those that have a key of this row
     const float *from = a.scratch + (((size_t)b * a.Hkv + hk) * a.rows + row) * a.parts * (DH + 2);
     float M = -FLT_MAX, sum = 0.f, acc = 0.f;
     for (uint32_t p = 0; p < parts; ++p) M = fmaxf(M, from[p * (DH + 2)]);
@@ -540,19 +561,19 @@ uint32_t parts_limit(const tgp_model_cfg *c, uint32_t B, uint32_t kvlen) {
     return std::max(1u, std::min({PARTS_MAX, (kvlen + 127) / 128, UNITS_MAX / std::max(1u, B * c->Hkv)}));
 }
 
-template <int DH>
+template <int DH, int NT, int U>
 int launch_attn(const AttnQ4Args &a, uint32_t B, cudaStream_t st) {
-    const dim3 grid(a.parts, a.Hkv * a.row_blocks, B);
-    int rc;
-    if (a.rows <= 8) {
-        if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, 1>>(attn_smem<DH>(1), true)) return TGP_E_CUDA;
-        rc = launch(tgp_attn_q4_kernel<DH, 1>, grid, dim3(WARPS * 32), attn_smem<DH>(1), st, 1, a);
-    } else {
-        if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, 2>>(attn_smem<DH>(2), true)) return TGP_E_CUDA;
-        rc = launch(tgp_attn_q4_kernel<DH, 2>, grid, dim3(WARPS * 32), attn_smem<DH>(2), st, 1, a);
-    }
+    constexpr uint32_t smem = attn_smem<DH, NT, U>();
+    if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U>>(smem, true)) return TGP_E_CUDA;
+    const int rc = launch(tgp_attn_q4_kernel<DH, NT, U>, dim3(a.parts, a.Hkv * a.row_blocks, B), dim3(WARPS * 32), smem, st, 1, a);
     if (rc || a.parts == 1) return rc;
     return launch(tgp_attn_q4_merge_kernel<DH>, dim3(a.rows, a.Hkv, B), dim3(DH), 0, st, 1, a);
+}
+
+template <int DH>
+int launch_attn(const AttnQ4Args &a, uint32_t B, cudaStream_t st) {
+    if (a.chunk == 2 * KEYS) return a.rows <= 8 ? launch_attn<DH, 1, 2>(a, B, st) : launch_attn<DH, 2, 2>(a, B, st);
+    return a.rows <= 8 ? launch_attn<DH, 1, 1>(a, B, st) : launch_attn<DH, 2, 1>(a, B, st);
 }
 
 uint32_t few_parts(const tgp_model_cfg *c, uint32_t B, uint32_t row_blocks, uint32_t kvlen, bool ragged) {
@@ -627,8 +648,9 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
     if (few(cfg, q_len)) {
         const uint32_t rows = q_len * G, rb = rows <= 8 ? 8 : 16, row_blocks = (rows + rb - 1) / rb;
         if ((uint64_t)cfg->Hkv * row_blocks > 65535u || rows > 65535u || B > 65535u) return TGP_E_TOO_LARGE;
-        const uint32_t nchunks = (kvlen + KEYS - 1) / KEYS, parts = few_parts(cfg, B, row_blocks, kvlen, pos_dev != nullptr), per = (nchunks + parts - 1) / parts;
-        AttnQ4Args a{(const bf16 *)qb, (bf16 *)ob, (float *)scratch_dev, pos_dev, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, rows, row_blocks, (nchunks + per - 1) / per, per,
+        const uint32_t chunk = cfg->TK % (2 * KEYS) ? KEYS : 2 * KEYS, nchunks = (kvlen + chunk - 1) / chunk;
+        const uint32_t parts = few_parts(cfg, B, row_blocks, kvlen, pos_dev != nullptr), per = (nchunks + parts - 1) / parts;
+        AttnQ4Args a{(const bf16 *)qb, (bf16 *)ob, (float *)scratch_dev, pos_dev, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, rows, row_blocks, (nchunks + per - 1) / per, per, chunk,
                      ldexpf(1.4426950408889634f / sqrtf((float)cfg->Dh), k_exp), ldexpf(1.f, v_exp), tiles};
         return cfg->Dh == 64 ? launch_attn<64>(a, B, st) : launch_attn<128>(a, B, st);
     }
