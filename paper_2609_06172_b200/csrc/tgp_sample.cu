@@ -1,12 +1,17 @@
 // The next token of every sequence by temperature, top-k, top-p and min-p from a given random number.
 //
 // Tokens are ordered by logit, the lower index first of equals; each filter keeps a beginning of that order, so what is kept is everything above
-// a logit t and the first so many of those equal to t.  Nothing is sorted: t is found by histograms that narrow the bin in which it lies -
-// first 2047 bins of 1 / 64 in (max - logit) / temperature, then equal ranges of the logits' bits, each 2048 times finer.
+// a logit t and the first so many of those equal to t.
 // A token weighs exp((logit - max) / temperature) as a whole number of 2^-44: sums of whole numbers are exact in any order, so the result does not
 // depend on which thread adds first, and what is drawn is what sums in 64-bit floating point would draw but for borders nearer than
 // about 1e-10 of the sum.  Tokens that round to 0 (31 below the maximum, in units of the temperature) are never drawn.
-// A row belongs to a cluster of CTAs, each with a contiguous part of it; histograms and sums meet through distributed shared memory.
+// A row belongs to a cluster of CTAs, each with a contiguous part of it, which is read once per step from memory, then from L2; histograms, lists and sums
+// meet through distributed shared memory.  Steps, after the maximum:
+//   top-k of a few hundred: the k-th largest of the threads' own maxima is a lower bound of the k-th largest logit.  What is not below its bin is a list
+//     of little more than k tokens, which the first CTA sorts; it finishes the row by itself, and only these tokens' weights are ever computed;
+//   else top-p: a histogram of the weights over 2047 bins of 1 / 64 in (max - logit) / temperature tells the bin in which t lies; its tokens are such a list;
+//   where a list would be too long (equal logits, a large top-k): further histograms, each 2048 times finer in the logits' bits, down to one value;
+//   the draw: sums of the kept weights by warp, in the order of the tokens, and the one segment that the random number falls into once more.
 #include <cuda_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -19,7 +24,7 @@ namespace {
 using namespace tgp_launch;
 
 constexpr int THREADS = 512, NW = THREADS / 32;
-constexpr uint32_t BINS = 2048, CLUSTER_MAX = 8;
+constexpr uint32_t BINS = 2048, CLUSTER_MAX = 8, LIST = 2048;
 constexpr double ONE = 17592186044416.0;                        // 2^44, the weight of the maximum
 typedef unsigned long long u64;
 
@@ -31,6 +36,9 @@ struct SampleArgs {
 // what the cluster's CTAs share lies in the first one
 struct Shared {
     uint32_t cnt[BINS], lo[BINS], hi[BINS];                      // histogram of the CTA's part: tokens, and their weight in two words
+    u64 list[LIST]; u64 sums[LIST];                              // tokens as key << 32 | ~index, and sums of their weights (first CTA)
+    double octave[32];                                           // 2^(i / 32)
+    uint32_t listed;
     uint32_t all_cnt[BINS]; u64 all_w[BINS];                     // of the row (first CTA)
     float top[CLUSTER_MAX]; uint32_t top_i[CLUSTER_MAX];         // the parts' maxima (first CTA)
     u64 seg_w[CLUSTER_MAX * NW]; uint32_t seg_t[CLUSTER_MAX * NW];      // the warps' sums and ties (first CTA)
@@ -47,6 +55,8 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_arrive() { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t in_cta(const void *p, uint32_t rank) {
     uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
@@ -55,6 +65,8 @@ __device__ __forceinline__ uint32_t in_cta(const void *p, uint32_t rank) {
 __device__ __forceinline__ uint32_t get32(const uint32_t *p, uint32_t rank) { uint32_t v; asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(in_cta(p, rank)) : "memory"); return v; }
 __device__ __forceinline__ void put32(uint32_t *p, uint32_t rank, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(p, rank)), "r"(v) : "memory"); }
 __device__ __forceinline__ void put64(u64 *p, uint32_t rank, u64 v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_cta(p, rank)), "l"(v) : "memory"); }
+
+__device__ __forceinline__ uint32_t add32(uint32_t *p, uint32_t rank, uint32_t v) { uint32_t old; asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(in_cta(p, rank)), "r"(v) : "memory"); return old; }
 
 template <typename T> __device__ __forceinline__ T warp_total(T v) {
 #pragma unroll
@@ -76,18 +88,47 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k &
 
 struct Row {
     float top, step;                                             // the maximum; 64 / temperature
-    double inv;                                                  // 1 / temperature
+    double top64, rate;                                          // 32 log2(e) / temperature
+    const double *octave;
     // bin of a logit that is no NaN and above -inf; BINS - 1 and more weigh nothing
     __device__ __forceinline__ uint32_t bin(float x) const {
         if (x == top) return 0;
         const float z = (top - x) * step;
         return z < (float)(BINS - 1) ? (uint32_t)z : BINS - 1;   // (a NaN: infinity times 0)
     }
-    __device__ __forceinline__ double weight(float x) const { return x == top ? 1.0 : exp(((double)x - (double)top) * inv); }
+    // The weight of a logit of a bin below BINS - 1: with t = 32 log2(e) (x - top) / temperature = n + f, |f| <= 1/2, it is 2^(n / 32) exp(f ln2 / 32), the latter by its
+    // series, whose sixth power is below 2^-48, the former from a table of 2^(i / 32).  Off by a few units of 2^-52 besides.
+    __device__ __forceinline__ u64 weight(float x) const {
+        constexpr double MAGIC = 6755399441055744.0;             // 1.5 * 2^52: a number plus this has its nearest integer in its low bits
+        constexpr double C = 0.021660849392498290;               // ln2 / 32
+        const double t = x == top ? 0.0 : ((double)x - top64) * rate, m = t + MAGIC, f = t - (m - MAGIC);
+        const int n = __double2loint(m);
+        double p = fma(f, C * C * C * C * C / 120, C * C * C * C / 24);
+        p = fma(f, p, C * C * C / 6);
+        p = fma(f, p, C * C / 2);
+        p = fma(f, p, C);
+        p = fma(f, p, 1.0);
+        const double o = octave[n & 31];
+        const double scale = __hiloint2double(__double2hiint(o) + ((n >> 5) + 44) * (1 << 20), __double2loint(o));
+        return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xfffffffffffffull;          // 2^52 puts the point behind the last bit
+    }
 };
-__device__ __forceinline__ u64 whole(double w) { return (u64)__double_as_longlong(fma(w, ONE, 4503599627370496.0)) & 0xfffffffffffffull; }      // 2^52 puts the point behind the last bit
 
-__global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a) {
+// Sorts the first n (a power of two) of a list, the largest first; all threads of the CTA.
+__device__ __forceinline__ void sort_list(u64 *list, uint32_t n) {
+    for (uint32_t k = 2; k <= n; k <<= 1)
+        for (uint32_t j = k >> 1; j; j >>= 1) {
+            __syncthreads();
+            for (uint32_t i = threadIdx.x; i < n / 2; i += THREADS) {
+                const uint32_t x = 2 * i - (i & (j - 1)), y = x + j;
+                const u64 p = list[x], q = list[y];
+                if ((p < q) == ((x & k) == 0)) { list[x] = q; list[y] = p; }
+            }
+        }
+    __syncthreads();
+}
+
+__global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs a) {
     pdl_enter();
     extern __shared__ __align__(16) uint8_t sample_sm[];
     Shared &sh = *reinterpret_cast<Shared *>(sample_sm);
@@ -98,58 +139,187 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
     const float *row = a.logits + (size_t)b * a.V;
     const uint32_t first = min(a.V, rank * a.per), end = min(a.V, first + a.per);
 
+    cluster_arrive();                                            // (the first access to another CTA's memory waits for it to run)
+    if (tid < 32) sh.octave[tid] = exp2((double)tid / 32);
+    if (tid == 0) sh.listed = 0;
+
+    // every logit of this CTA's part once, each thread every THREADS-th, eight loads under way
+    auto each = [&](auto &&f) {
+        uint32_t i = first + tid;
+        for (; i < end && end - i > 7 * THREADS; i += 8 * THREADS) {
+            float x[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * THREADS];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) f(x[j], i + j * THREADS);
+        }
+        for (; i < end; i += THREADS) f(row[i], i);
+    };
+
     // ---- the maximum ----
     Row r;
     uint32_t best;
+    float mine = -INFINITY;                                      // this thread's own
     {
-        float m = -INFINITY;
         uint32_t at = 0;                                         // a row of nothing but -inf and NaN gives token 0, as the argmax does
-        for (uint32_t i = first + tid; i < end; i += THREADS) { const float x = row[i]; if (x > m) { m = x; at = i; } }
+        each([&](float x, uint32_t i) { if (x > mine) { mine = x; at = i; } });
+        float m = mine;
         auto merge = [&](float om, uint32_t oi) { if (om > m || (om == m && oi < at)) { m = om; at = oi; } };
 #pragma unroll
         for (int o = 16; o; o >>= 1) { const float om = __shfl_xor_sync(0xffffffffu, m, o); const uint32_t oi = __shfl_xor_sync(0xffffffffu, at, o); merge(om, oi); }
         if (lane == 0) { sh.warp_m[warp] = m; sh.warp_i[warp] = at; }
-        cluster_sync();                                          // (and all CTAs run)
-        if (tid == 0) {
-            for (int w = 0; w < NW; ++w) merge(sh.warp_m[w], sh.warp_i[w]);
-            put32(reinterpret_cast<uint32_t *>(&sh.top[rank]), 0, __float_as_uint(m));
-            put32(&sh.top_i[rank], 0, at);
+        cluster_wait();
+        __syncthreads();
+        if (warp == 0) {
+            m = lane < NW ? sh.warp_m[lane] : -INFINITY;
+            at = lane < NW ? sh.warp_i[lane] : 0xffffffffu;
+#pragma unroll
+            for (int o = NW / 2; o; o >>= 1) { const float om = __shfl_xor_sync(0xffffffffu, m, o); const uint32_t oi = __shfl_xor_sync(0xffffffffu, at, o); merge(om, oi); }
+            if (lane < parts) { put32(reinterpret_cast<uint32_t *>(&sh.top[rank]), lane, __float_as_uint(m)); put32(&sh.top_i[rank], lane, at); }          // to every CTA
         }
         cluster_sync();
         m = -INFINITY; at = 0;
-        for (uint32_t p = 0; p < parts; ++p) merge(__uint_as_float(get32(reinterpret_cast<const uint32_t *>(&sh.top[p]), 0)), get32(&sh.top_i[p], 0));
+        for (uint32_t p = 0; p < parts; ++p) merge(sh.top[p], sh.top_i[p]);
         r.top = m; best = at;
     }
     const float temperature = a.temperature ? a.temperature[b] : 1.f, min_p = a.min_p ? a.min_p[b] : 0.f, top_p = a.top_p ? a.top_p[b] : 1.f;
     const int32_t top_k = a.top_k ? a.top_k[b] : 0;
-    if (!(temperature > 0.f) || r.top == -INFINITY || min_p > 1.f || top_k == 1) {               // the cluster's CTAs agree
+    if (!(temperature > 0.f) || r.top == -INFINITY || min_p > 1.f || top_k == 1 || top_p <= 0.f) {               // the cluster's CTAs agree
         if (rank == 0 && tid == 0) a.out[b] = (int32_t)best;
-        cluster_sync();
         return;
     }
-    r.inv = 1.0 / (double)temperature;
-    r.step = (float)fmin(64.0 * r.inv, 3.0e38);
+    const double inv = 1.0 / (double)fmaxf(temperature, 7.52316384526264e-37f);        // 2^-120: bins are told in fp32
+    r.rate = inv * 46.166241308446828;                           // 32 log2(e)
+    r.step = (float)(64.0 * inv);
+    r.top64 = (double)r.top;
+    r.octave = sh.octave;
     auto live = [&](float x) { return x > -INFINITY; };
+    const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * ONE) : 0;
+
+    // ---- tokens whose bin is in [z_lo, z_hi] and whose key is not below key_lo as a list in the first CTA; how many there are, LIST at most, or LIST + 1 ----
+    auto gather = [&](uint32_t z_lo, uint32_t z_hi, uint32_t key_lo) {
+        each([&](float x, uint32_t i) {
+            if (!live(x)) return;
+            const uint32_t z = r.bin(x);
+            if (z < z_lo || z > z_hi || key_of(x) < key_lo) return;
+            const uint32_t at = add32(&sh.listed, 0, 1);
+            if (at < LIST) put64(&sh.list[at], 0, (u64)key_of(x) << 32 | (uint32_t)~i);
+        });
+        cluster_sync();
+        return min(get32(&sh.listed, 0), LIST + 1);
+    };
+    // (first CTA) sorts n listed tokens, and gives the running sums of their weights: of their logits, or of the numbers in the low `bits`
+    auto sorted_sums = [&](uint32_t n, uint32_t bits) {
+        uint32_t size = 32;
+        while (size < n) size *= 2;
+        for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
+        sort_list(sh.list, size);
+        u64 before = 0;
+        for (uint32_t i0 = 0; i0 < n; i0 += THREADS) {
+            const uint32_t i = i0 + tid;
+            u64 w = i >= n ? 0 : bits ? sh.list[i] & ((1ull << bits) - 1) : r.weight(of_key((uint32_t)(sh.list[i] >> 32)));
+            w = warp_upto(w);
+            if (lane == 31) sh.warp_w[warp] = w;
+            __syncthreads();
+            u64 all = 0;
+            for (uint32_t v = 0; v < NW; ++v) { if (v < warp) w += sh.warp_w[v]; all += sh.warp_w[v]; }
+            if (i < n) sh.sums[i] = before + w;
+            before += all;
+            __syncthreads();
+        }
+    };
+    const double u = (double)a.u[b];
+    auto draw = [&](u64 sum) { return min(u > 0.0 ? (u64)fmin(u * (double)sum, 9.0e18) : 0ull, sum - 1); };
+    auto share = [&](u64 sum) { return max(1ull, min(sum, (u64)ceil((double)top_p * (double)sum))); };            // top_p of it
+
+    // ---- top-k by the list of what is not below the k-th largest of the threads' maxima ----
+    if (top_k > 0 && (uint32_t)top_k <= min(LIST / 2, parts * THREADS) && (uint32_t)top_k < a.V) {
+        for (uint32_t i = tid; i < BINS; i += THREADS) sh.cnt[i] = 0;
+        __syncthreads();
+        if (live(mine)) atomicAdd(&sh.cnt[r.bin(mine)], 1u);
+        cluster_sync();
+        constexpr uint32_t PER = BINS / THREADS;                 // every CTA adds all up for itself
+        uint32_t n[PER], all = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) {
+            n[i] = 0;
+            for (uint32_t p = 0; p < parts; ++p) n[i] += get32(&sh.cnt[tid * PER + i], p);
+            all += n[i];
+        }
+        uint32_t upto = warp_upto(all);
+        if (lane == 31) sh.warp_t[warp] = upto;
+        if (tid == 0) sh.bin = BINS - 2;                         // fewer maxima than k that weigh anything: whatever does
+        __syncthreads();
+        for (uint32_t v = 0; v < warp; ++v) upto += sh.warp_t[v];
+        upto -= all;
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) {
+            if (upto < (uint32_t)top_k && upto + n[i] >= (uint32_t)top_k) sh.bin = min(tid * PER + i, BINS - 2);
+            upto += n[i];
+        }
+        __syncthreads();
+        const uint32_t listed = gather(0, sh.bin, 0);
+        if (listed <= LIST) {
+            cluster_arrive();                                    // (everyone has read how many there are: nobody touches another CTA's memory any more)
+            if (rank) { cluster_wait(); return; }
+            sorted_sums(listed, 0);
+            uint32_t m = min(listed, (uint32_t)top_k);
+            // how many of the first m have a running sum below the need, or a weight of `least` at least: weights fall, so either is a beginning
+            auto count = [&](u64 need, bool weights) {
+                uint32_t n = 0;
+                for (uint32_t i = tid; i < m; i += THREADS) n += weights ? sh.sums[i] - (i ? sh.sums[i - 1] : 0) >= need : sh.sums[i] < need;
+                n = __reduce_add_sync(0xffffffffu, n);
+                if (lane == 0) sh.warp_t[warp] = n;
+                __syncthreads();
+                n = 0;
+                for (uint32_t v = 0; v < NW; ++v) n += sh.warp_t[v];
+                __syncthreads();
+                return n;
+            };
+            if (top_p < 1.f) m = count(share(sh.sums[m - 1]), false) + 1;
+            if (least) m = count(least, true);
+            const u64 target = draw(sh.sums[m - 1]);
+            // once more by index: the weight has 45 bits, the index below them is the order
+            u64 packed[LIST / 2 / THREADS];
+#pragma unroll
+            for (uint32_t j = 0; j < LIST / 2 / THREADS; ++j) {
+                const uint32_t i = j * THREADS + tid;
+                packed[j] = i < m ? (u64)(TGP_SAMPLE_MAX_V - 1 - ~(uint32_t)sh.list[i]) << 45 | (sh.sums[i] - (i ? sh.sums[i - 1] : 0)) : 0;
+            }
+            __syncthreads();
+#pragma unroll
+            for (uint32_t j = 0; j < LIST / 2 / THREADS; ++j) if (j * THREADS + tid < m) sh.list[j * THREADS + tid] = packed[j];
+            __syncthreads();
+            sorted_sums(m, 45);
+            for (uint32_t i = tid; i < m; i += THREADS)
+                if ((i ? sh.sums[i - 1] : 0) <= target && sh.sums[i] > target) a.out[b] = (int32_t)(TGP_SAMPLE_MAX_V - 1 - (uint32_t)(sh.list[i] >> 45));
+            cluster_wait();
+            return;
+        }
+        cluster_sync();                                          // (everyone has read how many there are)
+        if (tid == 0) sh.listed = 0;
+    }
 
     // ---- histogram of the tokens at or above key_lo, by bin (level 0) or by (key_hi - key) >> shift; the bin in which the need-th token (or
-    // unit of weight) lies goes to the Shared of every CTA, in_n = 0 if there is none ----
+    // unit of weight) lies goes to the Shared of every CTA, bin BINS if there is none, and what all weigh as `target`.  By weight, level 0 counts no tokens and
+    // the need is top_p of all (of kept_w), which goes to `target` ----
+    u64 kept_w = 0;                                              // what the tokens kept so far weigh, once a search has told
     auto search = [&](bool level0, uint32_t key_lo, uint32_t key_hi, uint32_t shift, bool by_weight, u64 need) {
         for (uint32_t i = tid; i < BINS; i += THREADS) { sh.cnt[i] = 0; sh.lo[i] = 0; sh.hi[i] = 0; }
         __syncthreads();
-        for (uint32_t i = first + tid; i < end; i += THREADS) {
-            const float x = row[i];
-            if (!live(x)) continue;
+        each([&](float x, uint32_t) {
+            if (!live(x)) return;
             const uint32_t key = key_of(x);
-            if (key < key_lo || key > key_hi) continue;
+            if (key < key_lo || key > key_hi) return;
             const uint32_t z = r.bin(x);
-            if (z >= BINS - 1) continue;
+            if (z >= BINS - 1) return;
             // (the highest keys first, as the bins of level 0)
             const uint32_t bin = level0 ? z : (key_hi - key) >> shift;
-            atomicAdd(&sh.cnt[bin], 1u);
-            const u64 w = whole(r.weight(x));
+            if (!level0 || !by_weight) atomicAdd(&sh.cnt[bin], 1u);
+            const u64 w = r.weight(x);
             const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh.lo[bin], lo), hi = (uint32_t)(w >> 32) + (old + lo < old);
             if (hi) atomicAdd(&sh.hi[bin], hi);
-        }
+        });
         cluster_sync();
         for (uint32_t i = rank * THREADS + tid; i < BINS; i += parts * THREADS) {
             uint32_t n = 0;
@@ -167,10 +337,12 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
             uint32_t n_to = warp_upto(n);
             u64 w_to = warp_upto(w);
             if (lane == 31) { sh.warp_t[warp] = n_to; sh.warp_w[warp] = w_to; }
-            if (tid == 0) { sh.in_n = 0; sh.in_w = 0; }
+            if (tid == 0) { sh.in_n = 0; sh.in_w = 0; sh.bin = BINS; }
             __syncthreads();
-            for (uint32_t v = 0; v < warp; ++v) { n_to += sh.warp_t[v]; w_to += sh.warp_w[v]; }
+            u64 total = 0;
+            for (uint32_t v = 0; v < NW; ++v) { if (v < warp) { n_to += sh.warp_t[v]; w_to += sh.warp_w[v]; } total += sh.warp_w[v]; }
             n_to -= n; w_to -= w;
+            if (level0 && by_weight) need = share(kept_w ? kept_w : total);
             for (uint32_t i = 0; i < PER; ++i) {
                 const uint32_t bn = sh.all_cnt[tid * PER + i];
                 const u64 bw = sh.all_w[tid * PER + i], have = by_weight ? w_to : n_to, more = by_weight ? bw : bn;
@@ -178,8 +350,8 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
                 n_to += bn; w_to += bw;
             }
             __syncthreads();
-            if (tid == THREADS - 1) {                            // what all weigh
-                sh.target = w_to;
+            if (tid == 0) {
+                sh.target = level0 && by_weight ? need : total;
                 for (uint32_t p = 1; p < parts; ++p) {
                     put32(&sh.bin, p, sh.bin); put32(&sh.before_n, p, sh.before_n); put32(&sh.in_n, p, sh.in_n);
                     put64(&sh.before_w, p, sh.before_w); put64(&sh.in_w, p, sh.in_w); put64(&sh.target, p, sh.target);
@@ -190,12 +362,33 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
     };
 
     uint32_t cut = 0, ties = 0xffffffffu;                        // kept: keys above cut, and the first `ties` tokens of that key
-    u64 kept_w = 0;                                              // their weight, once a search has told
     auto narrow = [&](bool by_weight, u64 need) {
         search(true, cut, 0xffffffffu, 0, by_weight, need);
-        if (sh.in_n == 0) { kept_w = sh.target; return; }        // fewer tokens than asked for: all
+        if (sh.bin == BINS) { kept_w = sh.target; return; }      // fewer tokens than asked for: all
+        if (by_weight) need = sh.target;
         u64 before_w = sh.before_w;
         u64 before = by_weight ? sh.before_w : sh.before_n;
+        if (by_weight) {                                         // the tokens of the bin as a list, sorted: the first that reaches the need is the last one kept
+            const uint32_t n = gather(sh.bin, sh.bin, cut);
+            if (n <= LIST) {
+                if (rank == 0) {
+                    sorted_sums(n, 0);
+                    for (uint32_t i = tid; i < n; i += THREADS)
+                        if ((i ? sh.sums[i - 1] : 0) < need - before && sh.sums[i] >= need - before) {
+                            const uint32_t key = (uint32_t)(sh.list[i] >> 32);
+                            uint32_t same = 1;
+                            for (uint32_t j = i; j && (uint32_t)(sh.list[j - 1] >> 32) == key; --j) ++same;
+                            for (uint32_t p = 0; p < parts; ++p) { put32(&sh.key_lo, p, key); put32(&sh.key_hi, p, same); }
+                        }
+                }
+                cluster_sync();
+                ties = sh.key_lo == cut ? min(ties, sh.key_hi) : sh.key_hi;
+                cut = sh.key_lo;
+                return;
+            }
+            cluster_sync();
+            if (tid == 0) sh.listed = 0;
+        }
         // the keys of the bin: the bins ascend where keys descend
         if (warp < 2) {                                          // warp 0: the lowest key with bin <= z; warp 1: the lowest with bin < z; 32 candidates at a time
             const uint32_t z = sh.bin;
@@ -218,13 +411,13 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
         __syncthreads();
         for (int level = 0; level < 4; ++level) {                // (32 bits at most, each search takes 11)
             // one token, or all that the bin holds: the cut is its lowest key (a lower cut found before keeps its ties)
-            if (in_n == 1 || (!by_weight && need - before == in_n)) {
+            if (in_n == 1 || (!by_weight && need - before == in_n)) {            // (by weight, in_n is known from the second search on)
                 if (key_lo > cut) { cut = key_lo; ties = 0xffffffffu; }
                 kept_w = before_w + in_w;
                 return;
             }
             if (key_lo == key_hi) {                              // equals: the first so many
-                const u64 one = in_w / in_n, n = by_weight ? (need - before + one - 1) / one : need - before;
+                const u64 one = r.weight(of_key(key_lo)), n = by_weight ? (need - before + one - 1) / one : need - before;
                 ties = (uint32_t)min((u64)(key_lo == cut ? ties : 0xffffffffu), n);
                 cut = key_lo;
                 kept_w = before_w + ties * one;
@@ -244,27 +437,34 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
     };
     if (top_k > 0 && (uint32_t)top_k < a.V) narrow(false, (u64)top_k);
     if (top_p < 1.f) {
-        if (kept_w == 0) { search(true, cut, 0xffffffffu, 0, true, ~0ull); kept_w = sh.target; __syncthreads(); }
-        const double want = ceil(fmax((double)top_p, 0.0) * (double)kept_w);
-        narrow(true, max(1ull, min(kept_w, (u64)want)));
+        narrow(true, 0);
     }
 
     // ---- the draw: sums of the warps' segments, in the order of the tokens ----
-    const double least = min_p > 0.f ? (double)min_p : 0.0;
-    auto segment = [&](uint32_t lo, uint32_t hi, u64 &w, uint32_t &t) {       // weight above the cut, and ties, of [lo, hi)
+    const uint32_t least_z = least ? (uint32_t)fmin(-64.0 * log((double)min_p) + 2, (double)(BINS - 2)) : BINS - 2;      // no token of a bin beyond is kept
+    // weight above the cut, and ties, of [lo, hi)
+    auto counts = [&](float x, u64 &w, uint32_t &t) {
+        if (!live(x)) return;
+        const uint32_t key = key_of(x);
+        if (key < cut || r.bin(x) > least_z) return;
+        const u64 e = r.weight(x);
+        if (e < least) return;
+        if (key == cut && ties != 0xffffffffu) ++t; else w += e;
+    };
+    auto segment = [&](uint32_t lo, uint32_t hi, u64 &w, uint32_t &t) {
         w = 0; t = 0;
-        for (uint32_t i = lo + lane; i < hi; i += 32) {
-            const float x = row[i];
-            if (!live(x)) continue;
-            const uint32_t key = key_of(x);
-            if (key < cut || r.bin(x) >= BINS - 1) continue;
-            const double e = r.weight(x);
-            if (!(e >= least)) continue;
-            if (key == cut) ++t; else w += whole(e);
+        uint32_t i = lo + lane;
+        for (; i < hi && hi - i > 7 * 32; i += 8 * 32) {
+            float x[8];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * 32];
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) counts(x[j], w, t);
         }
+        for (; i < hi; i += 32) counts(row[i], w, t);
         w = warp_total(w); t = warp_total(t);
     };
-    const u64 tie_w = cut ? whole(r.weight(of_key(cut))) : 0;
+    const u64 tie_w = cut && ties != 0xffffffffu ? r.weight(of_key(cut)) : 0;
     const uint32_t per_warp = (a.per + NW - 1) / NW, lo = min(end, first + warp * per_warp), hi = min(end, lo + per_warp);
     {
         u64 w; uint32_t t;
@@ -272,48 +472,65 @@ __global__ void __launch_bounds__(THREADS) tgp_sample_kernel(const SampleArgs a)
         if (lane == 0) { put64(&sh.seg_w[rank * NW + warp], 0, w); put32(&sh.seg_t[rank * NW + warp], 0, t); }
     }
     cluster_sync();
-    if (rank == 0 && tid == 0) {
-        u64 sum = 0;
-        uint32_t left = ties;
-        for (uint32_t s = 0; s < parts * NW; ++s) { const uint32_t t = min(left, sh.seg_t[s]); left -= t; sum += sh.seg_w[s] + t * tie_w; }
-        const double u = (double)a.u[b];
-        u64 target = u > 0.0 ? (u64)fmin(u * (double)sum, 9.0e18) : 0;
-        target = min(target, sum - 1);
-        u64 before = 0;
-        uint32_t seen = 0, s = 0;
-        for (; s < parts * NW; ++s) {
-            const uint32_t t = min(ties - min(ties, seen), sh.seg_t[s]);
-            const u64 w = sh.seg_w[s] + t * tie_w;
-            if (before + w > target) break;
-            before += w;
-            seen += sh.seg_t[s];
+    if (rank == 0 && warp == 0) {                                // four segments a lane: ties before them, then weight before them
+        constexpr uint32_t PER = CLUSTER_MAX * NW / 32;
+        uint32_t t[PER], all = 0;
+        u64 w[PER], sum = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) { t[i] = lane * PER + i < parts * NW ? sh.seg_t[lane * PER + i] : 0; all += t[i]; }
+        uint32_t seen = warp_upto(all) - all;
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) {
+            w[i] = (lane * PER + i < parts * NW ? sh.seg_w[lane * PER + i] : 0) + min(ties - min(ties, seen), t[i]) * tie_w;
+            seen += t[i];
+            sum += w[i];
         }
-        for (uint32_t p = 0; p < parts; ++p) { put32(&sh.seg, p, s); put64(&sh.target, p, target - before); put32(&sh.ties_before, p, seen); }
+        u64 upto = warp_upto(sum);
+        const u64 target = draw(__shfl_sync(0xffffffffu, upto, 31));
+        seen -= all;
+        upto -= sum;
+#pragma unroll
+        for (uint32_t i = 0; i < PER; ++i) {
+            if (upto <= target && upto + w[i] > target)
+                for (uint32_t p = 0; p < parts; ++p) { put32(&sh.seg, p, lane * PER + i); put64(&sh.target, p, target - upto); put32(&sh.ties_before, p, seen); }
+            upto += w[i];
+            seen += t[i];
+        }
     }
     cluster_sync();
-    if (sh.seg / NW == rank && sh.seg % NW == warp) {
-        u64 target = sh.target;
-        uint32_t seen = sh.ties_before;
-        for (uint32_t i0 = lo; i0 < hi; i0 += 32) {
-            const uint32_t i = i0 + lane;
-            const float x = i < hi ? row[i] : -INFINITY;
-            u64 w = 0;
-            bool tie = false;
-            if (live(x) && key_of(x) >= cut && r.bin(x) < BINS - 1) {
-                const double e = r.weight(x);
-                if (e >= least) { tie = key_of(x) == cut; w = whole(e); }
-            }
-            const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
-            if (tie && seen + __popc(tie_mask & ((1u << lane) - 1)) >= ties) w = 0;
-            const u64 upto = warp_upto(w);
-            const uint32_t found = __ballot_sync(0xffffffffu, upto > target);
-            if (found) {
-                if (lane == __ffs(found) - 1) a.out[b] = (int32_t)i;
-                break;
-            }
-            target -= __shfl_sync(0xffffffffu, upto, 31);
-            seen += __popc(tie_mask);
+    // ---- the CTA of the segment: its warps take a sixteenth of it each, then the one into which the rest of the target falls goes through its part ----
+    if (sh.seg / NW != rank) return;
+    const uint32_t s_lo = min(end, first + sh.seg % NW * per_warp), s_hi = min(end, s_lo + per_warp), per_part = (s_hi - s_lo + NW - 1) / NW;
+    const uint32_t m_lo = min(s_hi, s_lo + warp * per_part), m_hi = min(s_hi, m_lo + per_part);
+    {
+        u64 w; uint32_t t;
+        segment(m_lo, m_hi, w, t);
+        if (lane == 0) { sh.warp_w[warp] = w; sh.warp_t[warp] = t; }
+    }
+    __syncthreads();
+    u64 target = sh.target;
+    uint32_t seen = sh.ties_before;
+    for (uint32_t v = 0; v < NW; ++v) {
+        const u64 w = sh.warp_w[v] + min(ties - min(ties, seen), sh.warp_t[v]) * tie_w;
+        if (target < w) { if (v != warp) return; break; }
+        target -= w;
+        seen += sh.warp_t[v];
+    }
+    for (uint32_t i0 = m_lo; i0 < m_hi; i0 += 32) {
+        const uint32_t i = i0 + lane;
+        u64 w = 0;
+        uint32_t t = 0;
+        if (i < m_hi) counts(row[i], w, t);
+        const uint32_t tie_mask = __ballot_sync(0xffffffffu, t != 0);
+        if (t && seen + __popc(tie_mask & ((1u << lane) - 1)) < ties) w = tie_w;
+        const u64 upto = warp_upto(w);
+        const uint32_t found = __ballot_sync(0xffffffffu, upto > target);
+        if (found) {
+            if (lane == __ffs(found) - 1) a.out[b] = (int32_t)i;
+            break;
         }
+        target -= __shfl_sync(0xffffffffu, upto, 31);
+        seen += __popc(tie_mask);
     }
 }
 
@@ -325,7 +542,7 @@ extern "C" int tgp_k_sample(const float *logits, const float *u_dev, int32_t *ou
     if (V > TGP_SAMPLE_MAX_V) return TGP_E_TOO_LARGE;
     if (!B) return TGP_OK;
     uint32_t parts = V > 4096 ? 8 : 1;
-    while (parts > 1 && (uint64_t)B * parts > (uint32_t)tgpk_sms()) parts /= 2;
+    while (parts > 1 && (uint64_t)B * parts > 2u * (uint32_t)tgpk_sms()) parts /= 2;
     if ((uint64_t)B * parts > 0x7fffffffu) return TGP_E_TOO_LARGE;
     if (!tgpk_allow_smem<tgp_sample_kernel>(sizeof(Shared))) return TGP_E_CUDA;
     const SampleArgs a{logits, u_dev, temperature_dev, top_p_dev, min_p_dev, top_k_dev, out, V, (V + parts - 1) / parts};
