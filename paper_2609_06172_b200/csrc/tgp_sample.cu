@@ -87,16 +87,15 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
 struct Row {
-    float top, step;                                             // the maximum; 64 / temperature
+    float top, step, low;                                        // the maximum; 64 / temperature; what is below weighs nothing (and is no NaN, nor -inf)
     double top64, rate;                                          // 32 log2(e) / temperature
     const double *octave;
-    // bin of a logit that is no NaN and above -inf; BINS - 1 and more weigh nothing
+    // bin of a logit that is no NaN and above -inf; those of BINS - 1 weigh nothing.  (Rounded by what 2^23 leaves of the fraction, without a conversion.)
     __device__ __forceinline__ uint32_t bin(float x) const {
-        if (x == top) return 0;
-        const float z = (top - x) * step;
-        return z < (float)(BINS - 1) ? (uint32_t)z : BINS - 1;   // (a NaN: infinity times 0)
+        const float z = x == top ? 0.f : fminf((top - x) * step, (float)(BINS - 1));            // (fminf: a NaN, infinity times 0, is BINS - 1)
+        return __float_as_uint(z + 8388608.f) & (BINS - 1);
     }
-    // The weight of a logit of a bin below BINS - 1: with t = 32 log2(e) (x - top) / temperature = n + f, |f| <= 1/2, it is 2^(n / 32) exp(f ln2 / 32), the latter by its
+    // The weight of a logit not below `low`: with t = 32 log2(e) (x - top) / temperature = n + f, |f| <= 1/2, it is 2^(n / 32) exp(f ln2 / 32), the latter by its
     // series, whose sixth power is below 2^-48, the former from a table of 2^(i / 32).  Off by a few units of 2^-52 besides.
     __device__ __forceinline__ u64 weight(float x) const {
         constexpr double MAGIC = 6755399441055744.0;             // 1.5 * 2^52: a number plus this has its nearest integer in its low bits
@@ -114,8 +113,33 @@ struct Row {
     }
 };
 
-// Sorts the first n (a power of two) of a list, the largest first; all threads of the CTA.
+// Sorts the first n of a list of different numbers, the largest first; all threads of the CTA.  Up to 256 by counting, for each, those that are larger - a
+// warp per number - else in a bitonic network over a power of two.
 __device__ __forceinline__ void sort_list(u64 *list, uint32_t n) {
+    __syncthreads();
+    if (n <= 256) {
+        const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        u64 x[8], mine = 0;
+        uint32_t at = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) x[j] = j * 32 + lane < n ? list[j * 32 + lane] : 0;
+        for (uint32_t i = warp, turn = 0; i < n; i += NW, ++turn) {
+            const u64 y = list[i];
+            uint32_t larger = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) if (j * 32 < n) larger += x[j] > y;
+            larger = __reduce_add_sync(0xffffffffu, larger);
+            if (turn == lane) { mine = y; at = larger; }
+        }
+        __syncthreads();
+        if (warp + NW * lane < n) list[at] = mine;
+        __syncthreads();
+        return;
+    }
+    uint32_t size = 512;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + threadIdx.x; i < size; i += THREADS) list[i] = 0;
+    n = size;
     for (uint32_t k = 2; k <= n; k <<= 1)
         for (uint32_t j = k >> 1; j; j >>= 1) {
             __syncthreads();
@@ -142,6 +166,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     cluster_arrive();                                            // (the first access to another CTA's memory waits for it to run)
     if (tid < 32) sh.octave[tid] = exp2((double)tid / 32);
     if (tid == 0) sh.listed = 0;
+    for (uint32_t i = tid; i < BINS; i += THREADS) sh.cnt[i] = 0;
 
     // every logit of this CTA's part once, each thread every THREADS-th, eight loads under way
     auto each = [&](auto &&f) {
@@ -192,14 +217,14 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     r.rate = inv * 46.166241308446828;                           // 32 log2(e)
     r.step = (float)(64.0 * inv);
     r.top64 = (double)r.top;
+    r.low = r.top == INFINITY ? INFINITY : fmaxf((float)(r.top64 - 33.0 / inv), -3.402823466e38f);
     r.octave = sh.octave;
-    auto live = [&](float x) { return x > -INFINITY; };
     const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * ONE) : 0;
 
     // ---- tokens whose bin is in [z_lo, z_hi] and whose key is not below key_lo as a list in the first CTA; how many there are, LIST at most, or LIST + 1 ----
     auto gather = [&](uint32_t z_lo, uint32_t z_hi, uint32_t key_lo) {
         each([&](float x, uint32_t i) {
-            if (!live(x)) return;
+            if (!(x >= r.low)) return;
             const uint32_t z = r.bin(x);
             if (z < z_lo || z > z_hi || key_of(x) < key_lo) return;
             const uint32_t at = add32(&sh.listed, 0, 1);
@@ -210,10 +235,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     };
     // (first CTA) sorts n listed tokens, and gives the running sums of their weights: of their logits, or of the numbers in the low `bits`
     auto sorted_sums = [&](uint32_t n, uint32_t bits) {
-        uint32_t size = 32;
-        while (size < n) size *= 2;
-        for (uint32_t i = n + tid; i < size; i += THREADS) sh.list[i] = 0;
-        sort_list(sh.list, size);
+        sort_list(sh.list, n);
         u64 before = 0;
         for (uint32_t i0 = 0; i0 < n; i0 += THREADS) {
             const uint32_t i = i0 + tid;
@@ -234,29 +256,23 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
 
     // ---- top-k by the list of what is not below the k-th largest of the threads' maxima ----
     if (top_k > 0 && (uint32_t)top_k <= min(LIST / 2, parts * THREADS) && (uint32_t)top_k < a.V) {
-        for (uint32_t i = tid; i < BINS; i += THREADS) sh.cnt[i] = 0;
-        __syncthreads();
-        if (live(mine)) atomicAdd(&sh.cnt[r.bin(mine)], 1u);
+        // (bins of eight: a histogram of 256, which every CTA adds up for itself)
+        constexpr uint32_t EIGHT = BINS / 8;
+        if (mine >= r.low) atomicAdd(&sh.cnt[r.bin(mine) / 8], 1u);
         cluster_sync();
-        constexpr uint32_t PER = BINS / THREADS;                 // every CTA adds all up for itself
-        uint32_t n[PER], all = 0;
+        uint32_t n = 0, c[CLUSTER_MAX];
+        if (tid < EIGHT) {
 #pragma unroll
-        for (uint32_t i = 0; i < PER; ++i) {
-            n[i] = 0;
-            for (uint32_t p = 0; p < parts; ++p) n[i] += get32(&sh.cnt[tid * PER + i], p);
-            all += n[i];
+            for (uint32_t p = 0; p < CLUSTER_MAX; ++p) if (p < parts) c[p] = get32(&sh.cnt[tid], p);
+#pragma unroll
+            for (uint32_t p = 0; p < CLUSTER_MAX; ++p) if (p < parts) n += c[p];
         }
-        uint32_t upto = warp_upto(all);
+        uint32_t upto = warp_upto(n);
         if (lane == 31) sh.warp_t[warp] = upto;
         if (tid == 0) sh.bin = BINS - 2;                         // fewer maxima than k that weigh anything: whatever does
         __syncthreads();
         for (uint32_t v = 0; v < warp; ++v) upto += sh.warp_t[v];
-        upto -= all;
-#pragma unroll
-        for (uint32_t i = 0; i < PER; ++i) {
-            if (upto < (uint32_t)top_k && upto + n[i] >= (uint32_t)top_k) sh.bin = min(tid * PER + i, BINS - 2);
-            upto += n[i];
-        }
+        if (upto - n < (uint32_t)top_k && upto >= (uint32_t)top_k) sh.bin = min(tid * 8 + 7, BINS - 2);
         __syncthreads();
         const uint32_t listed = gather(0, sh.bin, 0);
         if (listed <= LIST) {
@@ -308,7 +324,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         for (uint32_t i = tid; i < BINS; i += THREADS) { sh.cnt[i] = 0; sh.lo[i] = 0; sh.hi[i] = 0; }
         __syncthreads();
         each([&](float x, uint32_t) {
-            if (!live(x)) return;
+            if (!(x >= r.low)) return;
             const uint32_t key = key_of(x);
             if (key < key_lo || key > key_hi) return;
             const uint32_t z = r.bin(x);
@@ -324,7 +340,11 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         for (uint32_t i = rank * THREADS + tid; i < BINS; i += parts * THREADS) {
             uint32_t n = 0;
             u64 w = 0;
-            for (uint32_t p = 0; p < parts; ++p) { n += get32(&sh.cnt[i], p); w += (u64)get32(&sh.lo[i], p) + ((u64)get32(&sh.hi[i], p) << 32); }
+            uint32_t c[CLUSTER_MAX], l[CLUSTER_MAX], h[CLUSTER_MAX];
+#pragma unroll
+            for (uint32_t p = 0; p < CLUSTER_MAX; ++p) if (p < parts) { c[p] = get32(&sh.cnt[i], p); l[p] = get32(&sh.lo[i], p); h[p] = get32(&sh.hi[i], p); }
+#pragma unroll
+            for (uint32_t p = 0; p < CLUSTER_MAX; ++p) if (p < parts) { n += c[p]; w += (u64)l[p] + ((u64)h[p] << 32); }
             put32(&sh.all_cnt[i], 0, n);
             put64(&sh.all_w[i], 0, w);
         }
@@ -441,15 +461,15 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     }
 
     // ---- the draw: sums of the warps' segments, in the order of the tokens ----
-    const uint32_t least_z = least ? (uint32_t)fmin(-64.0 * log((double)min_p) + 2, (double)(BINS - 2)) : BINS - 2;      // no token of a bin beyond is kept
+    // no token below is kept: it is below the cut, or too far from the maximum for min_p (by more than what rounding the bound to fp32 takes)
+    float lowest = cut ? fmaxf(r.low, of_key(cut)) : r.low;
+    if (ties == 0xffffffffu && least) lowest = fmaxf(lowest, (float)(r.top64 + (log((double)min_p) - 1e-3) / inv) - fabsf(r.top) * 1e-6f);
     // weight above the cut, and ties, of [lo, hi)
     auto counts = [&](float x, u64 &w, uint32_t &t) {
-        if (!live(x)) return;
-        const uint32_t key = key_of(x);
-        if (key < cut || r.bin(x) > least_z) return;
+        if (!(x >= lowest)) return;
         const u64 e = r.weight(x);
         if (e < least) return;
-        if (key == cut && ties != 0xffffffffu) ++t; else w += e;
+        if (x == lowest && ties != 0xffffffffu) ++t; else w += e;
     };
     auto segment = [&](uint32_t lo, uint32_t hi, u64 &w, uint32_t &t) {
         w = 0; t = 0;
