@@ -24,7 +24,7 @@ namespace {
 using namespace tgp_launch;
 
 constexpr int THREADS = 512, NW = THREADS / 32;
-constexpr uint32_t BINS = 2048, CLUSTER_MAX = 8, LIST = 2048;
+constexpr uint32_t BINS = 2048, CLUSTER_MAX = 8, LIST = 2048, OCTAVE = 512;
 constexpr double ONE = 17592186044416.0;                        // 2^44, the weight of the maximum
 typedef unsigned long long u64;
 
@@ -37,8 +37,8 @@ struct SampleArgs {
 struct Shared {
     uint32_t cnt[BINS], lo[BINS], hi[BINS];                      // histogram of the CTA's part: tokens, and their weight in two words
     u64 list[LIST]; u64 sums[LIST];                              // tokens as key << 32 | ~index, and sums of their weights (first CTA)
-    double octave[32];                                           // 2^(i / 32)
-    uint32_t listed;
+    double octave[OCTAVE];                                       // 2^(44 + i / OCTAVE)
+    uint32_t listed, counts[CLUSTER_MAX];                        // tokens that this CTA found, and each CTA
     uint32_t all_cnt[BINS]; u64 all_w[BINS];                     // of the row (first CTA)
     float top[CLUSTER_MAX]; uint32_t top_i[CLUSTER_MAX];         // the parts' maxima (first CTA)
     u64 seg_w[CLUSTER_MAX * NW]; uint32_t seg_t[CLUSTER_MAX * NW];      // the warps' sums and ties (first CTA)
@@ -66,7 +66,6 @@ __device__ __forceinline__ uint32_t get32(const uint32_t *p, uint32_t rank) { ui
 __device__ __forceinline__ void put32(uint32_t *p, uint32_t rank, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(in_cta(p, rank)), "r"(v) : "memory"); }
 __device__ __forceinline__ void put64(u64 *p, uint32_t rank, u64 v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_cta(p, rank)), "l"(v) : "memory"); }
 
-__device__ __forceinline__ uint32_t add32(uint32_t *p, uint32_t rank, uint32_t v) { uint32_t old; asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(in_cta(p, rank)), "r"(v) : "memory"); return old; }
 
 template <typename T> __device__ __forceinline__ T warp_total(T v) {
 #pragma unroll
@@ -88,30 +87,26 @@ __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k &
 
 struct Row {
     float top, step, low;                                        // the maximum; 64 / temperature; what is below weighs nothing (and is no NaN, nor -inf)
-    double top64, rate;                                          // 32 log2(e) / temperature
+    double top64, rate;                                          // the maximum (0 where it is infinite); OCTAVE * log2(e) / temperature
     const double *octave;
     // bin of a logit that is no NaN and above -inf; those of BINS - 1 weigh nothing.  (Rounded by what 2^23 leaves of the fraction, without a conversion.)
     __device__ __forceinline__ uint32_t bin(float x) const {
         const float z = x == top ? 0.f : fminf((top - x) * step, (float)(BINS - 1));            // (fminf: a NaN, infinity times 0, is BINS - 1)
         return __float_as_uint(z + 8388608.f) & (BINS - 1);
     }
-    // The weight of a logit not below `low`: with t = 32 log2(e) (x - top) / temperature = n + f, |f| <= 1/2, it is 2^(n / 32) exp(f ln2 / 32), the latter by its
-    // series, whose sixth power is below 2^-48, the former from a table of 2^(i / 32).  Off by a few units of 2^-52 besides.
+    // The weight of a logit not below `low` (of others: any number): with t = OCTAVE log2(e) (x - top) / temperature = n + f, |f| <= 1/2, it is 2^(n / OCTAVE)
+    // exp(f ln2 / OCTAVE), the latter by its series, whose fourth power is below 2^-46, the former from a table.  The last sum with 2^52 puts the point behind its last bit.
     __device__ __forceinline__ u64 weight(float x) const {
         constexpr double MAGIC = 6755399441055744.0;             // 1.5 * 2^52: a number plus this has its nearest integer in its low bits
-        constexpr double C = 0.021660849392498290;               // ln2 / 32
-        const double t = x == top ? 0.0 : ((double)x - top64) * rate, m = t + MAGIC, f = t - (m - MAGIC);
+        constexpr double C = 0.69314718055994530942 / OCTAVE;
+        const double t = ((double)(top == INFINITY ? 0.f : x) - top64) * rate, m = t + MAGIC, f = t - (m - MAGIC);
         const int n = __double2loint(m);
-        double p = fma(f, C * C * C * C * C / 120, C * C * C * C / 24);
-        p = fma(f, p, C * C * C / 6);
-        p = fma(f, p, C * C / 2);
-        p = fma(f, p, C);
-        p = fma(f, p, 1.0);
-        const double o = octave[n & 31];
-        const double scale = __hiloint2double(__double2hiint(o) + ((n >> 5) + 44) * (1 << 20), __double2loint(o));
-        return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xfffffffffffffull;          // 2^52 puts the point behind the last bit
+        const double p = fma(f, fma(f, fma(f, C * C * C / 6, C * C / 2), C), 1.0), o = octave[n & (OCTAVE - 1)];
+        const double scale = __hiloint2double((int)((uint32_t)__double2hiint(o) + (((uint32_t)n & ~(OCTAVE - 1)) << 11)), __double2loint(o));
+        return (u64)__double_as_longlong(fma(p, scale, 4503599627370496.0)) & 0xfffffffffffffull;
     }
 };
+static_assert(OCTAVE << 11 == 1 << 20, "weight() adds n / OCTAVE to an exponent");
 
 // Sorts the first n of a list of different numbers, the largest first; all threads of the CTA.  Up to 256 by counting, for each, those that are larger - a
 // warp per number - else in a bitonic network over a power of two.
@@ -140,9 +135,12 @@ __device__ __forceinline__ void sort_list(u64 *list, uint32_t n) {
     while (size < n) size *= 2;
     for (uint32_t i = n + threadIdx.x; i < size; i += THREADS) list[i] = 0;
     n = size;
+    // (a warp's 32 pairs of a step with j <= 32 are 64 neighbours, which it alone touches in all such steps)
+    __syncthreads();
     for (uint32_t k = 2; k <= n; k <<= 1)
         for (uint32_t j = k >> 1; j; j >>= 1) {
-            __syncthreads();
+            if (j >= 64 || (j == 32 && k > 64)) __syncthreads();
+            else __syncwarp();
             for (uint32_t i = threadIdx.x; i < n / 2; i += THREADS) {
                 const uint32_t x = 2 * i - (i & (j - 1)), y = x + j;
                 const u64 p = list[x], q = list[y];
@@ -164,7 +162,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     const uint32_t first = min(a.V, rank * a.per), end = min(a.V, first + a.per);
 
     cluster_arrive();                                            // (the first access to another CTA's memory waits for it to run)
-    if (tid < 32) sh.octave[tid] = exp2((double)tid / 32);
+    for (uint32_t i = tid; i < OCTAVE; i += THREADS) sh.octave[i] = ONE * exp2((double)i / OCTAVE);
     if (tid == 0) sh.listed = 0;
     for (uint32_t i = tid; i < BINS; i += THREADS) sh.cnt[i] = 0;
 
@@ -214,24 +212,52 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         return;
     }
     const double inv = 1.0 / (double)fmaxf(temperature, 7.52316384526264e-37f);        // 2^-120: bins are told in fp32
-    r.rate = inv * 46.166241308446828;                           // 32 log2(e)
+    r.rate = inv * (OCTAVE * 1.4426950408889634074);
     r.step = (float)(64.0 * inv);
     r.top64 = (double)r.top;
     r.low = r.top == INFINITY ? INFINITY : fmaxf((float)(r.top64 - 33.0 / inv), -3.402823466e38f);
     r.octave = sh.octave;
+    if (r.top == INFINITY) r.top64 = 0.0;
     const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * ONE) : 0;
 
-    // ---- tokens whose bin is in [z_lo, z_hi] and whose key is not below key_lo as a list in the first CTA; how many there are, LIST at most, or LIST + 1 ----
-    auto gather = [&](uint32_t z_lo, uint32_t z_hi, uint32_t key_lo) {
+    // ---- the keys of a bin, as key_lo and key_hi of every CTA's Shared: bins ascend where keys descend.  Warp 0: the lowest key with bin <= z; warp 1: the lowest
+    // with bin < z; 32 candidates at a time ----
+    auto keys_of = [&](uint32_t z) {
+        if (warp < 2) {
+            u64 lo = 0, hi = (u64)key_of(r.top) + 1;             // the answer lies in [lo, hi]; hi: of warp 1 where the bin holds the maximum
+            while (lo < hi) {
+                const u64 step = (hi - lo + 31) / 32, k = lo + lane * step;
+                const float x = of_key((uint32_t)k);
+                const bool in = k < hi && !isnan(x) && x > -INFINITY && (warp == 0 ? r.bin(x) <= z : r.bin(x) < z);
+                const uint32_t mask = __ballot_sync(0xffffffffu, in || k >= hi);                 // a beginning of zeros, then ones
+                const uint32_t at = mask ? __ffs(mask) - 1 : 32;
+                const u64 new_hi = at == 32 ? hi : min(hi, lo + at * step);
+                lo = at == 0 ? new_hi : min(hi, lo + (at - 1) * step + 1);
+                hi = new_hi;
+            }
+            if (lane == 0) { if (warp == 0) sh.key_lo = (uint32_t)hi; else sh.key_hi = (uint32_t)(hi - 1); }
+        }
+        __syncthreads();
+    };
+    // ---- tokens whose key is in [key_lo, key_hi], which are those of numbers, as a list in the first CTA; how many there are (more than LIST: there is no list).
+    // Each CTA lists its own, then the others send theirs behind the first one's. ----
+    auto gather = [&](uint32_t key_lo, uint32_t key_hi) {
+        const float x_lo = of_key(key_lo), x_hi = of_key(key_hi);
         each([&](float x, uint32_t i) {
-            if (!(x >= r.low)) return;
-            const uint32_t z = r.bin(x);
-            if (z < z_lo || z > z_hi || key_of(x) < key_lo) return;
-            const uint32_t at = add32(&sh.listed, 0, 1);
-            if (at < LIST) put64(&sh.list[at], 0, (u64)key_of(x) << 32 | (uint32_t)~i);
+            if (!(x >= x_lo && x <= x_hi)) return;
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i;
         });
+        __syncthreads();
+        const uint32_t n = sh.listed;
+        if (tid < parts) put32(&sh.counts[rank], tid, n);
         cluster_sync();
-        return min(get32(&sh.listed, 0), LIST + 1);
+        uint32_t before = 0, all = 0;
+        for (uint32_t p = 0; p < parts; ++p) { if (p < rank) before += sh.counts[p]; all += sh.counts[p]; }
+        if (rank && all <= LIST) for (uint32_t i = tid; i < n; i += THREADS) put64(&sh.list[before + i], 0, sh.list[i]);
+        if (tid == 0) sh.listed = 0;
+        cluster_sync();
+        return all;
     };
     // (first CTA) sorts n listed tokens, and gives the running sums of their weights: of their logits, or of the numbers in the low `bits`
     auto sorted_sums = [&](uint32_t n, uint32_t bits) {
@@ -274,10 +300,10 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         for (uint32_t v = 0; v < warp; ++v) upto += sh.warp_t[v];
         if (upto - n < (uint32_t)top_k && upto >= (uint32_t)top_k) sh.bin = min(tid * 8 + 7, BINS - 2);
         __syncthreads();
-        const uint32_t listed = gather(0, sh.bin, 0);
+        keys_of(sh.bin);
+        const uint32_t listed = gather(sh.key_lo, key_of(r.top));
         if (listed <= LIST) {
-            cluster_arrive();                                    // (everyone has read how many there are: nobody touches another CTA's memory any more)
-            if (rank) { cluster_wait(); return; }
+            if (rank) return;                                    // (nobody touches another CTA's memory any more)
             sorted_sums(listed, 0);
             uint32_t m = min(listed, (uint32_t)top_k);
             // how many of the first m have a running sum below the need, or a weight of `least` at least: weights fall, so either is a beginning
@@ -309,19 +335,72 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             sorted_sums(m, 45);
             for (uint32_t i = tid; i < m; i += THREADS)
                 if ((i ? sh.sums[i - 1] : 0) <= target && sh.sums[i] > target) a.out[b] = (int32_t)(TGP_SAMPLE_MAX_V - 1 - (uint32_t)(sh.list[i] >> 45));
-            cluster_wait();
             return;
         }
-        cluster_sync();                                          // (everyone has read how many there are)
-        if (tid == 0) sh.listed = 0;
     }
 
     // ---- histogram of the tokens at or above key_lo, by bin (level 0) or by (key_hi - key) >> shift; the bin in which the need-th token (or
     // unit of weight) lies goes to the Shared of every CTA, bin BINS if there is none, and what all weigh as `target`.  By weight, level 0 counts no tokens and
     // the need is top_p of all (of kept_w), which goes to `target` ----
     u64 kept_w = 0;                                              // what the tokens kept so far weigh, once a search has told
+    uint32_t cut = 0, ties = 0xffffffffu;                        // kept: keys above cut, and the first `ties` tokens of that key
     auto search = [&](bool level0, uint32_t key_lo, uint32_t key_hi, uint32_t shift, bool by_weight, u64 need) {
         for (uint32_t i = tid; i < BINS; i += THREADS) { sh.cnt[i] = 0; sh.lo[i] = 0; sh.hi[i] = 0; }
+        auto add = [&](uint32_t bin, u64 w) {
+            const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh.lo[bin], lo), hi = (uint32_t)(w >> 32) + (old + lo < old);
+            if (hi) atomicAdd(&sh.hi[bin], hi);
+        };
+        auto cta_total = [&](u64 w) {                            // of all threads
+            w = warp_total(w);
+            if (lane == 0) sh.warp_w[warp] = w;
+            __syncthreads();
+            w = 0;
+            for (uint32_t v = 0; v < NW; ++v) w += sh.warp_w[v];
+            __syncthreads();
+            return w;
+        };
+        if (level0 && by_weight) {
+            // What weighs less than w1 = (1 - top_p) * sum / V adds up to less than (1 - top_p) * sum, so t weighs w1 at least, and bins beyond are left out; the sum is at
+            // least that of the threads' maxima (of this CTA: its bins go further than they need to)
+            const float floor_x = cut ? fmaxf(r.low, of_key(cut)) : r.low;
+            const u64 sum = max(kept_w ? kept_w : cta_total(mine >= r.low ? r.weight(mine) : 0), (u64)ONE);
+            const float z1 = 64.f * logf((float)((double)a.V * ONE / ((1.0 - (double)top_p) * (double)sum))) + 2.f;
+            const uint32_t last = z1 < (float)(BINS - 2) ? (uint32_t)fmaxf(z1, 0.f) : BINS - 2;
+            __syncthreads();
+            u64 all = 0;
+            // four at a time: their weights, then their additions to the low words, then what those carry
+            auto four = [&](const float (&x)[4]) {
+                u64 w[4];
+                uint32_t z[4], old[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    w[j] = r.weight(x[j]);
+                    z[j] = x[j] >= floor_x ? r.bin(x[j]) : BINS;
+                    all += z[j] < BINS ? w[j] : 0;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (z[j] <= last) old[j] = atomicAdd(&sh.lo[z[j]], (uint32_t)w[j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t hi = z[j] <= last ? (uint32_t)(w[j] >> 32) + (old[j] + (uint32_t)w[j] < old[j]) : 0;
+                    if (hi) atomicAdd(&sh.hi[z[j]], hi);
+                }
+            };
+            uint32_t i = first + tid;
+            float next[4];
+            auto fetch = [&]() {
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) next[j] = i < end && end - i > j * THREADS ? row[i + j * THREADS] : -INFINITY;
+            };
+            for (fetch(); i < end;) {
+                const float x[4] = {next[0], next[1], next[2], next[3]};
+                i = end - i > 4 * THREADS ? i + 4 * THREADS : end;
+                fetch();
+                four(x);
+            }
+            all = cta_total(all);
+            if (tid == 0) put64(&sh.seg_w[rank], 0, all);
+        } else {
         __syncthreads();
         each([&](float x, uint32_t) {
             if (!(x >= r.low)) return;
@@ -331,11 +410,10 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             if (z >= BINS - 1) return;
             // (the highest keys first, as the bins of level 0)
             const uint32_t bin = level0 ? z : (key_hi - key) >> shift;
-            if (!level0 || !by_weight) atomicAdd(&sh.cnt[bin], 1u);
-            const u64 w = r.weight(x);
-            const uint32_t lo = (uint32_t)w, old = atomicAdd(&sh.lo[bin], lo), hi = (uint32_t)(w >> 32) + (old + lo < old);
-            if (hi) atomicAdd(&sh.hi[bin], hi);
+            atomicAdd(&sh.cnt[bin], 1u);
+            add(bin, r.weight(x));
         });
+        }
         cluster_sync();
         for (uint32_t i = rank * THREADS + tid; i < BINS; i += parts * THREADS) {
             uint32_t n = 0;
@@ -362,7 +440,11 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             u64 total = 0;
             for (uint32_t v = 0; v < NW; ++v) { if (v < warp) { n_to += sh.warp_t[v]; w_to += sh.warp_w[v]; } total += sh.warp_w[v]; }
             n_to -= n; w_to -= w;
-            if (level0 && by_weight) need = share(kept_w ? kept_w : total);
+            if (level0 && by_weight) {
+                total = 0;
+                for (uint32_t p = 0; p < parts; ++p) total += sh.seg_w[p];
+                need = share(kept_w ? kept_w : total);
+            }
             for (uint32_t i = 0; i < PER; ++i) {
                 const uint32_t bn = sh.all_cnt[tid * PER + i];
                 const u64 bw = sh.all_w[tid * PER + i], have = by_weight ? w_to : n_to, more = by_weight ? bw : bn;
@@ -381,15 +463,18 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         cluster_sync();
     };
 
-    uint32_t cut = 0, ties = 0xffffffffu;                        // kept: keys above cut, and the first `ties` tokens of that key
     auto narrow = [&](bool by_weight, u64 need) {
         search(true, cut, 0xffffffffu, 0, by_weight, need);
         if (sh.bin == BINS) { kept_w = sh.target; return; }      // fewer tokens than asked for: all
         if (by_weight) need = sh.target;
         u64 before_w = sh.before_w;
         u64 before = by_weight ? sh.before_w : sh.before_n;
+        keys_of(sh.bin);
+        uint32_t key_lo = max(sh.key_lo, cut), key_hi = sh.key_hi, in_n = sh.in_n;
+        u64 in_w = sh.in_w;
+        __syncthreads();
         if (by_weight) {                                         // the tokens of the bin as a list, sorted: the first that reaches the need is the last one kept
-            const uint32_t n = gather(sh.bin, sh.bin, cut);
+            const uint32_t n = gather(key_lo, key_hi);
             if (n <= LIST) {
                 if (rank == 0) {
                     sorted_sums(n, 0);
@@ -406,29 +491,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
                 cut = sh.key_lo;
                 return;
             }
-            cluster_sync();
-            if (tid == 0) sh.listed = 0;
         }
-        // the keys of the bin: the bins ascend where keys descend
-        if (warp < 2) {                                          // warp 0: the lowest key with bin <= z; warp 1: the lowest with bin < z; 32 candidates at a time
-            const uint32_t z = sh.bin;
-            u64 lo = 0, hi = (u64)key_of(r.top) + 1;             // the answer lies in [lo, hi]; hi: of warp 1 where the bin holds the maximum
-            while (lo < hi) {
-                const u64 step = (hi - lo + 31) / 32, k = lo + lane * step;
-                const float x = of_key((uint32_t)k);
-                const bool in = k < hi && !isnan(x) && x > -INFINITY && (warp == 0 ? r.bin(x) <= z : r.bin(x) < z);
-                const uint32_t mask = __ballot_sync(0xffffffffu, in || k >= hi);                 // a beginning of zeros, then ones
-                const uint32_t at = mask ? __ffs(mask) - 1 : 32;
-                const u64 new_hi = at == 32 ? hi : min(hi, lo + at * step);
-                lo = at == 0 ? new_hi : min(hi, lo + (at - 1) * step + 1);
-                hi = new_hi;
-            }
-            if (lane == 0) { if (warp == 0) sh.key_lo = (uint32_t)hi; else sh.key_hi = (uint32_t)(hi - 1); }
-        }
-        __syncthreads();
-        uint32_t key_lo = max(sh.key_lo, cut), key_hi = sh.key_hi, in_n = sh.in_n;
-        u64 in_w = sh.in_w;
-        __syncthreads();
         for (int level = 0; level < 4; ++level) {                // (32 bits at most, each search takes 11)
             // one token, or all that the bin holds: the cut is its lowest key (a lower cut found before keeps its ties)
             if (in_n == 1 || (!by_weight && need - before == in_n)) {            // (by weight, in_n is known from the second search on)
@@ -463,13 +526,14 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     // ---- the draw: sums of the warps' segments, in the order of the tokens ----
     // no token below is kept: it is below the cut, or too far from the maximum for min_p (by more than what rounding the bound to fp32 takes)
     float lowest = cut ? fmaxf(r.low, of_key(cut)) : r.low;
+    const float tie_x = ties == 0xffffffffu ? NAN : lowest;      // of the tokens of this logit only the first so many are kept
     if (ties == 0xffffffffu && least) lowest = fmaxf(lowest, (float)(r.top64 + (log((double)min_p) - 1e-3) / inv) - fabsf(r.top) * 1e-6f);
     // weight above the cut, and ties, of [lo, hi)
     auto counts = [&](float x, u64 &w, uint32_t &t) {
-        if (!(x >= lowest)) return;
         const u64 e = r.weight(x);
-        if (e < least) return;
-        if (x == lowest && ties != 0xffffffffu) ++t; else w += e;
+        const bool kept = x >= lowest && e >= least, tie = kept && x == tie_x;
+        w += kept && !tie ? e : 0;
+        t += tie;
     };
     auto segment = [&](uint32_t lo, uint32_t hi, u64 &w, uint32_t &t) {
         w = 0; t = 0;
@@ -478,8 +542,10 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             float x[8];
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * 32];
+            // (few tokens are kept as a rule: none of eight saves their weights, one of them costs eight that do not wait for one another)
+            if (fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) >= lowest)
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) counts(x[j], w, t);
+                for (uint32_t j = 0; j < 8; ++j) counts(x[j], w, t);
         }
         for (; i < hi; i += 32) counts(row[i], w, t);
         w = warp_total(w); t = warp_total(t);
