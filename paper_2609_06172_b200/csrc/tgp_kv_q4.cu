@@ -14,10 +14,12 @@
 #include "tgp.h"
 #include "tgp_kernels.h"
 #include "tgp_launch.cuh"
+#include "tgp_sm100.cuh"
 
 namespace {
 
 using namespace tgp_launch;
+using tgp_sm100::cluster_sync_all; using tgp_sm100::ld_remote_f32x2; using tgp_sm100::smem_u32;
 typedef __nv_bfloat16 bf16;
 constexpr uint32_t KEYS = 16;                    // positions that an MMA of the attention takes; a tile holds whole ones
 constexpr uint32_t E4M3_NAN = 0x7f;
@@ -202,6 +204,7 @@ struct AttnQ4Args {
     TgpTilePtrs tiles;
 };
 constexpr int WARPS = 4;
+constexpr uint32_t PARTS_MAX = 64, CLUSTER_MAX = 8;              // parts of a context, and of them those of a cluster
 constexpr float BELOW = 6.f, ABOVE = 14.f;
 
 // A chunk in shared memory: codes of its keys, codes of its values, scales of both.  A 16-byte piece of a row lies where neither the copies in nor the loads of
@@ -215,7 +218,7 @@ template <int DH, int U> struct Stage {
 };
 template <int DH, int U> constexpr int STAGES = U == 2 ? (DH == 128 ? 3 : 4) : DH == 128 ? 5 : 6;
 template <int DH, int NT, int U> constexpr uint32_t attn_smem() {
-    const uint32_t ring = WARPS * STAGES<DH, U> * Stage<DH, U>::BYTES, partial = WARPS * 8 * NT * (DH + 4 + 2) * 4;
+    const uint32_t ring = WARPS * STAGES<DH, U> * Stage<DH, U>::BYTES, partial = 8 * NT * (WARPS * (DH + 8 + 2) + 2) * 4;
     return ring > partial ? ring : partial;
 }
 
@@ -231,16 +234,17 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     return d;
 }
 
-template <int DH, int NT, int U>
+template <int DH, int NT, int U, bool CLUSTER>
 __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kernel(const AttnQ4Args a) {
     pdl_enter();
     constexpr int KS = DH / 16;                                   // MMAs of either product
-    constexpr uint32_t RB = 8 * NT, LD = DH + 4, CODES = row_codes(DH), SCALES = row_scales(DH), CHUNK = U * KEYS;
+    constexpr uint32_t RB = 8 * NT, LD = DH + 8, CODES = row_codes(DH), SCALES = row_scales(DH), CHUNK = U * KEYS;
     using St = Stage<DH, U>;
     constexpr uint32_t RING = STAGES<DH, U> * St::BYTES;
     extern __shared__ __align__(128) uint8_t q4_sm[];
     float (*part_o)[RB][LD] = reinterpret_cast<float (*)[RB][LD]>(q4_sm);                                  // (of the warps, when the chunks are done)
     float (*part_ml)[RB][2] = reinterpret_cast<float (*)[RB][2]>(q4_sm + sizeof(float) * WARPS * RB * LD);
+    float2 *cta_ml = reinterpret_cast<float2 *>(q4_sm + sizeof(float) * WARPS * RB * (LD + 2));
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     const uint32_t part = blockIdx.x, hk = blockIdx.y / a.row_blocks, row0 = (blockIdx.y - hk * a.row_blocks) * RB, b = blockIdx.z;
     const uint32_t nrows = min(RB, a.rows - row0);
@@ -257,40 +261,6 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kerne
     const uint32_t lim_first = (uint32_t)first + row0 / a.G, kvlen = (uint32_t)first + (row0 + nrows - 1) / a.G + 1;
     const uint32_t nchunks = (kvlen + CHUNK - 1) / CHUNK, p_lo = min(nchunks, part * a.per_part), p_n = min(nchunks - p_lo, a.per_part);
     const uint32_t q_lo = p_lo + p_n * warp / WARPS, q_hi = p_lo + p_n * (warp + 1) / WARPS;          // this warp's chunks
-
-    // ---- the rows of Q: fp16 has fewer exponents than bf16, so each row is scaled to [1, 2) by a power of two, which its scores get back ----
-    uint32_t qf[NT][KS][2];
-    float fix[NT][2];                                             // of the rows 2c and 2c + 1, which this lane's scores belong to
-    uint32_t lim[NT][2];                                          // the last key that these rows see
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const uint32_t row = nt * 8 + r;
-        uint4 w[DH / 32];
-#pragma unroll
-        for (int i = 0; i < DH / 32; ++i) w[i] = row < nrows ? reinterpret_cast<const uint4 *>(a.qb + out_row(row) + c * (DH / 4))[i] : make_uint4(0, 0, 0, 0);
-        const uint32_t *x = reinterpret_cast<const uint32_t *>(w);
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < DH / 8; ++i) top = max(top, max(x[i] << 16 & 0x7fff0000u, x[i] & 0x7fff0000u));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        uint32_t e = top >> 23;                                   // exponent of the largest; 0 (nothing but zeros and subnormals) and 255 (not finite) leave the row as it is
-        if (e == 0 || e == 255) e = 127;
-        // 2^(127 - e) in two factors: it has no fp32 of its own where e is at its ends
-        const uint32_t up = (254 - e) / 2, up2 = 254 - e - up;
-        const float f0 = __uint_as_float((up + 64) << 23), f1 = __uint_as_float((up2 + 63) << 23);
-#pragma unroll
-        for (int i = 0; i < DH / 8; ++i) {
-            const float lo = __uint_as_float(x[i] << 16) * f0 * f1, hi = __uint_as_float(x[i] & 0xffff0000u) * f0 * f1;
-            qf[nt][i / 2][i & 1] = pack_f16(lo, hi);
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const uint32_t ee = __shfl_sync(0xffffffffu, e, (2 * c + i) * 4);
-            fix[nt][i] = fminf(fmaxf(a.qk * __uint_as_float(ee << 23), FLT_MIN), FLT_MAX);      // (neither 0 nor infinite: a masked score is -inf, a zero one 0)
-            lim[nt][i] = (uint32_t)first + min(row0 + nt * 8 + 2 * c + i, a.rows - 1) / a.G;
-        }
-    }
 
     // ---- chunks of 16 or 32 keys (32 where a tile holds whole ones), requested STAGES - 1 ahead; the addresses of a lane's pieces run along a tile ----
     const uint64_t page = ((uint64_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
@@ -323,6 +293,39 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kerne
         asm volatile("cp.async.commit_group;" ::: "memory");
         fill = fill + St::BYTES == ring + RING ? ring : fill + St::BYTES;
     };
+#pragma unroll
+    for (int i = 0; i < STAGES<DH, U> - 1; ++i) request();
+
+    // ---- the rows of Q: fp16 has fewer exponents than bf16, so each row is scaled to [1, 2) by a power of two, which its scores get back ----
+    uint32_t qf[NT][KS][2];
+    float fix[NT][2];                                             // of the rows 2c and 2c + 1, which this lane's scores belong to
+    uint32_t lim[NT][2];                                          // the last key that these rows see
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const uint32_t row = nt * 8 + r;
+        uint4 w[DH / 32];
+#pragma unroll
+        for (int i = 0; i < DH / 32; ++i) w[i] = row < nrows ? reinterpret_cast<const uint4 *>(a.qb + out_row(row) + c * (DH / 4))[i] : make_uint4(0, 0, 0, 0);
+        const uint32_t *x = reinterpret_cast<const uint32_t *>(w);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i) top = __vmaxu2(top, x[i] & 0x7fff7fffu);
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        top = max(top << 16, top & 0x7fff0000u);
+        uint32_t e = top >> 23;                                   // exponent of the largest; 0 (nothing but zeros and subnormals) and 255 (not finite) leave the row as it is
+        if (e == 0 || e == 255) e = 127;
+        const float f = __uint_as_float(e == 254 ? 0x00400000u : (254 - e) << 23);          // 2^(127 - e), subnormal at the end
+#pragma unroll
+        for (int i = 0; i < DH / 8; ++i) qf[nt][i / 2][i & 1] = pack_f16(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xffff0000u) * f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t ee = __shfl_sync(0xffffffffu, e, (2 * c + i) * 4);
+            fix[nt][i] = fminf(fmaxf(a.qk * __uint_as_float(ee << 23), FLT_MIN), FLT_MAX);      // (neither 0 nor infinite: a masked score is -inf, a zero one 0)
+            lim[nt][i] = (uint32_t)first + min(row0 + nt * 8 + 2 * c + i, a.rows - 1) / a.G;
+        }
+    }
+
     float o[NT][KS][4], m_ref[NT][2], l[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -461,8 +464,6 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kerne
             }
         }
     };
-#pragma unroll
-    for (int i = 0; i < STAGES<DH, U> - 1; ++i) request();
     uint32_t at = ring;
     for (uint32_t q = q_lo; q < q_hi; ++q) {
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES<DH, U> - 2) : "memory");
@@ -486,52 +487,122 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kerne
             const uint32_t row = nt * 8 + 2 * c + i;
             if (r == 0) { part_ml[warp][row][0] = m_ref[nt][i]; part_ml[warp][row][1] = sum; }
 #pragma unroll
-            for (int j = 0; j < KS; ++j) *reinterpret_cast<float2 *>(&part_o[warp][row][r * (DH / 8) + 2 * j]) = make_float2(o[nt][j][i], o[nt][j][i + 2]);
+            for (int j = 0; j < KS; ++j) *reinterpret_cast<float2 *>(&part_o[warp][row][(j * 8 + r) * 2]) = make_float2(o[nt][j][i], o[nt][j][i + 2]);        // (without bank conflicts)
         }
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < nrows * DH; e += blockDim.x) {
-        const uint32_t row = e / DH, d = e % DH;
-        float M = -FLT_MAX, sum = 0.f, acc = 0.f;
+    // what a row's partial of each warp counts, and the row's reference and sum in this CTA
+    if (threadIdx.x < RB) {
+        const uint32_t row = threadIdx.x;
+        float m[WARPS], M = -FLT_MAX, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) M = fmaxf(M, part_ml[w][row][0]);
+        for (int w = 0; w < WARPS; ++w) { m[w] = part_ml[w][row][0]; M = fmaxf(M, m[w]); }
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) { const float f = ex2(m[w] - M); sum += f * part_ml[w][row][1]; part_ml[w][row][0] = f; }
+        cta_ml[row] = make_float2(M, sum);
+    }
+    __syncthreads();
+    constexpr uint32_t QUADS = DH / 4;
+    // four neighbouring dimensions d of a row: two pairs, 16 apart in shared memory
+    for (uint32_t e = threadIdx.x; e < nrows * QUADS; e += WARPS * 32) {
+        const uint32_t row = e / QUADS, q = e % QUADS, d = (q & 7) * (DH / 8) + (q >> 3) * 4, at0 = ((q >> 3) * 16 + (q & 7)) * 2;
+        float4 x[WARPS], acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const float f = ex2(part_ml[w][row][0] - M);
-            sum += f * part_ml[w][row][1];
-            acc += f * part_o[w][row][d];
+            const float2 lo = *reinterpret_cast<const float2 *>(&part_o[w][row][at0]), hi = *reinterpret_cast<const float2 *>(&part_o[w][row][at0 + 16]);
+            x[w] = make_float4(lo.x, lo.y, hi.x, hi.y);
         }
-        if (a.parts == 1) a.ob[out_row(row) + d] = __float2bfloat16_rn(acc / sum * a.v_up);
-        else {
-            float *to = a.scratch + ((((size_t)b * a.Hkv + hk) * a.rows + row0 + row) * a.parts + part) * (DH + 2);
-            if (d == 0) { to[0] = M; to[1] = sum; }
-            to[2 + d] = acc;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) { const float f = part_ml[w][row][0]; acc.x += f * x[w].x; acc.y += f * x[w].y; acc.z += f * x[w].z; acc.w += f * x[w].w; }
+        const float2 ml = cta_ml[row];
+        if (!CLUSTER && a.parts == 1) {
+            const float f = a.v_up / ml.y;
+            *reinterpret_cast<uint2 *>(a.ob + out_row(row) + d) = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
+        } else if (!CLUSTER) {                                    // the row's parts: four numbers (reference, sum, -, -), then the outputs
+            float *to = a.scratch + ((((size_t)b * a.Hkv + hk) * a.rows + row0 + row) * a.parts + part) * (DH + 4);
+            if (d == 0) *reinterpret_cast<float2 *>(to) = ml;
+            *reinterpret_cast<float4 *>(to + 4 + d) = acc;
+        } else {                                                  // (over what this thread has read)
+            *reinterpret_cast<float2 *>(&part_o[0][row][at0]) = make_float2(acc.x, acc.y);
+            *reinterpret_cast<float2 *>(&part_o[0][row][at0 + 16]) = make_float2(acc.z, acc.w);
         }
     }
+    if constexpr (!CLUSTER) return;
+    // the CTAs of a cluster are the parts of one unit: each takes a share of the outputs and reads all partials of it
+    cluster_sync_all();
+    const uint32_t share = (nrows * QUADS + a.parts - 1) / a.parts, end = min(nrows * QUADS, (part + 1) * share);
+    for (uint32_t e = part * share + threadIdx.x; e < end; e += WARPS * 32) {
+        const uint32_t row = e / QUADS, q = e % QUADS, d = (q & 7) * (DH / 8) + (q >> 3) * 4, at0 = ((q >> 3) * 16 + (q & 7)) * 2;
+        float2 ml[CLUSTER_MAX];
+        float4 x[CLUSTER_MAX];
+        float M = -FLT_MAX, sum = 0.f;
+#pragma unroll
+        for (uint32_t p = 0; p < CLUSTER_MAX; ++p)
+            if (p < a.parts) {
+                ml[p] = ld_remote_f32x2(smem_u32(&cta_ml[row]), p);
+                const float2 lo = ld_remote_f32x2(smem_u32(&part_o[0][row][at0]), p), hi = ld_remote_f32x2(smem_u32(&part_o[0][row][at0 + 16]), p);
+                x[p] = make_float4(lo.x, lo.y, hi.x, hi.y);
+            }
+#pragma unroll
+        for (uint32_t p = 0; p < CLUSTER_MAX; ++p) if (p < a.parts) M = fmaxf(M, ml[p].x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (uint32_t p = 0; p < CLUSTER_MAX; ++p)
+            if (p < a.parts) { const float f = ex2(ml[p].x - M); sum += f * ml[p].y; acc.x += f * x[p].x; acc.y += f * x[p].y; acc.z += f * x[p].z; acc.w += f * x[p].w; }
+        const float f = a.v_up / sum;
+        *reinterpret_cast<uint2 *>(a.ob + out_row(row) + d) = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
+    }
+    cluster_sync_all();                                           // no CTA leaves while another may still read its partials
 }
 
-// One CTA per row: the parts' partial results.
+// One warp per row, four or two dimensions a lane; a lane holds what a part counts, eight parts' outputs are under way at a time.
 template <int DH>
-__global__ void __launch_bounds__(DH) tgp_attn_q4_merge_kernel(const AttnQ4Args a) {
+__global__ void __launch_bounds__(128) tgp_attn_q4_merge_kernel(const AttnQ4Args a) {
     pdl_enter();
-    const uint32_t row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z, d = threadIdx.x, t = row / a.G;
+    const uint32_t row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, hk = blockIdx.y, b = blockIdx.z, t = row / a.G;
+    if (row >= a.rows) return;
     const int first = position_of(a.pos, b, a.pos0);
     if (first < 0) return;                                        // (written by the kernel before)
+    constexpr uint32_t LD = DH + 4, V = DH / 32;
     const uint32_t nchunks = ((uint32_t)first + t + a.chunk) / a.chunk, parts = (nchunks + a.per_part - 1) / a.per_part;      // those that have a key of this row
-    const float *from = a.scratch + (((size_t)b * a.Hkv + hk) * a.rows + row) * a.parts * (DH + 2);
-    float M = -FLT_MAX, sum = 0.f, acc = 0.f;
-    for (uint32_t p = 0; p < parts; ++p) M = fmaxf(M, from[p * (DH + 2)]);
-    for (uint32_t p = 0; p < parts; ++p) {
-        const float f = ex2(from[p * (DH + 2)] - M);
-        sum += f * from[p * (DH + 2) + 1];
-        acc += f * from[p * (DH + 2) + 2 + d];
+    const float *from = a.scratch + (((size_t)b * a.Hkv + hk) * a.rows + row) * a.parts * LD;
+    static_assert(PARTS_MAX == 64, "two parts a lane");
+    const float2 ml0 = lane < parts ? *reinterpret_cast<const float2 *>(from + lane * LD) : make_float2(-FLT_MAX, 0.f);
+    const float2 ml1 = lane + 32 < parts ? *reinterpret_cast<const float2 *>(from + (lane + 32) * LD) : make_float2(-FLT_MAX, 0.f);
+    float M = fmaxf(ml0.x, ml1.x);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    const float f0 = ex2(ml0.x - M), f1 = ex2(ml1.x - M);
+    float sum = f0 * ml0.y + f1 * ml1.y, acc[V];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+#pragma unroll
+    for (uint32_t i = 0; i < V; ++i) acc[i] = 0.f;
+    for (uint32_t p0 = 0; p0 < parts; p0 += 8) {
+        float x[8][V];
+#pragma unroll
+        for (uint32_t p = 0; p < 8; ++p)
+#pragma unroll
+            for (uint32_t i = 0; i < V; i += 2) {
+                const float2 w = p0 + p < parts ? *reinterpret_cast<const float2 *>(from + (p0 + p) * LD + 4 + lane * V + i) : make_float2(0.f, 0.f);
+                x[p][i] = w.x; x[p][i + 1] = w.y;
+            }
+#pragma unroll
+        for (uint32_t p = 0; p < 8; ++p) {
+            const float f = __shfl_sync(0xffffffffu, p0 + p < 32 ? f0 : f1, (p0 + p) & 31);      // (0 behind the last part: its reference is the lowest number ...
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i) acc[i] += p0 + p < parts ? f * x[p][i] : 0.f;       // ... as the others' may be, too, of a row of nothing but -inf)
+        }
     }
-    a.ob[((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row - t * a.G)) * DH + d] = __float2bfloat16_rn(acc / sum * a.v_up);
+    bf16 *to = a.ob + ((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row - t * a.G)) * DH + lane * V;
+    const float f = a.v_up / sum;
+#pragma unroll
+    for (uint32_t i = 0; i < V; i += 2) *reinterpret_cast<uint32_t *>(to + i) = pack_bf16(acc[i] * f, acc[i + 1] * f);
 }
 
 // ---- host side ---------------------------------------------------------------------------------------------------------------------
 
 constexpr uint32_t FEW_ROWS = 64;                                // query rows per KV head that the kernel above serves; of a single token any number
-constexpr uint32_t PARTS_MAX = 64, UNITS_MAX = 8192;             // parts of a context; parts of all sequences and KV heads
+constexpr uint32_t UNITS_MAX = 8192;                             // parts of all sequences and KV heads
 
 bool q4_geometry(const tgp_model_cfg *c) {
     return c && (c->Dh == 64 || c->Dh == 128) && c->Hkv && c->Hq && c->Hq % c->Hkv == 0 && c->TK && c->TK % KEYS == 0 && c->TK <= (1u << 20);
@@ -562,24 +633,35 @@ uint32_t parts_limit(const tgp_model_cfg *c, uint32_t B, uint32_t kvlen) {
 }
 
 template <int DH, int NT, int U>
-int launch_attn(const AttnQ4Args &a, uint32_t B, cudaStream_t st) {
+int launch_attn(const AttnQ4Args &a, uint32_t B, bool cluster, cudaStream_t st) {
     constexpr uint32_t smem = attn_smem<DH, NT, U>();
-    if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U>>(smem, true)) return TGP_E_CUDA;
-    const int rc = launch(tgp_attn_q4_kernel<DH, NT, U>, dim3(a.parts, a.Hkv * a.row_blocks, B), dim3(WARPS * 32), smem, st, 1, a);
+    const dim3 grid(a.parts, a.Hkv * a.row_blocks, B);
+    if (cluster && a.parts > 1) {
+        if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U, true>>(smem, true)) return TGP_E_CUDA;
+        return launch(tgp_attn_q4_kernel<DH, NT, U, true>, grid, dim3(WARPS * 32), smem, st, a.parts, a);
+    }
+    if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U, false>>(smem, true)) return TGP_E_CUDA;
+    const int rc = launch(tgp_attn_q4_kernel<DH, NT, U, false>, grid, dim3(WARPS * 32), smem, st, 1, a);
     if (rc || a.parts == 1) return rc;
-    return launch(tgp_attn_q4_merge_kernel<DH>, dim3(a.rows, a.Hkv, B), dim3(DH), 0, st, 1, a);
+    return launch(tgp_attn_q4_merge_kernel<DH>, dim3((a.rows + 3) / 4, a.Hkv, B), dim3(128), 0, st, 1, a);
 }
 
 template <int DH>
-int launch_attn(const AttnQ4Args &a, uint32_t B, cudaStream_t st) {
-    if (a.chunk == 2 * KEYS) return a.rows <= 8 ? launch_attn<DH, 1, 2>(a, B, st) : launch_attn<DH, 2, 2>(a, B, st);
-    return a.rows <= 8 ? launch_attn<DH, 1, 1>(a, B, st) : launch_attn<DH, 2, 1>(a, B, st);
+int launch_attn(const AttnQ4Args &a, uint32_t B, bool cluster, cudaStream_t st) {
+    if (a.chunk == 2 * KEYS) return a.rows <= 8 ? launch_attn<DH, 1, 2>(a, B, cluster, st) : launch_attn<DH, 2, 2>(a, B, cluster, st);
+    return a.rows <= 8 ? launch_attn<DH, 1, 1>(a, B, cluster, st) : launch_attn<DH, 2, 1>(a, B, cluster, st);
 }
 
-uint32_t few_parts(const tgp_model_cfg *c, uint32_t B, uint32_t row_blocks, uint32_t kvlen, bool ragged) {
-    const uint32_t units = B * c->Hkv * row_blocks, slots = (uint32_t)tgpk_sms() * 4 * (ragged ? 3 : 1), nchunks = (kvlen + KEYS - 1) / KEYS;
-    const uint32_t want = std::max(1u, std::min(slots / units, (nchunks + 2 * WARPS - 1) / (2 * WARPS)));
-    return std::min(want, parts_limit(c, B, kvlen));
+// Parts of each context, and whether a cluster merges them.  One wave of CTAs (four fit an SM, three with 16 rows), a chunk for every warp; twice that many where the sequences have
+// positions of their own, because most end sooner (61 of them up to 2500, us with 1 / 2 / 3 / 4 / 8 parts: 35.0 / 30.6 / 31.0 / 31.0 / 37.3).  Short parts meet in a cluster of up to
+// eight: its barrier takes longer than a second kernel once the parts do not end together (us in a cluster and through the scratch array: one sequence of 32 heads over
+// 8 x 64, 701 keys 4.2 / 5.1; five tokens of three, 2005 keys, eight parts 12.1 / 12.8; 24 sequences of 12001 keys, three parts 88 / 70).
+struct Parts { uint32_t n; bool cluster; };
+Parts few_parts(const tgp_model_cfg *c, uint32_t B, uint32_t row_blocks, uint32_t rb, uint32_t kvlen, uint32_t nchunks, bool ragged) {
+    const uint32_t units = B * c->Hkv * row_blocks, slots = (uint32_t)tgpk_sms() * (rb == 8 ? 4 : 3);
+    const uint32_t most = std::min(parts_limit(c, B, kvlen), (nchunks + WARPS - 1) / WARPS), wave = std::max(1u, std::min(slots / units, most)), close = std::min(wave, CLUSTER_MAX);
+    if (close > 1 && nchunks <= 4 * WARPS * close) return {close, true};
+    return {ragged ? std::max(1u, std::min(2 * slots / units, most)) : wave, false};
 }
 
 bool few(const tgp_model_cfg *c, uint32_t q_len) { return q_len == 1 || (uint64_t)q_len * (c->Hq / c->Hkv) <= FEW_ROWS; }
@@ -631,7 +713,7 @@ int tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64
     if (!bytes || !q4_geometry(cfg) || !cfg->B || !q_len || q_len > cfg->max_len) return TGP_E_INVAL;
     if (few(cfg, q_len)) {                                        // partial results; fewer sequences than cfg->B may have more parts each
         const uint64_t rows = (uint64_t)q_len * (cfg->Hq / cfg->Hkv), units = (uint64_t)cfg->B * cfg->Hkv, longest = std::min<uint64_t>(PARTS_MAX, ((uint64_t)cfg->max_len + 127) / 128);
-        *bytes = std::min(units * longest, std::max<uint64_t>(units, UNITS_MAX)) * rows * (cfg->Dh + 2) * sizeof(float);
+        *bytes = std::min(units * longest, std::max<uint64_t>(units, UNITS_MAX)) * rows * (cfg->Dh + 4) * sizeof(float);
     } else                                                        // keys and values as bf16
         *bytes = 2 * (uint64_t)cfg->B * cfg->Hkv * unpacked_rows(cfg->max_len) * cfg->Dh * sizeof(bf16);
     return TGP_OK;
@@ -649,10 +731,11 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
         const uint32_t rows = q_len * G, rb = rows <= 8 ? 8 : 16, row_blocks = (rows + rb - 1) / rb;
         if ((uint64_t)cfg->Hkv * row_blocks > 65535u || rows > 65535u || B > 65535u) return TGP_E_TOO_LARGE;
         const uint32_t chunk = cfg->TK % (2 * KEYS) ? KEYS : 2 * KEYS, nchunks = (kvlen + chunk - 1) / chunk;
-        const uint32_t parts = few_parts(cfg, B, row_blocks, kvlen, pos_dev != nullptr), per = (nchunks + parts - 1) / parts;
+        const Parts parts = few_parts(cfg, B, row_blocks, rb, kvlen, nchunks, pos_dev != nullptr);
+        const uint32_t per = (nchunks + parts.n - 1) / parts.n;
         AttnQ4Args a{(const bf16 *)qb, (bf16 *)ob, (float *)scratch_dev, pos_dev, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, rows, row_blocks, (nchunks + per - 1) / per, per, chunk,
                      ldexpf(1.4426950408889634f / sqrtf((float)cfg->Dh), k_exp), ldexpf(1.f, v_exp), tiles};
-        return cfg->Dh == 64 ? launch_attn<64>(a, B, st) : launch_attn<128>(a, B, st);
+        return cfg->Dh == 64 ? launch_attn<64>(a, B, parts.cluster, st) : launch_attn<128>(a, B, parts.cluster, st);
     }
     // more rows: keys and values once as bf16, exactly what the cache stands for, and the attention over a bf16 cache of one tile
     if ((uint64_t)B * cfg->Hkv > 65535u) return TGP_E_TOO_LARGE;

@@ -190,6 +190,12 @@ __device__ __forceinline__ float4 ld_remote_f32x4(uint32_t addr, uint32_t rank) 
     asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
     return v;
 }
+__device__ __forceinline__ float2 ld_remote_f32x2(uint32_t addr, uint32_t rank) {
+    uint32_t remote; float2 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(remote) : "memory");
+    return v;
+}
 __device__ __forceinline__ float ld_remote_f32(uint32_t addr, uint32_t rank) {
     uint32_t remote; float v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
