@@ -179,7 +179,8 @@ def _load_fastcall(l):
         from . import _fastcall
     except ImportError:
         return
-    _fastcall.bind(tuple(C.cast(getattr(l, "tgp_k_" + n), C.c_void_p).value for n in ("embed", "rmsnorm", "gemm", "gemm_group", "rope_kv", "attn", "swiglu", "argmax")),
+    _fastcall.bind(tuple(C.cast(getattr(l, "tgp_k_" + n), C.c_void_p).value for n in ("embed", "rmsnorm", "gemm", "gemm_group", "rope_kv", "attn", "swiglu", "argmax",
+                                                                                                         "rope_kv_q4", "kv_unpack_q4", "attn_q4", "kv_move", "sample")),
                    ModelCfg, np.ndarray)
     _fast = _fastcall
 
@@ -662,20 +663,31 @@ def k_kv_q4_tile_bytes(cfg):
 
 
 def k_rope_kv_q4(q32, k32, v32, qb, k_tiles, v_tiles, cos, sin, cfg, B, q_len, pos0, k_exp=0, v_exp=0, pos=None, stream=None):
-    ka, va, n = _tile_arrays(k_tiles, v_tiles)
-    _k(lib().tgp_k_rope_kv_q4(_ptr(q32), _ptr(k32), _ptr(v32), _ptr(qb), ka, va, n, _ptr(cos), _ptr(sin), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(stream)),
-       "tgp_k_rope_kv_q4")
+    rc = _fast.rope_kv_q4(q32, k32, v32, qb, k_tiles, v_tiles, cos, sin, cfg, B, q_len, pos0, k_exp, v_exp, pos, stream)
+    if rc is None:
+        ka, va, n = _tile_arrays(k_tiles, v_tiles)
+        rc = lib().tgp_k_rope_kv_q4(_ptr(q32), _ptr(k32), _ptr(v32), _ptr(qb), ka, va, n, _ptr(cos), _ptr(sin), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_rope_kv_q4")
 
 
 def k_kv_unpack_q4(k_tiles, v_tiles, kb, vb, cfg, B, q_len, pos0, k_exp=0, v_exp=0, pos=None, stream=None):
-    ka, va, n = _tile_arrays(k_tiles, v_tiles)
-    _k(lib().tgp_k_kv_unpack_q4(ka, va, n, _ptr(kb), _ptr(vb), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(stream)), "tgp_k_kv_unpack_q4")
+    rc = _fast.kv_unpack_q4(k_tiles, v_tiles, kb, vb, cfg, B, q_len, pos0, k_exp, v_exp, pos, stream)
+    if rc is None:
+        ka, va, n = _tile_arrays(k_tiles, v_tiles)
+        rc = lib().tgp_k_kv_unpack_q4(ka, va, n, _ptr(kb), _ptr(vb), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_kv_unpack_q4")
 
 
 def k_attn_q4(qb, k_tiles, v_tiles, ob, cfg, B, q_len, pos0, k_exp=0, v_exp=0, pos=None, scratch=None, stream=None):
     """scratch: k_attn_q4_scratch_bytes(cfg, q_len) of device memory, needed by every call."""
-    ka, va, n = _tile_arrays(k_tiles, v_tiles)
-    _k(lib().tgp_k_attn_q4(_ptr(qb), ka, va, n, _ptr(ob), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(scratch), _ptr(stream)), "tgp_k_attn_q4")
+    rc = _fast.attn_q4(qb, k_tiles, v_tiles, ob, cfg, B, q_len, pos0, k_exp, v_exp, pos, scratch, stream)
+    if rc is None:
+        ka, va, n = _tile_arrays(k_tiles, v_tiles)
+        rc = lib().tgp_k_attn_q4(_ptr(qb), ka, va, n, _ptr(ob), C.byref(cfg), B, q_len, pos0, k_exp, v_exp, _ptr(pos), _ptr(scratch), _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_attn_q4")
 
 
 def k_attn_q4_scratch_bytes(cfg, q_len):
@@ -686,12 +698,20 @@ def k_attn_q4_scratch_bytes(cfg, q_len):
 
 def k_kv_move(k_tiles, v_tiles, src, dst, cfg, form, B, length, stream=None):
     """Place dst[i] of the batch becomes what src[i] was (zeros where src[i] is -1), in every tile; form KV_BF16 or KV_Q4.  src, dst: sequences of ints."""
-    n = len(src)
-    if len(dst) != n:
-        raise ValueError(f"{n} sources and {len(dst)} destinations")
-    ka, va, tiles = _tile_arrays(k_tiles, v_tiles)
-    _k(lib().tgp_k_kv_move(ka, va, tiles, (_I32 * max(1, n))(*src), (_I32 * max(1, n))(*dst), n, C.byref(cfg), form, B, length, _ptr(stream)), "tgp_k_kv_move")
+    rc = _fast.kv_move(k_tiles, v_tiles, src, dst, cfg, form, B, length, stream)
+    if rc is None:
+        n = len(src)
+        if len(dst) != n:
+            raise ValueError(f"{n} sources and {len(dst)} destinations")
+        ka, va, tiles = _tile_arrays(k_tiles, v_tiles)
+        rc = lib().tgp_k_kv_move(ka, va, tiles, (_I32 * max(1, n))(*src), (_I32 * max(1, n))(*dst), n, C.byref(cfg), form, B, length, _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_kv_move")
 
 
 def k_sample(logits, u, out, B, V, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
-    _k(lib().tgp_k_sample(_ptr(logits), _ptr(u), _ptr(out), B, V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(stream)), "tgp_k_sample")
+    rc = _fast.sample(logits, u, out, B, V, temperature, top_k, top_p, min_p, stream)
+    if rc is None:
+        rc = lib().tgp_k_sample(_ptr(logits), _ptr(u), _ptr(out), B, V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_sample")

@@ -10,6 +10,7 @@
 #include "tgp.h"
 
 #define TILES_MAX 256
+#define PLACES_MAX 512
 
 static struct {
     int (*embed)(const void *, const int32_t *, float *, uint32_t, uint32_t, uint32_t, void *);
@@ -21,6 +22,12 @@ static struct {
     int (*attn)(const void *, void *const *, void *const *, uint32_t, void *, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, float *, void *);
     int (*swiglu)(const float *, const float *, void *, uint64_t, void *);
     int (*argmax)(const float *, int32_t *, uint32_t, uint32_t, void *);
+    int (*rope_kv_q4)(const float *, const float *, const float *, void *, void *const *, void *const *, uint32_t, const float *, const float *, const tgp_model_cfg *,
+                      uint32_t, uint32_t, uint32_t, int, int, const int32_t *, void *);
+    int (*kv_unpack_q4)(void *const *, void *const *, uint32_t, void *, void *, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, int, int, const int32_t *, void *);
+    int (*attn_q4)(const void *, void *const *, void *const *, uint32_t, void *, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, int, int, const int32_t *, void *, void *);
+    int (*kv_move)(void *const *, void *const *, uint32_t, const int32_t *, const int32_t *, uint32_t, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, void *);
+    int (*sample)(const float *, const float *, int32_t *, uint32_t, uint32_t, const float *, const int32_t *, const float *, const float *, void *);
 } lib;
 static PyObject *s_data_ptr, *s_cuda_stream, *cfg_type, *array_type;
 
@@ -202,20 +209,87 @@ static PyObject *f_argmax(PyObject *self, PyObject *const *a, Py_ssize_t nargs) 
     CALL(rc, lib.argmax(logits, out, B, V, st));
 }
 
-/* bind(addresses of the eight entry points in the order of `lib`, type of the model configuration, type of numpy's arrays) */
+/* (an exponent: a negative number is the same one as an int) */
+static int exponent(PyObject *x, int *out) { uint32_t v; if (!u32(x, &v)) return 0; *out = (int)v; return 1; }
+
+static PyObject *f_rope_kv_q4(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *q, *k, *v, *qb, *cs, *sn, *pos, *st, *kt[TILES_MAX], *vt[TILES_MAX];
+    uint32_t B, q_len, pos0;
+    int k_exp, v_exp;
+    tgp_model_cfg cfg;
+    ARGS(16);
+    const Py_ssize_t n = length(a[4]);
+    if (n < 1 || n > TILES_MAX || !address(a[0], &q) || !address(a[1], &k) || !address(a[2], &v) || !address(a[3], &qb) || !addresses(a[4], n, kt) || !addresses(a[5], n, vt) ||
+        !address(a[6], &cs) || !address(a[7], &sn) || !config(a[8], &cfg) || !u32(a[9], &B) || !u32(a[10], &q_len) || !u32(a[11], &pos0) || !exponent(a[12], &k_exp) ||
+        !exponent(a[13], &v_exp) || !address(a[14], &pos) || !address(a[15], &st)) return not_mine();
+    CALL(rc, lib.rope_kv_q4(q, k, v, qb, kt, vt, (uint32_t)n, cs, sn, &cfg, B, q_len, pos0, k_exp, v_exp, pos, st));
+}
+
+static PyObject *f_kv_unpack_q4(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *kb, *vb, *pos, *st, *kt[TILES_MAX], *vt[TILES_MAX];
+    uint32_t B, q_len, pos0;
+    int k_exp, v_exp;
+    tgp_model_cfg cfg;
+    ARGS(12);
+    const Py_ssize_t n = length(a[0]);
+    if (n < 1 || n > TILES_MAX || !addresses(a[0], n, kt) || !addresses(a[1], n, vt) || !address(a[2], &kb) || !address(a[3], &vb) || !config(a[4], &cfg) || !u32(a[5], &B) ||
+        !u32(a[6], &q_len) || !u32(a[7], &pos0) || !exponent(a[8], &k_exp) || !exponent(a[9], &v_exp) || !address(a[10], &pos) || !address(a[11], &st)) return not_mine();
+    CALL(rc, lib.kv_unpack_q4(kt, vt, (uint32_t)n, kb, vb, &cfg, B, q_len, pos0, k_exp, v_exp, pos, st));
+}
+
+static PyObject *f_attn_q4(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *qb, *ob, *pos, *scratch, *st, *kt[TILES_MAX], *vt[TILES_MAX];
+    uint32_t B, q_len, pos0;
+    int k_exp, v_exp;
+    tgp_model_cfg cfg;
+    ARGS(13);
+    const Py_ssize_t n = length(a[1]);
+    if (n < 1 || n > TILES_MAX || !address(a[0], &qb) || !addresses(a[1], n, kt) || !addresses(a[2], n, vt) || !address(a[3], &ob) || !config(a[4], &cfg) || !u32(a[5], &B) ||
+        !u32(a[6], &q_len) || !u32(a[7], &pos0) || !exponent(a[8], &k_exp) || !exponent(a[9], &v_exp) || !address(a[10], &pos) || !address(a[11], &scratch) || !address(a[12], &st)) return not_mine();
+    CALL(rc, lib.attn_q4(qb, kt, vt, (uint32_t)n, ob, &cfg, B, q_len, pos0, k_exp, v_exp, pos, scratch, st));
+}
+
+static PyObject *f_kv_move(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *st, *kt[TILES_MAX], *vt[TILES_MAX];
+    uint32_t src[PLACES_MAX], dst[PLACES_MAX], form, B, len;
+    tgp_model_cfg cfg;
+    ARGS(9);
+    const Py_ssize_t n = length(a[0]), m = length(a[2]);
+    if (n < 1 || n > TILES_MAX || m < 1 || m > PLACES_MAX || !addresses(a[0], n, kt) || !addresses(a[1], n, vt) || !numbers(a[2], m, src) || !numbers(a[3], m, dst) || !config(a[4], &cfg) ||
+        !u32(a[5], &form) || !u32(a[6], &B) || !u32(a[7], &len) || !address(a[8], &st)) return not_mine();
+    CALL(rc, lib.kv_move(kt, vt, (uint32_t)n, (const int32_t *)src, (const int32_t *)dst, (uint32_t)m, &cfg, form, B, len, st));
+}
+
+static PyObject *f_sample(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *logits, *u, *out, *t, *k, *p, *m, *st;
+    uint32_t B, V;
+    ARGS(10);
+    if (!address(a[0], &logits) || !address(a[1], &u) || !address(a[2], &out) || !u32(a[3], &B) || !u32(a[4], &V) || !address(a[5], &t) || !address(a[6], &k) || !address(a[7], &p) ||
+        !address(a[8], &m) || !address(a[9], &st)) return not_mine();
+    CALL(rc, lib.sample(logits, u, out, B, V, t, k, p, m, st));
+}
+
+#define ENTRIES 13
+/* bind(addresses of the entry points in the order of `lib`, type of the model configuration, type of numpy's arrays) */
 static PyObject *f_bind(PyObject *self, PyObject *args) {
-    unsigned long long p[8];
-    PyObject *cfg, *array;
-    if (!PyArg_ParseTuple(args, "(KKKKKKKK)OO", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &cfg, &array)) return NULL;
-    void **f = (void **)&lib;
-    for (int i = 0; i < 8; ++i) f[i] = (void *)(uintptr_t)p[i];
+    PyObject *points, *cfg, *array;
+    if (!PyArg_ParseTuple(args, "O!OO", &PyTuple_Type, &points, &cfg, &array)) return NULL;
+    if (PyTuple_GET_SIZE(points) != ENTRIES) { PyErr_SetString(PyExc_ValueError, "an address for every entry point"); return NULL; }
+    _Static_assert(sizeof(lib) == ENTRIES * sizeof(void *), "entry points");
+    void *p[ENTRIES];
+    for (int i = 0; i < ENTRIES; ++i) {
+        p[i] = (void *)(uintptr_t)PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(points, i));
+        if (PyErr_Occurred()) return NULL;
+    }
+    memcpy(&lib, p, sizeof(lib));
     Py_INCREF(cfg); Py_XSETREF(cfg_type, cfg);
     Py_INCREF(array); Py_XSETREF(array_type, array);
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))f_##name, METH_FASTCALL, NULL}
-static PyMethodDef methods[] = {{"bind", f_bind, METH_VARARGS, NULL}, FAST(embed), FAST(rmsnorm), FAST(gemm), FAST(gemm_group), FAST(rope_kv), FAST(attn), FAST(swiglu), FAST(argmax), {NULL, NULL, 0, NULL}};
+static PyMethodDef methods[] = {{"bind", f_bind, METH_VARARGS, NULL}, FAST(embed), FAST(rmsnorm), FAST(gemm), FAST(gemm_group), FAST(rope_kv), FAST(attn), FAST(swiglu), FAST(argmax),
+                                FAST(rope_kv_q4), FAST(kv_unpack_q4), FAST(attn_q4), FAST(kv_move), FAST(sample), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fastcall(void) {

@@ -11,6 +11,14 @@ from paper_2609_06172_b200 import binding as tb
 A = 4096                                                   # an address that nothing reads: every call here returns before it would
 
 
+@pytest.fixture(params=["extension", "ctypes"], autouse=True)
+def way(request, monkeypatch):
+    """Every call both ways: through the extension, which serves exact lists and integers, and through ctypes."""
+    tb.lib()
+    if request.param == "ctypes":
+        monkeypatch.setattr(tb, "_fast", tb._General())
+
+
 def cfg(**over):
     c = dict(L=1, d=256, Hq=8, Hkv=2, Dh=64, F=1, V=1, E=0, topk=0, B=4, max_len=256, TK=32, rope_base=10000.0, eps=1e-5)
     return tb.ModelCfg(**{**c, **over})
@@ -121,6 +129,18 @@ def test_sampling_refuses():
         refused(tb.E_INVAL, tb.k_sample, *args)
     refused(tb.E_TOO_LARGE, tb.k_sample, A, A, A, 1, tb.SAMPLE_MAX_V + 1)
     tb.k_sample(A, A, A, 0, 10)
+
+
+def test_other_kinds_of_arguments_are_the_same_call():
+    """Tuples, arrays and generators of numbers take the general path, with the same checks."""
+    c = cfg()
+    for src, dst in (((0, 1), (2, 2)), (np.array([0, 1]), np.array([2, 2])), ([0, 1], np.array([2, 2]))):
+        refused(tb.E_INVAL, tb.k_kv_move, (A, A), [A, A], src, dst, c, tb.KV_Q4, 4, 40)
+    refused(tb.E_INVAL, tb.k_attn_q4, A, (A,) * 8, [A] * 8, A, c, 5, 1, 10, 0, 0, None, A)
+    refused(tb.E_INVAL, tb.k_attn_q4, A, [A] * 8, [A] * 8, A, c, np.uint32(4), 1, 300, scratch=A)
+    refused(tb.E_INVAL, tb.k_sample, A, A, A, np.int64(1), 0)
+    with pytest.raises((TypeError, C.ArgumentError)):
+        tb.k_attn_q4(A, [A] * 8, [A] * 8, A, c, 4, 1, 10, 0.5, 0, None, A)
 
 
 def test_null_configurations():
