@@ -154,10 +154,10 @@ extern "C" int tgp_k_kv_move(void *const *k_tiles, void *const *v_tiles, uint32_
         a.n_steps = (uint32_t)std::min<size_t>(STEPS_MAX, steps.size() - at);
         a.n_copies = (uint32_t)std::min<size_t>(a.n_steps, n_copies > at ? n_copies - at : 0);
         std::copy(steps.begin() + at, steps.begin() + at + a.n_steps, a.steps);
-        // few steps: several pieces per thread are under way instead
-        const uint32_t U = a.n_copies > 2 ? 2 : 4;
+        // one piece a thread, four steps at a time (20 sequences of 700 positions in 4 bits 7.0 us, 8.7 with two pieces); with one or two steps, four pieces
+        const uint32_t U = a.n_copies > 2 ? 1 : 4;
         const dim3 grid((uint32_t)std::min<uint64_t>((columns * cfg->Hkv + 256 * U - 1) / (256 * U), 1u << 16), 2 * tiles);
-        if (int rc = U == 2 ? launch(tgp_kv_move_kernel<2, 4>, grid, dim3(256), 0, (cudaStream_t)stream, 1, a) : launch(tgp_kv_move_kernel<4, 2>, grid, dim3(256), 0, (cudaStream_t)stream, 1, a)) return rc;
+        if (int rc = U == 1 ? launch(tgp_kv_move_kernel<1, 4>, grid, dim3(256), 0, (cudaStream_t)stream, 1, a) : launch(tgp_kv_move_kernel<4, 2>, grid, dim3(256), 0, (cudaStream_t)stream, 1, a)) return rc;
     }
     return TGP_OK;
 } catch (const std::bad_alloc &) { return TGP_E_TOO_LARGE; }
