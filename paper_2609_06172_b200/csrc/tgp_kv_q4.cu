@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(256) tgp_rope_kv_q4_kernel(const AppendArgs a)
 
 struct UnpackArgs {
     bf16 *kb, *vb; const int32_t *pos;
-    uint32_t Hkv, TK, count, pos0, ld;                           // rows of a head in kb and vb are ld apart from head to head
+    uint32_t Hkv, TK, count, pos0, ld, no_nan;                   // rows of a head in kb and vb are ld apart from head to head; values of positions from no_nan on that stand for NaN are zeros
     float k_up, v_up;                                            // 2^exp
     TgpTilePtrs tiles;
 };
@@ -172,7 +172,9 @@ __global__ void __launch_bounds__(256) tgp_kv_unpack_q4_kernel(const UnpackArgs 
         const uint32_t t = idx / GROUPS, g = idx % GROUPS, pos = (uint32_t)first + t, tile = pos / a.TK, slot = pos - tile * a.TK;
         const uint8_t *page = reinterpret_cast<const uint8_t *>(is_v ? a.tiles.v[tile] : a.tiles.k[tile]) + ((size_t)b * a.Hkv + hk) * page_bytes(DH, a.TK);
         const uint2 w = *reinterpret_cast<const uint2 *>(page + slot * row_codes(DH) + g * 8);
-        const float s = half_lo(e4m3_f16x2(page[a.TK * row_codes(DH) + slot * row_scales(DH) + g])) * up;
+        uint32_t scale = page[a.TK * row_codes(DH) + slot * row_scales(DH) + g];
+        if (is_v && pos >= a.no_nan && (scale & 0x7fu) == E4M3_NAN) scale = 0;
+        const float s = half_lo(e4m3_f16x2(scale)) * up;
         const uint32_t h[8] = {e2m1_f16x2<0>(w.x), e2m1_f16x2<1>(w.x), e2m1_f16x2<2>(w.x), e2m1_f16x2<3>(w.x),
                                e2m1_f16x2<0>(w.y), e2m1_f16x2<1>(w.y), e2m1_f16x2<2>(w.y), e2m1_f16x2<3>(w.y)};
         uint32_t o[8];
@@ -182,6 +184,41 @@ __global__ void __launch_bounds__(256) tgp_kv_unpack_q4_kernel(const UnpackArgs 
         dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
         dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
     }
+}
+
+// A value that stands for NaN makes NaN of the queries that see it, and of no other.  The attention kernels over bf16 multiply values by weights of 0 where a query does
+// not see them, so those of a call's own positions, which only its later queries see, are unpacked as zeros (no_nan), and this kernel writes what they make of
+// the outputs: a thread looks at the scales of one new position, and as a rule nobody finds anything.
+struct NanArgs {
+    bf16 *ob;
+    uint32_t Hq, Hkv, G, TK, q_len, pos0;
+    TgpTilePtrs tiles;
+};
+template <int DH>
+__global__ void __launch_bounds__(256) tgp_attn_q4_nan_kernel(const NanArgs a) {
+    pdl_enter();
+    constexpr uint32_t GROUPS = DH / 16;
+    __shared__ uint32_t first[GROUPS];                           // the first query that sees a NaN in a group of dimensions
+    const uint32_t hk = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
+    if (threadIdx.x < GROUPS) first[threadIdx.x] = a.q_len;
+    __syncthreads();
+    const uint32_t t = blockIdx.y * blockDim.x + threadIdx.x;
+    if (t < a.q_len) {
+        const uint32_t pos = a.pos0 + t, tile = pos / a.TK, slot = pos - tile * a.TK;
+        const uint32_t *row = reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint8_t *>(a.tiles.v[tile]) + ((size_t)b * a.Hkv + hk) * page_bytes(DH, a.TK) + a.TK * row_codes(DH) + slot * row_scales(DH));
+#pragma unroll
+        for (uint32_t w = 0; w < GROUPS / 4; ++w) {
+            const uint32_t nan = __vcmpeq4(row[w] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            if (nan)
+                for (uint32_t i = 0; i < 4; ++i) if (nan >> (8 * i) & 1) atomicMin(&first[4 * w + i], t);
+        }
+    }
+    __syncthreads();
+    for (uint32_t g = 0; g < GROUPS; ++g)
+        for (uint32_t i = first[g] * a.G * 16 + threadIdx.x; i < a.q_len * a.G * 16; i += blockDim.x) {
+            const uint32_t t = i / 16 / a.G, h = i / 16 - t * a.G;
+            a.ob[((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + h) * DH + g * 16 + i % 16] = __float2bfloat16_rn(NAN);
+        }
 }
 
 // ---- attention of a few query rows ------------------------------------------------------------------------------------------------
@@ -701,7 +738,7 @@ int tgp_k_rope_kv_q4(const float *q32, const float *k32, const float *v32, void 
 int tgp_k_kv_unpack_q4(void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *kb, void *vb, const tgp_model_cfg *cfg, uint32_t B, uint32_t q_len, uint32_t pos0,
                        int k_exp, int v_exp, const int32_t *pos_dev, void *stream) {
     if (!kb || !vb || !aligned16(kb) || !aligned16(vb) || !q4_call(cfg, n_tiles, B, q_len, pos0, pos_dev, k_exp, v_exp)) return TGP_E_INVAL;
-    UnpackArgs a{(bf16 *)kb, (bf16 *)vb, pos_dev, cfg->Hkv, cfg->TK, q_len, pos0, q_len, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), {}};
+    UnpackArgs a{(bf16 *)kb, (bf16 *)vb, pos_dev, cfg->Hkv, cfg->TK, q_len, pos0, q_len, 0xffffffffu, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), {}};
     const uint32_t end = B && q_len ? (pos0 + q_len - 1) / cfg->TK + 1 : 0;
     if (int rc = q4_tiles(a.tiles, k_tiles, v_tiles, n_tiles, pos_dev ? 0 : pos0 / cfg->TK, end)) return rc;
     if (!B || !q_len) return TGP_OK;
@@ -738,16 +775,19 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
         return cfg->Dh == 64 ? launch_attn<64>(a, B, parts.cluster, st) : launch_attn<128>(a, B, parts.cluster, st);
     }
     // more rows: keys and values once as bf16, exactly what the cache stands for, and the attention over a bf16 cache of one tile
-    if ((uint64_t)B * cfg->Hkv > 65535u) return TGP_E_TOO_LARGE;
+    if ((uint64_t)B * cfg->Hkv > 65535u || q_len > 65535u * 256 || (uint64_t)q_len * G > (1u << 27)) return TGP_E_TOO_LARGE;
     const uint64_t ld = unpacked_rows(kvlen);
     bf16 *kb = (bf16 *)scratch_dev, *vb = kb + (uint64_t)B * cfg->Hkv * ld * cfg->Dh;
-    UnpackArgs u{kb, vb, nullptr, cfg->Hkv, cfg->TK, kvlen, 0, (uint32_t)ld, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), tiles};
+    UnpackArgs u{kb, vb, nullptr, cfg->Hkv, cfg->TK, kvlen, 0, (uint32_t)ld, pos0, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), tiles};
     if (int rc = launch_unpack(u, cfg, B, st)) return rc;
     tgp_model_cfg one = *cfg;
     one.TK = (uint32_t)ld;
     TgpTilePtrs whole{};
     whole.k[0] = kb; whole.v[0] = vb;
-    return tgpk_attn(qb, whole, 1, ob, &one, B, q_len, pos0, nullptr, st);
+    if (int rc = tgpk_attn(qb, whole, 1, ob, &one, B, q_len, pos0, nullptr, st)) return rc;
+    const dim3 grid(B * cfg->Hkv, (q_len + 255) / 256);
+    const NanArgs n{(bf16 *)ob, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, tiles};
+    return cfg->Dh == 64 ? launch(tgp_attn_q4_nan_kernel<64>, grid, dim3(256), 0, st, 1, n) : launch(tgp_attn_q4_nan_kernel<128>, grid, dim3(256), 0, st, 1, n);
 }
 
 }  // extern "C"

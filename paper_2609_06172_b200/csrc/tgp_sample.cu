@@ -67,6 +67,14 @@ __device__ __forceinline__ void put32(uint32_t *p, uint32_t rank, uint32_t v) { 
 __device__ __forceinline__ void put64(u64 *p, uint32_t rank, u64 v) { asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(in_cta(p, rank)), "l"(v) : "memory"); }
 
 
+// additions to shared memory under a predicate, without a branch
+__device__ __forceinline__ uint32_t atom_if(bool p, uint32_t at, uint32_t v) {
+    uint32_t old = 0;
+    asm volatile("{.reg .pred p; setp.ne.u32 p, %1, 0; @p atom.shared.add.u32 %0, [%2], %3;}" : "+r"(old) : "r"((uint32_t)p), "r"(at), "r"(v) : "memory");
+    return old;
+}
+__device__ __forceinline__ void red_if_nonzero(uint32_t at, uint32_t v) { asm volatile("{.reg .pred p; setp.ne.u32 p, %1, 0; @p red.shared.add.u32 [%0], %1;}" ::"r"(at), "r"(v) : "memory"); }
+
 template <typename T> __device__ __forceinline__ T warp_total(T v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -368,6 +376,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             const uint32_t last = z1 < (float)(BINS - 2) ? (uint32_t)fmaxf(z1, 0.f) : BINS - 2;
             __syncthreads();
             u64 all = 0;
+            const uint32_t lo_at = (uint32_t)__cvta_generic_to_shared(sh.lo), hi_at = (uint32_t)__cvta_generic_to_shared(sh.hi);
             // four at a time: their weights, then their additions to the low words, then what those carry
             auto four = [&](const float (&x)[4]) {
                 u64 w[4];
@@ -379,12 +388,9 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
                     all += z[j] < BINS ? w[j] : 0;
                 }
 #pragma unroll
-                for (int j = 0; j < 4; ++j) if (z[j] <= last) old[j] = atomicAdd(&sh.lo[z[j]], (uint32_t)w[j]);
+                for (int j = 0; j < 4; ++j) old[j] = atom_if(z[j] <= last, lo_at + z[j] * 4, (uint32_t)w[j]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t hi = z[j] <= last ? (uint32_t)(w[j] >> 32) + (old[j] + (uint32_t)w[j] < old[j]) : 0;
-                    if (hi) atomicAdd(&sh.hi[z[j]], hi);
-                }
+                for (int j = 0; j < 4; ++j) red_if_nonzero(hi_at + z[j] * 4, z[j] <= last ? (uint32_t)(w[j] >> 32) + (old[j] + (uint32_t)w[j] < old[j]) : 0);
             };
             uint32_t i = first + tid;
             float next[4];

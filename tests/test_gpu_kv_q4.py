@@ -254,7 +254,8 @@ def test_what_lies_behind_the_sequence_is_not_read(S, pos0):
     check_attn(c, 2, S, pos0, change=change, p_half=HALF_BF16 if S > 16 else HALF_FP16)
 
 
-@pytest.mark.parametrize("Dh,G,S,pos0,TK", [(64, 4, 5, 30, 16), (128, 4, 16, 10, 32), (64, 1, 9, 0, 16), (128, 2, 30, 3, 16)])
+@pytest.mark.parametrize("Dh,G,S,pos0,TK", [(64, 4, 5, 30, 16), (128, 4, 16, 10, 32), (64, 1, 9, 0, 16), (128, 2, 30, 3, 16),
+                                              (64, 4, 20, 30, 16), (128, 4, 70, 10, 32), (64, 2, 200, 40, 64), (128, 8, 130, 0, 16)])
 @pytest.mark.parametrize("side", ["k", "v"])
 def test_a_nan_reaches_the_queries_that_see_it_and_no_other(Dh, G, S, pos0, TK, side):
     """A group of a key or value stands for NaN at one of the call's own positions, which earlier queries do not see."""
@@ -265,6 +266,7 @@ def test_a_nan_reaches_the_queries_that_see_it_and_no_other(Dh, G, S, pos0, TK, 
     (kh, _), (vh, _) = random_tiles(rng, c, n_tiles, 0), random_tiles(rng, c, n_tiles, 0)
     q = bf16_round(rng.standard_normal((1, S, 2 * G, Dh)).astype(np.float32))
     clean = run_attn(c, 1, S, pos0, q, *([torch.from_numpy(t).to(DEV) for t in s] for s in (kh, vh)))
+    K, V = decoded(kh, c, 0)[0], decoded(vh, c, 0)[0]
     t = kh if side == "k" else vh
     t[at // TK, 0, head, TK * Dh // 2 + (at % TK) * Dh // 16 + group] = 0x7f
     got = run_attn(c, 1, S, pos0, q, *([torch.from_numpy(t).to(DEV) for t in s] for s in (kh, vh)))
@@ -272,7 +274,12 @@ def test_a_nan_reaches_the_queries_that_see_it_and_no_other(Dh, G, S, pos0, TK, 
     nan[0, S // 2:, head * G:] = True
     if side == "v":
         nan[..., :16 * group] = nan[..., 16 * (group + 1):] = False
-    assert np.array_equal(np.isnan(got), nan) and np.array_equal(got[~nan], clean[~nan])
+    assert np.array_equal(np.isnan(got), nan)
+    if S * G <= 64:
+        assert np.array_equal(got[~nan], clean[~nan])
+    else:                                                  # (a NaN moves the reference of the rows of its warp: other bits, by what any reference may differ)
+        want = kv_q4.attention(q[0].astype(np.float64), K, V, pos0)
+        within(np.where(nan, want[0], got)[0], *want, HALF_BF16)
 
 
 @pytest.mark.parametrize("bad", [np.inf, -np.inf, np.nan])
