@@ -236,12 +236,12 @@ __global__ void __launch_bounds__(256) tgp_attn_q4_nan_kernel(const NanArgs a) {
 // S leaves the MMA with a key per lane row, P enters the next with a key per register pair: two 8 x 8 transposes (movmatrix) of P in fp16.
 struct AttnQ4Args {
     const bf16 *qb; bf16 *ob; float *scratch; const int32_t *pos;
-    uint32_t Hq, Hkv, G, TK, q_len, pos0, rows, row_blocks, parts, per_part, chunk;      // chunk: keys of one, 16 or 32; per_part: chunks
+    uint32_t Hq, Hkv, G, TK, q_len, pos0, rows, row_blocks, parts, per_part, chunk, B;      // chunk: keys of one, 16 or 32; per_part: chunks
     float qk, v_up;                                              // score = q k * qk in units of log2; 2^v_exp
     TgpTilePtrs tiles;
 };
 constexpr int WARPS = 4;
-constexpr uint32_t PARTS_MAX = 64, CLUSTER_MAX = 8;              // parts of a context, and of them those of a cluster
+constexpr uint32_t CLUSTER_MAX = 8;
 constexpr float BELOW = 6.f, ABOVE = 14.f;
 
 // A chunk in shared memory: codes of its keys, codes of its values, scales of both.  A 16-byte piece of a row lies where neither the copies in nor the loads of
@@ -271,32 +271,26 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     return d;
 }
 
+// One unit - a sequence, a KV head and a block of rows - or some of its chunks, [c_lo, c_lo + c_n): by all warps of the CTA.  The result goes to the output, with `partial` to that array,
+// per row a reference and a sum, in four numbers, and the outputs before the division.  In a cluster (CTAs of the grid's x) the parts are merged.
 template <int DH, int NT, int U, bool CLUSTER>
-__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kernel(const AttnQ4Args a) {
-    pdl_enter();
+__device__ __forceinline__ void attend_unit(const AttnQ4Args &a, uint8_t *q4_sm, uint32_t b, uint32_t hk, uint32_t row0, int first, uint32_t c_lo, uint32_t c_n, float *partial) {
     constexpr int KS = DH / 16;                                   // MMAs of either product
     constexpr uint32_t RB = 8 * NT, LD = DH + 8, CODES = row_codes(DH), SCALES = row_scales(DH), CHUNK = U * KEYS;
     using St = Stage<DH, U>;
     constexpr uint32_t RING = STAGES<DH, U> * St::BYTES;
-    extern __shared__ __align__(128) uint8_t q4_sm[];
     float (*part_o)[RB][LD] = reinterpret_cast<float (*)[RB][LD]>(q4_sm);                                  // (of the warps, when the chunks are done)
     float (*part_ml)[RB][2] = reinterpret_cast<float (*)[RB][2]>(q4_sm + sizeof(float) * WARPS * RB * LD);
     float2 *cta_ml = reinterpret_cast<float2 *>(q4_sm + sizeof(float) * WARPS * RB * (LD + 2));
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-    const uint32_t part = blockIdx.x, hk = blockIdx.y / a.row_blocks, row0 = (blockIdx.y - hk * a.row_blocks) * RB, b = blockIdx.z;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3, part = blockIdx.x;
     const uint32_t nrows = min(RB, a.rows - row0);
     auto out_row = [&](uint32_t row) {
         const uint32_t t = (row0 + row) / a.G;
         return ((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row0 + row - t * a.G)) * DH;
     };
-    const int first = position_of(a.pos, b, a.pos0);
-    if (first < 0) {                                              // an idle sequence: its rows are zeros
-        if (part == 0) for (uint32_t e = threadIdx.x; e < nrows * DH; e += blockDim.x) a.ob[out_row(e / DH) + e % DH] = __float2bfloat16_rn(0.f);
-        return;
-    }
     // keys that this block's rows see: the last row's; the first row's tells from where on a chunk has masked ones
     const uint32_t lim_first = (uint32_t)first + row0 / a.G, kvlen = (uint32_t)first + (row0 + nrows - 1) / a.G + 1;
-    const uint32_t nchunks = (kvlen + CHUNK - 1) / CHUNK, p_lo = min(nchunks, part * a.per_part), p_n = min(nchunks - p_lo, a.per_part);
+    const uint32_t nchunks = (kvlen + CHUNK - 1) / CHUNK, p_lo = min(nchunks, c_lo), p_n = min(nchunks - p_lo, c_n);
     const uint32_t q_lo = p_lo + p_n * warp / WARPS, q_hi = p_lo + p_n * (warp + 1) / WARPS;          // this warp's chunks
 
     // ---- chunks of 16 or 32 keys (32 where a tile holds whole ones), requested STAGES - 1 ahead; the addresses of a lane's pieces run along a tile ----
@@ -551,11 +545,11 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kerne
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) { const float f = part_ml[w][row][0]; acc.x += f * x[w].x; acc.y += f * x[w].y; acc.z += f * x[w].z; acc.w += f * x[w].w; }
         const float2 ml = cta_ml[row];
-        if (!CLUSTER && a.parts == 1) {
+        if (!CLUSTER && !partial) {
             const float f = a.v_up / ml.y;
             *reinterpret_cast<uint2 *>(a.ob + out_row(row) + d) = make_uint2(pack_bf16(acc.x * f, acc.y * f), pack_bf16(acc.z * f, acc.w * f));
-        } else if (!CLUSTER) {                                    // the row's parts: four numbers (reference, sum, -, -), then the outputs
-            float *to = a.scratch + ((((size_t)b * a.Hkv + hk) * a.rows + row0 + row) * a.parts + part) * (DH + 4);
+        } else if (!CLUSTER) {
+            float *to = partial + row * (DH + 4);
             if (d == 0) *reinterpret_cast<float2 *>(to) = ml;
             *reinterpret_cast<float4 *>(to + 4 + d) = acc;
         } else {                                                  // (over what this thread has read)
@@ -591,46 +585,135 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kerne
     cluster_sync_all();                                           // no CTA leaves while another may still read its partials
 }
 
-// One warp per row, four or two dimensions a lane; a lane holds what a part counts, eight parts' outputs are under way at a time.
+template <int DH, int NT, int U, bool CLUSTER>
+__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_kernel(const AttnQ4Args a) {
+    pdl_enter();
+    extern __shared__ __align__(128) uint8_t q4_sm[];
+    const uint32_t hk = blockIdx.y / a.row_blocks, row0 = (blockIdx.y - hk * a.row_blocks) * 8 * NT, b = blockIdx.z;
+    const int first = position_of(a.pos, b, a.pos0);
+    if (first < 0) {                                              // an idle sequence: its rows are zeros
+        if (blockIdx.x == 0)
+            for (uint32_t e = threadIdx.x; e < min(8u * NT, a.rows - row0) * DH; e += WARPS * 32) {
+                const uint32_t row = row0 + e / DH, t = row / a.G;
+                a.ob[((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row - t * a.G)) * DH + e % DH] = __float2bfloat16_rn(0.f);
+            }
+        return;
+    }
+    attend_unit<DH, NT, U, CLUSTER>(a, q4_sm, b, hk, row0, first, blockIdx.x * a.per_part, a.per_part, nullptr);
+}
+
+// Contexts longer than a CTA should have to itself, and of any lengths: all chunks of all units lie in a row - sequence by sequence, in it unit by unit - and every CTA of one
+// wave takes an equal stretch of it.  What a unit costs besides its chunks, queries and merging, is as long as SETUP chunks take, and lies before them in the row (61 sequences of up
+// to 2500 keys, some of a few: 45 us without).  A unit that lies in one stretch is finished there; of others each CTA leaves a partial in the scratch array, in its place 2 i + 1 if the unit
+// goes on behind its stretch, else 2 i, which the merge kernel finds again by the same arithmetic.  The array begins with the length of a stretch and where each sequence's
+// chunks begin, which the first CTA writes for it.
+constexpr uint32_t SETUP = 12;
+struct Stretch { uint32_t per, total; };                         // (chunks; with the sequences' beginnings behind it in the scratch array)
+__device__ __host__ constexpr uint64_t stretch_bytes(uint64_t B) { return (sizeof(Stretch) + 4 * (B + 1) + 15) / 16 * 16; }
+
+template <int DH, int NT, int U>
+__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 4 : 3) tgp_attn_q4_stretch_kernel(const AttnQ4Args a) {
+    pdl_enter();
+    extern __shared__ __align__(128) uint8_t q4_sm[];
+    __shared__ uint32_t sums[WARPS], found[2];                   // of the warps' sequences; the stretch's first sequence and where its chunks begin
+    constexpr uint32_t RB = 8 * NT, CHUNK = U * KEYS;
+    const uint32_t units = a.Hkv * a.row_blocks, tid = threadIdx.x;
+    auto chunks_of = [&](uint32_t b) {
+        const int first = position_of(a.pos, b, a.pos0);
+        return first < 0 ? 0u : ((uint32_t)first + a.q_len + CHUNK - 1) / CHUNK;
+    };
+    // a thread adds up the chunks of neighbouring sequences, the threads' sums are added up
+    const uint32_t each = (a.B + WARPS * 32 - 1) / (WARPS * 32), b_lo = min(a.B, tid * each), b_hi = min(a.B, b_lo + each);
+    uint32_t mine = 0;
+    auto length_of = [&](uint32_t b) { const uint32_t n = chunks_of(b); return n ? n + SETUP : 0; };
+    for (uint32_t b = b_lo; b < b_hi; ++b) mine += length_of(b) * units;
+    uint32_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o); if ((tid & 31) >= o) upto += v; }
+    if ((tid & 31) == 31) sums[tid / 32] = upto;
+    __syncthreads();
+    uint32_t total = 0;
+#pragma unroll
+    for (uint32_t w = 0; w < WARPS; ++w) { if (w < tid / 32) upto += sums[w]; total += sums[w]; }
+    uint32_t begin = upto - mine;                                // of this thread's first sequence
+    const uint32_t per = max((total + gridDim.x - 1) / gridDim.x, SETUP + 2 * WARPS), w_lo = min(total, blockIdx.x * per), w_hi = min(total, w_lo + per);
+    Stretch *head = reinterpret_cast<Stretch *>(a.scratch);
+    uint32_t *begins = reinterpret_cast<uint32_t *>(head + 1);
+    if (blockIdx.x == 0 && tid == 0) *head = {per, total};
+    for (uint32_t b = b_lo; b < b_hi; ++b) {
+        const uint32_t n = length_of(b) * units;
+        if (blockIdx.x == 0) begins[b] = begin;
+        if (w_lo >= begin && w_lo < begin + n) { found[0] = b; found[1] = begin; }
+        begin += n;
+    }
+    __syncthreads();
+    float *partials = a.scratch + stretch_bytes(a.B) / sizeof(float);
+    uint32_t b = found[0], base = found[1];
+    for (uint32_t w = w_lo; w < w_hi;) {
+        const uint32_t n = chunks_of(b), unit = (w - base) / (n + SETUP), at = w - base - unit * (n + SETUP), end = min(n + SETUP, at + w_hi - w), hk = unit / a.row_blocks;
+        const uint32_t c_lo = at > SETUP ? at - SETUP : 0, c_hi = end > SETUP ? end - SETUP : 0;
+        if (c_hi > c_lo) {
+            if (w != w_lo) __syncthreads();                      // (the unit before is written: its shared memory is free)
+            attend_unit<DH, NT, U, false>(a, q4_sm, b, hk, (unit - hk * a.row_blocks) * RB, position_of(a.pos, b, a.pos0), c_lo, c_hi - c_lo,
+                                          c_hi - c_lo == n ? nullptr : partials + (2 * (size_t)blockIdx.x + (c_hi < n)) * RB * (DH + 4));
+        }
+        w += end - at;
+        if (w < w_hi && w == base + (n + SETUP) * units) {
+            base = w;
+            do ++b; while (!chunks_of(b));
+        }
+    }
+}
+
+// One warp per row, four or two dimensions a lane: merges what the CTAs have left of its unit, eight partials' outputs under way at a time; zeros for idle sequences.
 template <int DH>
 __global__ void __launch_bounds__(128) tgp_attn_q4_merge_kernel(const AttnQ4Args a) {
     pdl_enter();
     const uint32_t row = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x & 31, hk = blockIdx.y, b = blockIdx.z, t = row / a.G;
     if (row >= a.rows) return;
-    const int first = position_of(a.pos, b, a.pos0);
-    if (first < 0) return;                                        // (written by the kernel before)
     constexpr uint32_t LD = DH + 4, V = DH / 32;
-    const uint32_t nchunks = ((uint32_t)first + t + a.chunk) / a.chunk, parts = (nchunks + a.per_part - 1) / a.per_part;      // those that have a key of this row
-    const float *from = a.scratch + (((size_t)b * a.Hkv + hk) * a.rows + row) * a.parts * LD;
-    static_assert(PARTS_MAX == 64, "two parts a lane");
-    const float2 ml0 = lane < parts ? *reinterpret_cast<const float2 *>(from + lane * LD) : make_float2(-FLT_MAX, 0.f);
-    const float2 ml1 = lane + 32 < parts ? *reinterpret_cast<const float2 *>(from + (lane + 32) * LD) : make_float2(-FLT_MAX, 0.f);
-    float M = fmaxf(ml0.x, ml1.x);
+    const Stretch head = *reinterpret_cast<const Stretch *>(a.scratch);
+    const uint32_t begin = reinterpret_cast<const uint32_t *>(a.scratch)[2 + b];
+    const int first = position_of(a.pos, b, a.pos0);
+    bf16 *to = a.ob + ((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row - t * a.G)) * DH + lane * V;
+    if (first < 0) {
+#pragma unroll
+        for (uint32_t i = 0; i < V; i += 2) *reinterpret_cast<uint32_t *>(to + i) = 0;
+        return;
+    }
+    const uint32_t RB = a.rows <= 8 ? 8 : 16, n = ((uint32_t)first + a.q_len + a.chunk - 1) / a.chunk, at = begin + (hk * a.row_blocks + row / RB) * (n + SETUP) + SETUP;
+    const uint32_t i_lo = at / head.per, parts = (at + n - 1) / head.per - i_lo + 1;                   // stretches that the unit lies in
+    if (parts == 1) return;
+    // the partial of part p, and of the last
+    const float *from = a.scratch + stretch_bytes(a.B) / sizeof(float) + ((2 * (size_t)i_lo + 1) * RB + row % RB) * LD;
+    const uint32_t step = 2 * RB * LD;
+    auto part = [&](uint32_t p) { return from + (size_t)p * step - (p + 1 == parts ? RB * LD : 0); };
+    float M = -FLT_MAX, sum = 0.f, acc[V];
+    for (uint32_t p = lane; p < parts; p += 32) M = fmaxf(M, part(p)[0]);
 #pragma unroll
     for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    const float f0 = ex2(ml0.x - M), f1 = ex2(ml1.x - M);
-    float sum = f0 * ml0.y + f1 * ml1.y, acc[V];
-#pragma unroll
-    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
 #pragma unroll
     for (uint32_t i = 0; i < V; ++i) acc[i] = 0.f;
     for (uint32_t p0 = 0; p0 < parts; p0 += 8) {
         float x[8][V];
+        float2 ml[8];
 #pragma unroll
         for (uint32_t p = 0; p < 8; ++p)
+            if (p0 + p < parts) {
+                const float *src = part(p0 + p);
+                ml[p] = *reinterpret_cast<const float2 *>(src);
 #pragma unroll
-            for (uint32_t i = 0; i < V; i += 2) {
-                const float2 w = p0 + p < parts ? *reinterpret_cast<const float2 *>(from + (p0 + p) * LD + 4 + lane * V + i) : make_float2(0.f, 0.f);
-                x[p][i] = w.x; x[p][i + 1] = w.y;
+                for (uint32_t i = 0; i < V; i += 2) { const float2 v = *reinterpret_cast<const float2 *>(src + 4 + lane * V + i); x[p][i] = v.x; x[p][i + 1] = v.y; }
             }
 #pragma unroll
-        for (uint32_t p = 0; p < 8; ++p) {
-            const float f = __shfl_sync(0xffffffffu, p0 + p < 32 ? f0 : f1, (p0 + p) & 31);      // (0 behind the last part: its reference is the lowest number ...
+        for (uint32_t p = 0; p < 8; ++p)
+            if (p0 + p < parts) {
+                const float f = ex2(ml[p].x - M);
+                sum += f * ml[p].y;
 #pragma unroll
-            for (uint32_t i = 0; i < V; ++i) acc[i] += p0 + p < parts ? f * x[p][i] : 0.f;       // ... as the others' may be, too, of a row of nothing but -inf)
-        }
+                for (uint32_t i = 0; i < V; ++i) acc[i] += f * x[p][i];
+            }
     }
-    bf16 *to = a.ob + ((size_t)(b * a.q_len + t) * a.Hq + hk * a.G + (row - t * a.G)) * DH + lane * V;
     const float f = a.v_up / sum;
 #pragma unroll
     for (uint32_t i = 0; i < V; i += 2) *reinterpret_cast<uint32_t *>(to + i) = pack_bf16(acc[i] * f, acc[i + 1] * f);
@@ -639,7 +722,6 @@ __global__ void __launch_bounds__(128) tgp_attn_q4_merge_kernel(const AttnQ4Args
 // ---- host side ---------------------------------------------------------------------------------------------------------------------
 
 constexpr uint32_t FEW_ROWS = 64;                                // query rows per KV head that the kernel above serves; of a single token any number
-constexpr uint32_t UNITS_MAX = 8192;                             // parts of all sequences and KV heads
 
 bool q4_geometry(const tgp_model_cfg *c) {
     return c && (c->Dh == 64 || c->Dh == 128) && c->Hkv && c->Hq && c->Hq % c->Hkv == 0 && c->TK && c->TK % KEYS == 0 && c->TK <= (1u << 20);
@@ -665,40 +747,38 @@ int q4_tiles(TgpTilePtrs &t, void *const *k, void *const *v, uint32_t n, uint32_
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-uint32_t parts_limit(const tgp_model_cfg *c, uint32_t B, uint32_t kvlen) {
-    return std::max(1u, std::min({PARTS_MAX, (kvlen + 127) / 128, UNITS_MAX / std::max(1u, B * c->Hkv)}));
+// How the CTAs share the work: a CTA per unit, a cluster of `parts` per unit, or (parts 0) stretches of all units' chunks, one CTA each.
+// CTAs of one wave: four fit an SM, three with 16 rows.  A cluster's barrier takes longer than a second kernel once its parts do not end together, so it is for short parts (us in a
+// cluster and with a second kernel: one sequence of 32 heads over 8 x 64, 701 keys 4.2 / 5.1; five tokens of three, 2005 keys, eight parts 12.1 / 12.8; 24 sequences of 12001 keys, three
+// parts 88 / 70).  A unit of up to two chunks a warp is a CTA's own, and so are all units where there are several waves of equal ones.
+uint32_t wave(uint32_t rb) { return (uint32_t)tgpk_sms() * (rb == 8 ? 4 : 3); }
+uint32_t few_parts(uint32_t units, uint32_t rb, uint32_t nchunks, bool ragged) {
+    const uint32_t close = std::min({std::max(1u, wave(rb) / units), CLUSTER_MAX, (nchunks + WARPS - 1) / WARPS});
+    if (close > 1 && nchunks <= 4 * WARPS * close) return close;
+    return nchunks <= 2 * WARPS || (!ragged && units >= 4 * wave(rb)) ? 1 : 0;
 }
 
 template <int DH, int NT, int U>
-int launch_attn(const AttnQ4Args &a, uint32_t B, bool cluster, cudaStream_t st) {
+int launch_attn(const AttnQ4Args &a, cudaStream_t st) {
     constexpr uint32_t smem = attn_smem<DH, NT, U>();
-    const dim3 grid(a.parts, a.Hkv * a.row_blocks, B);
-    if (cluster && a.parts > 1) {
+    const dim3 grid(a.parts, a.Hkv * a.row_blocks, a.B), block(WARPS * 32);
+    if (a.parts > 1) {
         if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U, true>>(smem, true)) return TGP_E_CUDA;
-        return launch(tgp_attn_q4_kernel<DH, NT, U, true>, grid, dim3(WARPS * 32), smem, st, a.parts, a);
+        return launch(tgp_attn_q4_kernel<DH, NT, U, true>, grid, block, smem, st, a.parts, a);
     }
-    if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U, false>>(smem, true)) return TGP_E_CUDA;
-    const int rc = launch(tgp_attn_q4_kernel<DH, NT, U, false>, grid, dim3(WARPS * 32), smem, st, 1, a);
-    if (rc || a.parts == 1) return rc;
-    return launch(tgp_attn_q4_merge_kernel<DH>, dim3((a.rows + 3) / 4, a.Hkv, B), dim3(128), 0, st, 1, a);
+    if (a.parts == 1) {
+        if (!tgpk_allow_smem<tgp_attn_q4_kernel<DH, NT, U, false>>(smem, true)) return TGP_E_CUDA;
+        return launch(tgp_attn_q4_kernel<DH, NT, U, false>, grid, block, smem, st, 1, a);
+    }
+    if (!tgpk_allow_smem<tgp_attn_q4_stretch_kernel<DH, NT, U>>(smem, true)) return TGP_E_CUDA;
+    if (int rc = launch(tgp_attn_q4_stretch_kernel<DH, NT, U>, dim3(wave(8 * NT)), block, smem, st, 1, a)) return rc;
+    return launch(tgp_attn_q4_merge_kernel<DH>, dim3((a.rows + 3) / 4, a.Hkv, a.B), dim3(128), 0, st, 1, a);
 }
 
 template <int DH>
-int launch_attn(const AttnQ4Args &a, uint32_t B, bool cluster, cudaStream_t st) {
-    if (a.chunk == 2 * KEYS) return a.rows <= 8 ? launch_attn<DH, 1, 2>(a, B, cluster, st) : launch_attn<DH, 2, 2>(a, B, cluster, st);
-    return a.rows <= 8 ? launch_attn<DH, 1, 1>(a, B, cluster, st) : launch_attn<DH, 2, 1>(a, B, cluster, st);
-}
-
-// Parts of each context, and whether a cluster merges them.  One wave of CTAs (four fit an SM, three with 16 rows), a chunk for every warp; twice that many where the sequences have
-// positions of their own, because most end sooner (61 of them up to 2500, us with 1 / 2 / 3 / 4 / 8 parts: 35.0 / 30.6 / 31.0 / 31.0 / 37.3).  Short parts meet in a cluster of up to
-// eight: its barrier takes longer than a second kernel once the parts do not end together (us in a cluster and through the scratch array: one sequence of 32 heads over
-// 8 x 64, 701 keys 4.2 / 5.1; five tokens of three, 2005 keys, eight parts 12.1 / 12.8; 24 sequences of 12001 keys, three parts 88 / 70).
-struct Parts { uint32_t n; bool cluster; };
-Parts few_parts(const tgp_model_cfg *c, uint32_t B, uint32_t row_blocks, uint32_t rb, uint32_t kvlen, uint32_t nchunks, bool ragged) {
-    const uint32_t units = B * c->Hkv * row_blocks, slots = (uint32_t)tgpk_sms() * (rb == 8 ? 4 : 3);
-    const uint32_t most = std::min(parts_limit(c, B, kvlen), (nchunks + WARPS - 1) / WARPS), wave = std::max(1u, std::min(slots / units, most)), close = std::min(wave, CLUSTER_MAX);
-    if (close > 1 && nchunks <= 4 * WARPS * close) return {close, true};
-    return {ragged ? std::max(1u, std::min(2 * slots / units, most)) : wave, false};
+int launch_attn(const AttnQ4Args &a, cudaStream_t st) {
+    if (a.chunk == 2 * KEYS) return a.rows <= 8 ? launch_attn<DH, 1, 2>(a, st) : launch_attn<DH, 2, 2>(a, st);
+    return a.rows <= 8 ? launch_attn<DH, 1, 1>(a, st) : launch_attn<DH, 2, 1>(a, st);
 }
 
 bool few(const tgp_model_cfg *c, uint32_t q_len) { return q_len == 1 || (uint64_t)q_len * (c->Hq / c->Hkv) <= FEW_ROWS; }
@@ -748,9 +828,9 @@ int tgp_k_kv_unpack_q4(void *const *k_tiles, void *const *v_tiles, uint32_t n_ti
 
 int tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64_t *bytes) {
     if (!bytes || !q4_geometry(cfg) || !cfg->B || !q_len || q_len > cfg->max_len) return TGP_E_INVAL;
-    if (few(cfg, q_len)) {                                        // partial results; fewer sequences than cfg->B may have more parts each
-        const uint64_t rows = (uint64_t)q_len * (cfg->Hq / cfg->Hkv), units = (uint64_t)cfg->B * cfg->Hkv, longest = std::min<uint64_t>(PARTS_MAX, ((uint64_t)cfg->max_len + 127) / 128);
-        *bytes = std::min(units * longest, std::max<uint64_t>(units, UNITS_MAX)) * rows * (cfg->Dh + 4) * sizeof(float);
+    if (few(cfg, q_len)) {                                        // two partial results for each CTA of a wave
+        const uint64_t rb = (uint64_t)q_len * (cfg->Hq / cfg->Hkv) <= 8 ? 8 : 16;
+        *bytes = stretch_bytes(cfg->B) + 2ull * wave((uint32_t)rb) * rb * (cfg->Dh + 4) * sizeof(float);
     } else                                                        // keys and values as bf16
         *bytes = 2 * (uint64_t)cfg->B * cfg->Hkv * unpacked_rows(cfg->max_len) * cfg->Dh * sizeof(bf16);
     return TGP_OK;
@@ -768,11 +848,11 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
         const uint32_t rows = q_len * G, rb = rows <= 8 ? 8 : 16, row_blocks = (rows + rb - 1) / rb;
         if ((uint64_t)cfg->Hkv * row_blocks > 65535u || rows > 65535u || B > 65535u) return TGP_E_TOO_LARGE;
         const uint32_t chunk = cfg->TK % (2 * KEYS) ? KEYS : 2 * KEYS, nchunks = (kvlen + chunk - 1) / chunk;
-        const Parts parts = few_parts(cfg, B, row_blocks, rb, kvlen, nchunks, pos_dev != nullptr);
-        const uint32_t per = (nchunks + parts.n - 1) / parts.n;
-        AttnQ4Args a{(const bf16 *)qb, (bf16 *)ob, (float *)scratch_dev, pos_dev, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, rows, row_blocks, (nchunks + per - 1) / per, per, chunk,
-                     ldexpf(1.4426950408889634f / sqrtf((float)cfg->Dh), k_exp), ldexpf(1.f, v_exp), tiles};
-        return cfg->Dh == 64 ? launch_attn<64>(a, B, parts.cluster, st) : launch_attn<128>(a, B, parts.cluster, st);
+        if ((uint64_t)B * cfg->Hkv * row_blocks * (nchunks + SETUP) > 0x7fffffffu) return TGP_E_TOO_LARGE;
+        const uint32_t parts = few_parts(B * cfg->Hkv * row_blocks, rb, nchunks, pos_dev != nullptr);
+        AttnQ4Args a{(const bf16 *)qb, (bf16 *)ob, (float *)scratch_dev, pos_dev, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, rows, row_blocks, parts, parts ? (nchunks + parts - 1) / parts : 0,
+                     chunk, B, ldexpf(1.4426950408889634f / sqrtf((float)cfg->Dh), k_exp), ldexpf(1.f, v_exp), tiles};
+        return cfg->Dh == 64 ? launch_attn<64>(a, st) : launch_attn<128>(a, st);
     }
     // more rows: keys and values once as bf16, exactly what the cache stands for, and the attention over a bf16 cache of one tile
     if ((uint64_t)B * cfg->Hkv > 65535u || q_len > 65535u * 256 || (uint64_t)q_len * G > (1u << 27)) return TGP_E_TOO_LARGE;
