@@ -747,15 +747,24 @@ int q4_tiles(TgpTilePtrs &t, void *const *k, void *const *v, uint32_t n, uint32_
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// How the CTAs share the work: a CTA per unit, a cluster of `parts` per unit, or (parts 0) stretches of all units' chunks, one CTA each.
-// CTAs of one wave: four fit an SM, three with 16 rows.  A cluster's barrier takes longer than a second kernel once its parts do not end together, so it is for short parts (us in a
-// cluster and with a second kernel: one sequence of 32 heads over 8 x 64, 701 keys 4.2 / 5.1; five tokens of three, 2005 keys, eight parts 12.1 / 12.8; 24 sequences of 12001 keys, three
-// parts 88 / 70).  A unit of up to two chunks a warp is a CTA's own, and so are all units where there are several waves of equal ones.
+// How the CTAs share the work: 1, a CTA per unit; 2 - 8, a cluster of as many per unit; 0, stretches of all units' chunks.  By what each is expected to take, in chunks of a CTA on a full SM:
+// what a unit costs besides its chunks (SETUP), a cluster's barriers and that its parts do not end together, a second kernel.  The ways' times (us, 32-key chunks, one CTA / cluster / stretches):
+// 61 sequences of 701 keys, 32 heads over 8 x 128 15.2 / - / 20.0; 200 of 601, x 64 22.8 / - / 29.7; 16 of 2112, 64 over 8 x 128 25.7 / 14.7 (four) / 18.4; one of 4001, 32 over 8 x 64
+// 21 / 6.1 (eight) / 9.8; one of 16001, x 128 108 / 17.5 (eight) / 15.8; four of these 109 / 32.4 (eight) / 25.2; 24 of 12001, 64 over 8 109 / 88 (three) / 71; 61 of up to 2500 at positions of their
+// own 35 / 38 (two) / 27.4.  CTAs of a wave: four fit an SM, three with 16 rows.
 uint32_t wave(uint32_t rb) { return (uint32_t)tgpk_sms() * (rb == 8 ? 4 : 3); }
-uint32_t few_parts(uint32_t units, uint32_t rb, uint32_t nchunks, bool ragged) {
-    const uint32_t close = std::min({std::max(1u, wave(rb) / units), CLUSTER_MAX, (nchunks + WARPS - 1) / WARPS});
-    if (close > 1 && nchunks <= 4 * WARPS * close) return close;
-    return nchunks <= 2 * WARPS || (!ragged && units >= 4 * wave(rb)) ? 1 : 0;
+uint32_t few_parts(uint32_t units, uint32_t rb, uint32_t n, bool ragged) {
+    const uint32_t slots = wave(rb);
+    const float mean = ragged ? 0.5f * (float)n : (float)n;      // positions of their own: the longest is known, not the mean
+    float best = std::max((float)(SETUP + 2 * WARPS), (mean + SETUP) * (float)units / (float)slots) + 32.f;
+    uint32_t way = 0;
+    const float alone = (float)((units + slots - 1) / slots) * (float)(SETUP + n);
+    if (alone <= best) { best = alone; way = 1; }
+    for (uint32_t p = 2; p <= CLUSTER_MAX && p <= (n + WARPS - 1) / WARPS && (uint64_t)units * p <= slots; ++p) {
+        const float together = (float)(SETUP + 5) + 1.3f * (float)((n + p - 1) / p);
+        if (together < best) { best = together; way = p; }
+    }
+    return way;
 }
 
 template <int DH, int NT, int U>
