@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(128) tgp_attn_q4_merge_kernel(const AttnQ4Args
 
 // ---- host side ---------------------------------------------------------------------------------------------------------------------
 
-constexpr uint32_t FEW_ROWS = 64;                                // query rows per KV head that the kernel above serves; of a single token any number
+constexpr uint32_t UNPACK_FROM = 128;                            // queries from which on the cache may be unpacked and the tcgen05 kernel run on it
 
 bool q4_geometry(const tgp_model_cfg *c) {
     return c && (c->Dh == 64 || c->Dh == 128) && c->Hkv && c->Hq && c->Hq % c->Hkv == 0 && c->TK && c->TK % KEYS == 0 && c->TK <= (1u << 20);
@@ -790,7 +790,16 @@ int launch_attn(const AttnQ4Args &a, cudaStream_t st) {
     return a.rows <= 8 ? launch_attn<DH, 1, 1>(a, st) : launch_attn<DH, 2, 1>(a, st);
 }
 
-bool few(const tgp_model_cfg *c, uint32_t q_len) { return q_len == 1 || (uint64_t)q_len * (c->Hq / c->Hkv) <= FEW_ROWS; }
+uint32_t rows_of_block(const tgp_model_cfg *c, uint32_t q_len) { return (uint64_t)q_len * (c->Hq / c->Hkv) <= 8 ? 8 : 16; }
+
+// Does a call read the codes itself?  Below 128 queries always: unpacked, the cache would be the mma.sync kernel's, or the CUDA-core one's (us, codes / unpacked: 3 sequences of 2000 keys, 32 heads
+// over 8 x 128, 8 queries 12.6 / 1236, 32 24.5 / 92, 127 75 / 98; 64 heads, 127 queries 144 / 159).  Above, each block of 16 rows converts the cache again, while the tcgen05 kernel's time is the
+// chain of its key blocks: where the blocks fill little of the GPU (us, 200 queries of one sequence: 8 heads x 128, 8200 keys 42.7 / 61.6, 700 keys 11.8 / 13.3; 32 heads over 8, 8200 keys 131 / 63).
+bool reads_codes(const tgp_model_cfg *c, uint32_t B, uint32_t q_len, uint32_t kvlen) {
+    if (q_len < UNPACK_FROM) return true;
+    const float units = (float)B * (float)c->Hkv * (float)(((uint64_t)q_len * (c->Hq / c->Hkv) + 15) / 16), n = (float)kvlen / 32.f;
+    return 0.6f * units * (n + 12.f) <= (2.f + 0.225f * n) * 444.f;
+}
 
 uint64_t unpacked_rows(uint32_t kvlen) { return ((uint64_t)kvlen + 63) / 64 * 64; }
 
@@ -837,11 +846,9 @@ int tgp_k_kv_unpack_q4(void *const *k_tiles, void *const *v_tiles, uint32_t n_ti
 
 int tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64_t *bytes) {
     if (!bytes || !q4_geometry(cfg) || !cfg->B || !q_len || q_len > cfg->max_len) return TGP_E_INVAL;
-    if (few(cfg, q_len)) {                                        // two partial results for each CTA of a wave
-        const uint64_t rb = (uint64_t)q_len * (cfg->Hq / cfg->Hkv) <= 8 ? 8 : 16;
-        *bytes = stretch_bytes(cfg->B) + 2ull * wave((uint32_t)rb) * rb * (cfg->Dh + 4) * sizeof(float);
-    } else                                                        // keys and values as bf16
-        *bytes = 2 * (uint64_t)cfg->B * cfg->Hkv * unpacked_rows(cfg->max_len) * cfg->Dh * sizeof(bf16);
+    const uint64_t rb = rows_of_block(cfg, q_len);                // two partial results for each CTA of a wave; keys and values as bf16
+    *bytes = stretch_bytes(cfg->B) + 2ull * wave((uint32_t)rb) * rb * (cfg->Dh + 4) * sizeof(float);
+    if (q_len >= UNPACK_FROM) *bytes = std::max(*bytes, 2 * (uint64_t)cfg->B * cfg->Hkv * unpacked_rows(cfg->max_len) * cfg->Dh * sizeof(bf16));
     return TGP_OK;
 }
 
@@ -853,9 +860,10 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
     if (int rc = q4_tiles(tiles, k_tiles, v_tiles, n_tiles, 0, B && q_len ? (kvlen - 1) / cfg->TK + 1 : 0)) return rc;
     if (!B || !q_len) return TGP_OK;
     cudaStream_t st = (cudaStream_t)stream;
-    if (few(cfg, q_len)) {
-        const uint32_t rows = q_len * G, rb = rows <= 8 ? 8 : 16, row_blocks = (rows + rb - 1) / rb;
-        if ((uint64_t)cfg->Hkv * row_blocks > 65535u || rows > 65535u || B > 65535u) return TGP_E_TOO_LARGE;
+    if (reads_codes(cfg, B, q_len, kvlen)) {
+        if ((uint64_t)q_len * G > 1u << 20) return TGP_E_TOO_LARGE;
+        const uint32_t rows = q_len * G, rb = rows_of_block(cfg, q_len), row_blocks = (rows + rb - 1) / rb;
+        if ((uint64_t)cfg->Hkv * row_blocks > 65535u || B > 65535u) return TGP_E_TOO_LARGE;
         const uint32_t chunk = cfg->TK % (2 * KEYS) ? KEYS : 2 * KEYS, nchunks = (kvlen + chunk - 1) / chunk;
         if ((uint64_t)B * cfg->Hkv * row_blocks * (nchunks + SETUP) > 0x7fffffffu) return TGP_E_TOO_LARGE;
         const uint32_t parts = few_parts(B * cfg->Hkv * row_blocks, rb, nchunks, pos_dev != nullptr);
