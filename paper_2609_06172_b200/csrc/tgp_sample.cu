@@ -227,6 +227,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     r.octave = sh.octave;
     if (r.top == INFINITY) r.top64 = 0.0;
     const u64 least = min_p > 0.f ? (u64)ceil((double)min_p * ONE) : 0;
+    const uint32_t per_warp = (a.per + NW - 1) / NW, lo = min(end, first + warp * per_warp), hi = min(end, lo + per_warp);      // this warp's segment of the row, for the draw
 
     // ---- the keys of a bin, as key_lo and key_hi of every CTA's Shared: bins ascend where keys descend.  Warp 0: the lowest key with bin <= z; warp 1: the lowest
     // with bin < z; 32 candidates at a time ----
@@ -247,15 +248,8 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         }
         __syncthreads();
     };
-    // ---- tokens whose key is in [key_lo, key_hi], which are those of numbers, as a list in the first CTA; how many there are (more than LIST: there is no list).
-    // Each CTA lists its own, then the others send theirs behind the first one's. ----
-    auto gather = [&](uint32_t key_lo, uint32_t key_hi) {
-        const float x_lo = of_key(key_lo), x_hi = of_key(key_hi);
-        each([&](float x, uint32_t i) {
-            if (!(x >= x_lo && x <= x_hi)) return;
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i;
-        });
+    // the lists that the CTAs have made, behind one another in the first one's; how many tokens they hold (more than LIST: there is no list)
+    auto send_lists = [&]() {
         __syncthreads();
         const uint32_t n = sh.listed;
         if (tid < parts) put32(&sh.counts[rank], tid, n);
@@ -266,6 +260,16 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         if (tid == 0) sh.listed = 0;
         cluster_sync();
         return all;
+    };
+    // ---- tokens whose key is in [key_lo, key_hi], which are those of numbers, as a list in the first CTA ----
+    auto gather = [&](uint32_t key_lo, uint32_t key_hi) {
+        const float x_lo = of_key(key_lo), x_hi = of_key(key_hi);
+        each([&](float x, uint32_t i) {
+            if (!(x >= x_lo && x <= x_hi)) return;
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i;
+        });
+        return send_lists();
     };
     // (first CTA) sorts n listed tokens, and gives the running sums of their weights: of their logits, or of the numbers in the low `bits`
     auto sorted_sums = [&](uint32_t n, uint32_t bits) {
@@ -352,6 +356,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     // the need is top_p of all (of kept_w), which goes to `target` ----
     u64 kept_w = 0;                                              // what the tokens kept so far weigh, once a search has told
     uint32_t cut = 0, ties = 0xffffffffu;                        // kept: keys above cut, and the first `ties` tokens of that key
+    bool summed = false;                                         // the first CTA has the segments' sums, and what is kept is in key_lo (the cut) and key_hi (ties)
     auto search = [&](bool level0, uint32_t key_lo, uint32_t key_hi, uint32_t shift, bool by_weight, u64 need) {
         for (uint32_t i = tid; i < BINS; i += THREADS) { sh.cnt[i] = 0; sh.lo[i] = 0; sh.hi[i] = 0; }
         auto add = [&](uint32_t bin, u64 w) {
@@ -479,22 +484,48 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         uint32_t key_lo = max(sh.key_lo, cut), key_hi = sh.key_hi, in_n = sh.in_n;
         u64 in_w = sh.in_w;
         __syncthreads();
-        if (by_weight) {                                         // the tokens of the bin as a list, sorted: the first that reaches the need is the last one kept
-            const uint32_t n = gather(key_lo, key_hi);
+        if (by_weight) {
+            // One pass lists the tokens of the bin and adds up the weights above it, by segment.  The first CTA sorts the list: the first token that reaches the need is the last
+            // one kept, and those before it are added to their segments' sums.
+            const float x_lo = of_key(key_lo), x_hi = of_key(key_hi);
+            u64 w = 0;
+            auto look = [&](float x, uint32_t i) {
+                if (x > x_hi) { const u64 e = r.weight(x); w += e >= least ? e : 0; }
+                else if (x >= x_lo) { const uint32_t at = atomicAdd(&sh.listed, 1u); if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i; }
+            };
+            uint32_t i = lo + lane;
+            for (; i < hi && hi - i > 7 * 32; i += 8 * 32) {
+                float x[8];
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * 32];
+                if (fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) >= x_lo)
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) look(x[j], i + j * 32);
+            }
+            for (; i < hi; i += 32) look(row[i], i);
+            w = warp_total(w);
+            if (lane == 0) { put64(&sh.seg_w[rank * NW + warp], 0, w); put32(&sh.seg_t[rank * NW + warp], 0, 0); }
+            const uint32_t n = send_lists();
             if (n <= LIST) {
-                if (rank == 0) {
-                    sorted_sums(n, 0);
-                    for (uint32_t i = tid; i < n; i += THREADS)
-                        if ((i ? sh.sums[i - 1] : 0) < need - before && sh.sums[i] >= need - before) {
-                            const uint32_t key = (uint32_t)(sh.list[i] >> 32);
-                            uint32_t same = 1;
-                            for (uint32_t j = i; j && (uint32_t)(sh.list[j - 1] >> 32) == key; --j) ++same;
-                            for (uint32_t p = 0; p < parts; ++p) { put32(&sh.key_lo, p, key); put32(&sh.key_hi, p, same); }
-                        }
+                summed = true;
+                if (rank) return;
+                sorted_sums(n, 0);
+                for (uint32_t j = tid; j < n; j += THREADS)
+                    if ((j ? sh.sums[j - 1] : 0) < need - before && sh.sums[j] >= need - before) {
+                        const uint32_t key = (uint32_t)(sh.list[j] >> 32);
+                        uint32_t same = 1;
+                        for (uint32_t k = j; k && (uint32_t)(sh.list[k - 1] >> 32) == key; --k) ++same;
+                        sh.bin = j;
+                        for (uint32_t p = 0; p < parts; ++p) { put32(&sh.key_lo, p, key); put32(&sh.key_hi, p, same); }
+                    }
+                __syncthreads();
+                for (uint32_t j = tid; j <= sh.bin; j += THREADS) {
+                    const uint32_t i = ~(uint32_t)sh.list[j], part = i / a.per, seg = part * NW + (i - part * a.per) / per_warp;
+                    const u64 e = sh.sums[j] - (j ? sh.sums[j - 1] : 0);
+                    if (e < least) continue;
+                    if ((uint32_t)(sh.list[j] >> 32) == sh.key_lo) atomicAdd(&sh.seg_t[seg], 1u); else atomicAdd(&sh.seg_w[seg], e);
                 }
-                cluster_sync();
-                ties = sh.key_lo == cut ? min(ties, sh.key_hi) : sh.key_hi;
-                cut = sh.key_lo;
+                __syncthreads();
                 return;
             }
         }
@@ -525,15 +556,19 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         }
     };
     if (top_k > 0 && (uint32_t)top_k < a.V) narrow(false, (u64)top_k);
-    if (top_p < 1.f) {
-        narrow(true, 0);
-    }
+    if (top_p < 1.f) narrow(true, 0);
 
     // ---- the draw: sums of the warps' segments, in the order of the tokens ----
-    // no token below is kept: it is below the cut, or too far from the maximum for min_p (by more than what rounding the bound to fp32 takes)
-    float lowest = cut ? fmaxf(r.low, of_key(cut)) : r.low;
-    const float tie_x = ties == 0xffffffffu ? NAN : lowest;      // of the tokens of this logit only the first so many are kept
-    if (ties == 0xffffffffu && least) lowest = fmaxf(lowest, (float)(r.top64 + (log((double)min_p) - 1e-3) / inv) - fabsf(r.top) * 1e-6f);
+    float lowest, tie_x;                                         // no token below is kept; of the tokens of logit tie_x only the first so many are
+    u64 tie_w;
+    auto bounds = [&]() {
+        if (summed) { ties = sh.key_lo == cut ? min(ties, sh.key_hi) : sh.key_hi; cut = sh.key_lo; }
+        lowest = cut ? fmaxf(r.low, of_key(cut)) : r.low;
+        tie_x = ties == 0xffffffffu ? NAN : lowest;
+        tie_w = cut && ties != 0xffffffffu ? r.weight(of_key(cut)) : 0;
+        // too far from the maximum for min_p (by more than what rounding the bound to fp32 takes)
+        if (ties == 0xffffffffu && least) lowest = fmaxf(lowest, (float)(r.top64 + (log((double)min_p) - 1e-3) / inv) - fabsf(r.top) * 1e-6f);
+    };
     // weight above the cut, and ties, of [lo, hi)
     auto counts = [&](float x, u64 &w, uint32_t &t) {
         const u64 e = r.weight(x);
@@ -556,14 +591,13 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         for (; i < hi; i += 32) counts(row[i], w, t);
         w = warp_total(w); t = warp_total(t);
     };
-    const u64 tie_w = cut && ties != 0xffffffffu ? r.weight(of_key(cut)) : 0;
-    const uint32_t per_warp = (a.per + NW - 1) / NW, lo = min(end, first + warp * per_warp), hi = min(end, lo + per_warp);
-    {
+    if (!summed || rank == 0) bounds();
+    if (!summed) {
         u64 w; uint32_t t;
         segment(lo, hi, w, t);
         if (lane == 0) { put64(&sh.seg_w[rank * NW + warp], 0, w); put32(&sh.seg_t[rank * NW + warp], 0, t); }
+        cluster_sync();
     }
-    cluster_sync();
     if (rank == 0 && warp == 0) {                                // four segments a lane: ties before them, then weight before them
         constexpr uint32_t PER = CLUSTER_MAX * NW / 32;
         uint32_t t[PER], all = 0;
@@ -590,6 +624,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         }
     }
     cluster_sync();
+    if (summed && rank) bounds();
     // ---- the CTA of the segment: its warps take a sixteenth of it each, then the one into which the rest of the target falls goes through its part ----
     if (sh.seg / NW != rank) return;
     const uint32_t s_lo = min(end, first + sh.seg % NW * per_warp), s_hi = min(end, s_lo + per_warp), per_part = (s_hi - s_lo + NW - 1) / NW;
