@@ -489,20 +489,23 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             // one kept, and those before it are added to their segments' sums.
             const float x_lo = of_key(key_lo), x_hi = of_key(key_hi);
             u64 w = 0;
-            auto look = [&](float x, uint32_t i) {
-                if (x > x_hi) { const u64 e = r.weight(x); w += e >= least ? e : 0; }
-                else if (x >= x_lo) { const uint32_t at = atomicAdd(&sh.listed, 1u); if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i; }
+            auto weigh = [&](float x) { const u64 e = r.weight(x); w += x > x_hi && e >= least ? e : 0; };
+            auto list = [&](float x, uint32_t i) {
+                if (x >= x_lo && x <= x_hi) { const uint32_t at = atomicAdd(&sh.listed, 1u); if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i; }
             };
             uint32_t i = lo + lane;
             for (; i < hi && hi - i > 7 * 32; i += 8 * 32) {
                 float x[8];
 #pragma unroll
                 for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * 32];
-                if (fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) >= x_lo)
+                if (fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) >= x_lo) {
 #pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) look(x[j], i + j * 32);
+                    for (uint32_t j = 0; j < 8; ++j) weigh(x[j]);
+#pragma unroll
+                    for (uint32_t j = 0; j < 8; ++j) list(x[j], i + j * 32);
+                }
             }
-            for (; i < hi; i += 32) look(row[i], i);
+            for (; i < hi; i += 32) { weigh(row[i]); list(row[i], i); }
             w = warp_total(w);
             if (lane == 0) { put64(&sh.seg_w[rank * NW + warp], 0, w); put32(&sh.seg_t[rank * NW + warp], 0, 0); }
             const uint32_t n = send_lists();
