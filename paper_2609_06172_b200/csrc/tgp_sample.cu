@@ -12,9 +12,10 @@
 //   else top-p: a histogram of the weights over 2047 bins of 1 / 64 in (max - logit) / temperature tells the bin in which t lies; its tokens are such a list;
 //   where a list would be too long (equal logits, a large top-k): further histograms, each 2048 times finer in the logits' bits, down to one value;
 //   the draw: sums of the kept weights by warp, in the order of the tokens, and the one segment that the random number falls into once more.
-// Bound by instructions, not by the 4 B V bytes (5.1 us at 64 x 128256): us at 1 x 32000 and 64 x 128256: no filter 9.0 and 29 (the maximum and one sum of weights), top-k of 50 12.4 and 24 (two
-// passes that compute no weights), top-p of 0.9 24 and 71 (in the latter, per CTA and thousand cycles: maximum 12, histogram 37 - a weight in fp64 and two atomics per token -, its sums and bin 17,
-// list and segment sums about 23, sorting and drawing 14); a top-k of 900 sorts its list, 35 and 64.  Eight CTAs per row where that fits two to an SM (four at 64 rows; eight there are slower).
+// Bound by instructions, not by the 4 B V bytes (5.1 us at 64 x 128256): us at 1 x 32000 and 64 x 128256: the maximum alone 2.9 and 6.0 (5.5 TB/s), no filter 7.8 and 26 (one sum of weights
+// more: nine operations in fp64 and a conversion for each token that can be drawn), top-k of 50 11.1 and 19 (two passes that compute no weights), top-p of 0.9 21 and 61 (a weight and two atomics per
+// token, then the weights of those above the bin once more); a top-k of 900 sorts its list, 34 and 60.  Eight CTAs per row where that fits two to an SM (four at 64 rows; eight there are
+// slower).  A weight with a table of 32 entries, without bank conflicts, and two more terms: 28 instead of 26.
 #include <cuda_runtime.h>
 #include <algorithm>
 #include <cstdint>
@@ -177,18 +178,45 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     if (tid == 0) sh.listed = 0;
     for (uint32_t i = tid; i < BINS; i += THREADS) sh.cnt[i] = 0;
 
-    // every logit of this CTA's part once, each thread every THREADS-th, eight loads under way
-    auto each = [&](auto &&f) {
-        uint32_t i = first + tid;
-        for (; i < end && end - i > 7 * THREADS; i += 8 * THREADS) {
+    // every logit of this CTA's part once, each thread every THREADS-th, eight loads under way; -inf behind the end; f has a thread's eight and the first one's index.
+    // (Only the last eight are loaded with a look at the end, and they together: one by one behind the full ones, or all with a look, 1 x 32000 with no filter takes 9.1 instead of 7.8 us,
+    // 64 x 128256 with top-p 71 instead of 61.)
+    auto each_eight = [&](auto &&f) {
+        for (uint32_t i = first; i < end; i += 8 * THREADS) {
             float x[8];
+            const float *from = row + i + tid;
+            if (end - i >= 8 * THREADS) {
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * THREADS];
+                for (uint32_t j = 0; j < 8; ++j) x[j] = from[j * THREADS];
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) x[j] = end - i > j * THREADS + tid ? from[j * THREADS] : -INFINITY;
+            }
+            f(x, i + tid);
+        }
+    };
+    auto each = [&](auto &&f) {
+        each_eight([&](const float (&x)[8], uint32_t i) {
 #pragma unroll
             for (uint32_t j = 0; j < 8; ++j) f(x[j], i + j * THREADS);
-        }
-        for (; i < end; i += THREADS) f(row[i], i);
+        });
     };
+    // a warp's logits of [lo, hi), 256 at a time, -inf behind the end: f has a lane's eight, every 32nd, and the first one's index
+    auto by_eight = [&](uint32_t lo, uint32_t hi, auto &&f) {
+        for (uint32_t i = lo; i < hi; i += 8 * 32) {
+            float x[8];
+            const float *from = row + i + lane;
+            if (hi - i >= 8 * 32) {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) x[j] = from[j * 32];
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 8; ++j) x[j] = hi - i > j * 32 + lane ? from[j * 32] : -INFINITY;
+            }
+            f(x, i + lane);
+        }
+    };
+    auto top_of = [](const float (&x)[8]) { return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))); };
 
     // ---- the maximum ----
     Row r;
@@ -267,10 +295,14 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     // ---- tokens whose key is in [key_lo, key_hi], which are those of numbers, as a list in the first CTA ----
     auto gather = [&](uint32_t key_lo, uint32_t key_hi) {
         const float x_lo = of_key(key_lo), x_hi = of_key(key_hi);
-        each([&](float x, uint32_t i) {
-            if (!(x >= x_lo && x <= x_hi)) return;
-            const uint32_t at = atomicAdd(&sh.listed, 1u);
-            if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i;
+        each_eight([&](const float (&x)[8], uint32_t i) {
+            if (!(top_of(x) >= x_lo)) return;
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j)
+                if (x[j] >= x_lo && x[j] <= x_hi) {
+                    const uint32_t at = atomicAdd(&sh.listed, 1u);
+                    if (at < LIST) sh.list[at] = (u64)key_of(x[j]) << 32 | (uint32_t)~(i + j * THREADS);
+                }
         });
         return send_lists();
     };
@@ -400,18 +432,10 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
 #pragma unroll
                 for (int j = 0; j < 4; ++j) red_if_nonzero(hi_at + z[j] * 4, z[j] <= last ? (uint32_t)(w[j] >> 32) + (old[j] + (uint32_t)w[j] < old[j]) : 0);
             };
-            uint32_t i = first + tid;
-            float next[4];
-            auto fetch = [&]() {
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) next[j] = i < end && end - i > j * THREADS ? row[i + j * THREADS] : -INFINITY;
-            };
-            for (fetch(); i < end;) {
-                const float x[4] = {next[0], next[1], next[2], next[3]};
-                i = end - i > 4 * THREADS ? i + 4 * THREADS : end;
-                fetch();
-                four(x);
-            }
+            each_eight([&](const float (&x)[8], uint32_t) {
+                four({x[0], x[1], x[2], x[3]});
+                four({x[4], x[5], x[6], x[7]});
+            });
             all = cta_total(all);
             if (tid == 0) put64(&sh.seg_w[rank], 0, all);
         } else {
@@ -496,19 +520,13 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             auto list = [&](float x, uint32_t i) {
                 if (x >= x_lo && x <= x_hi) { const uint32_t at = atomicAdd(&sh.listed, 1u); if (at < LIST) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)~i; }
             };
-            uint32_t i = lo + lane;
-            for (; i < hi && hi - i > 7 * 32; i += 8 * 32) {
-                float x[8];
+            by_eight(lo, hi, [&](const float (&x)[8], uint32_t i) {
+                if (!__any_sync(0xffffffffu, top_of(x) >= x_lo)) return;
 #pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * 32];
-                if (fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) >= x_lo) {
+                for (uint32_t j = 0; j < 8; ++j) weigh(x[j]);
 #pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) weigh(x[j]);
-#pragma unroll
-                    for (uint32_t j = 0; j < 8; ++j) list(x[j], i + j * 32);
-                }
-            }
-            for (; i < hi; i += 32) { weigh(row[i]); list(row[i], i); }
+                for (uint32_t j = 0; j < 8; ++j) list(x[j], i + j * 32);
+            });
             w = warp_total(w);
             if (lane == 0) { put64(&sh.seg_w[rank * NW + warp], 0, w); put32(&sh.seg_t[rank * NW + warp], 0, 0); }
             const uint32_t n = send_lists();
@@ -584,17 +602,12 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     };
     auto segment = [&](uint32_t lo, uint32_t hi, u64 &w, uint32_t &t) {
         w = 0; t = 0;
-        uint32_t i = lo + lane;
-        for (; i < hi && hi - i > 7 * 32; i += 8 * 32) {
-            float x[8];
+        by_eight(lo, hi, [&](const float (&x)[8], uint32_t) {
+            // (few tokens are kept as a rule: none of 256 saves their weights, one of them costs eight a lane that do not wait for one another)
+            if (!__any_sync(0xffffffffu, top_of(x) >= lowest)) return;
 #pragma unroll
-            for (uint32_t j = 0; j < 8; ++j) x[j] = row[i + j * 32];
-            // (few tokens are kept as a rule: none of eight saves their weights, one of them costs eight that do not wait for one another)
-            if (fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7]))) >= lowest)
-#pragma unroll
-                for (uint32_t j = 0; j < 8; ++j) counts(x[j], w, t);
-        }
-        for (; i < hi; i += 32) counts(row[i], w, t);
+            for (uint32_t j = 0; j < 8; ++j) counts(x[j], w, t);
+        });
         w = warp_total(w); t = warp_total(t);
     };
     if (!summed || rank == 0) bounds();
