@@ -728,7 +728,7 @@ __global__ void __launch_bounds__(128) tgp_attn_q4_merge_kernel(const AttnQ4Args
 
 // ---- host side ---------------------------------------------------------------------------------------------------------------------
 
-constexpr uint32_t UNPACK_FROM = 128;                            // queries from which on the cache may be unpacked and the tcgen05 kernel run on it
+constexpr uint32_t UNPACK_FROM = 32;                             // queries from which on the cache may be unpacked and the tcgen05 kernel run on it
 
 bool q4_geometry(const tgp_model_cfg *c) {
     return c && (c->Dh == 64 || c->Dh == 128) && c->Hkv && c->Hq && c->Hq % c->Hkv == 0 && c->TK && c->TK % KEYS == 0 && c->TK <= (1u << 20);
@@ -799,13 +799,18 @@ int launch_attn(const AttnQ4Args &a, cudaStream_t st) {
 
 uint32_t rows_of_block(const tgp_model_cfg *c, uint32_t q_len) { return (uint64_t)q_len * (c->Hq / c->Hkv) <= 8 ? 8 : 16; }
 
-// Does a call read the codes itself?  Below 128 queries always: unpacked, the cache would be the mma.sync kernel's, or the CUDA-core one's (us, codes / unpacked: 3 sequences of 2000 keys, 32 heads
-// over 8 x 128, 8 queries 12.6 / 1236, 32 24.5 / 92, 127 75 / 98; 64 heads, 127 queries 144 / 159).  Above, each block of 16 rows converts the cache again, while the tcgen05 kernel's time is the
-// chain of its key blocks: where the blocks fill little of the GPU (us, 200 queries of one sequence: 8 heads x 128, 8200 keys 42.7 / 61.6, 700 keys 11.8 / 13.3; 32 heads over 8, 8200 keys 131 / 63).
+// Does a call read the codes itself?  Below 32 queries always.  From there on each block of 16 rows converts the cache again, while the tcgen05 kernel's time, on the unpacked cache, is a chain of its
+// blocks of 64 keys, or the GPU's rate where its CTAs of 128 queries are many.  Both times (us) as straight lines through 300 measured shapes (8 - 256 queries of 1 - 24 sequences, 100 - 8000 keys, 8 heads over
+// 1 to 64 over 8), off by an eighth as a rule; the choice costs 0.4 % on average over the better of the two, where reading the codes up to 127 queries cost 10 (us, codes / unpacked: 3 sequences of
+// 2000 keys, 32 heads over 8 x 128, 32 queries 24.5 / 30.9, 64 39.5 / 31.7, 127 74.9 / 33.7; 64 heads, 8 sequences, 127 366 / 99; 24 of 500 365 / 104; one of 8000, 8 heads x 128, 127 30.9 / 60.4).
+// The codes' weights keep fp16's eleven bits, the others' bf16's eight: unpacking has to gain a tenth.
 bool reads_codes(const tgp_model_cfg *c, uint32_t B, uint32_t q_len, uint32_t kvlen) {
     if (q_len < UNPACK_FROM) return true;
-    const float units = (float)B * (float)c->Hkv * (float)(((uint64_t)q_len * (c->Hq / c->Hkv) + 15) / 16), n = (float)kvlen / 32.f;
-    return 0.6f * units * (n + 12.f) <= (2.f + 0.225f * n) * 444.f;
+    const float wide = c->Dh == 128 ? 1.f : 0.f, chunks = (float)kvlen / 32.f, blocks = (float)kvlen / 64.f, pages = (float)B * (float)c->Hkv;
+    const float units = pages * (float)(((uint64_t)q_len * (c->Hq / c->Hkv) + 15) / 16), ctas = (float)B * (float)c->Hq * (float)((q_len + 127) / 128);
+    const float codes = 4.6f + 0.035f * chunks + 1.02e-3f * units * (chunks + 12.f) * (0.65f + 0.35f * wide);
+    const float unpacked = 7.5f + 0.26f * blocks + 3.6e-3f * ctas * blocks * (0.7f + 0.3f * wide) + 6.2e-5f * pages * (float)kvlen * (1.f + wide);
+    return codes * 0.9f <= unpacked;
 }
 
 uint64_t unpacked_rows(uint32_t kvlen) { return ((uint64_t)kvlen + 63) / 64 * 64; }
@@ -888,7 +893,8 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
     one.TK = (uint32_t)ld;
     TgpTilePtrs whole{};
     whole.k[0] = kb; whole.v[0] = vb;
-    if (int rc = tgpk_attn(qb, whole, 1, ob, &one, B, q_len, pos0, nullptr, st)) return rc;
+    // (tgpk_attn() would take the mma.sync kernel below 128 queries: 92 us for 32 of the three sequences above)
+    if (int rc = q_len < 128 ? tgpk_attn_prefill_tc5(qb, whole, ob, &one, B, q_len, pos0, st) : tgpk_attn(qb, whole, 1, ob, &one, B, q_len, pos0, nullptr, st)) return rc;
     const dim3 grid(B * cfg->Hkv, (q_len + 255) / 256);
     const NanArgs n{(bf16 *)ob, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, tiles};
     return cfg->Dh == 64 ? launch(tgp_attn_q4_nan_kernel<64>, grid, dim3(256), 0, st, 1, n) : launch(tgp_attn_q4_nan_kernel<128>, grid, dim3(256), 0, st, 1, n);

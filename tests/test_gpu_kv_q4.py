@@ -202,6 +202,48 @@ def test_prompts(Dh, G, Hkv, B, S, pos0, TK):
     check_attn(config(G * Hkv, Hkv, Dh, B, pos0 + S, TK), B, S, pos0, seed=S, p_half=HALF_FP16 if S < 128 else HALF_BF16)
 
 
+UNPACKED = [(64, 8, 4, 3, 127, 700, 64), (128, 4, 8, 6, 64, 601, 48), (128, 8, 8, 8, 33, 500, 128), (64, 1, 16, 8, 100, 200, 16), (64, 8, 8, 1, 200, 300, 32)]
+
+
+@pytest.mark.parametrize("Dh,G,Hkv,B,S,pos0,TK", UNPACKED)
+def test_queries_enough_to_unpack_the_cache_for(Dh, G, Hkv, B, S, pos0, TK):
+    """From 32 queries on, where that is expected to be faster: the scratch array then holds the keys as bf16 (weights are bf16 numbers, too)."""
+    c = config(G * Hkv, Hkv, Dh, B, pos0 + S, TK)
+    rng = np.random.default_rng(S)
+    n_tiles = (pos0 + S + TK - 1) // TK
+    (kh, kt), (vh, vt) = random_tiles(rng, c, n_tiles, 1), random_tiles(rng, c, n_tiles, -1)
+    q = bf16_round((rng.standard_normal((B, S, c.Hq, Dh)) / 2).astype(np.float32))
+    qb, ob = bf16(q.reshape(B * S, -1)), torch.full((B * S + 1, c.Hq * Dh), 7.0, dtype=torch.bfloat16, device=DEV)
+    s, n = scratch_for(c, S)
+    tb.k_attn_q4(qb, kt, vt, ob, c, B, S, pos0, 1, -1, None, s)
+    torch.cuda.synchronize()
+    assert (s[n:] == 77).all() and (ob[B * S] == 7).all()
+    K, V = decoded(kh, c, 1), decoded(vh, c, -1)
+    assert np.array_equal(f32(s[:2 * Dh * pos0].view(torch.bfloat16)).reshape(pos0, Dh), K[0, 0, :pos0])
+    got = f32(ob)[:B * S].reshape(B, S, c.Hq, Dh)
+    for b in range(B):
+        within(got[b], *kv_q4.attention(q[b].astype(np.float64), K[b], V[b], pos0), HALF_BF16)
+
+
+@pytest.mark.parametrize("Dh,G,Hkv,B,S,pos0,TK", UNPACKED)
+@pytest.mark.parametrize("side", ["k", "v"])
+def test_a_nan_in_a_cache_that_is_unpacked(Dh, G, Hkv, B, S, pos0, TK, side):
+    """A group of the last sequence stands for NaN at one of the call's own positions: of its head's outputs those that see it, and no other."""
+    c = config(G * Hkv, Hkv, Dh, B, pos0 + S, TK)
+    at, group, head = pos0 + S // 2, 2, 1
+    rng = np.random.default_rng(S + 1)
+    n_tiles = (pos0 + S + TK - 1) // TK
+    (kh, _), (vh, _) = random_tiles(rng, c, n_tiles, 0), random_tiles(rng, c, n_tiles, 0)
+    t = kh if side == "k" else vh
+    t[at // TK, B - 1, head, TK * Dh // 2 + (at % TK) * Dh // 16 + group] = 0x7f
+    got = run_attn(c, B, S, pos0, bf16_round(rng.standard_normal((B, S, c.Hq, Dh)).astype(np.float32)), *([torch.from_numpy(x).to(DEV) for x in y] for y in (kh, vh)))
+    nan = np.zeros(got.shape, bool)
+    nan[B - 1, S // 2:, head * G:(head + 1) * G] = True
+    if side == "v":
+        nan[..., :16 * group] = nan[..., 16 * (group + 1):] = False
+    assert np.array_equal(np.isnan(got), nan)
+
+
 @pytest.mark.parametrize("B,pos0,Hq,Hkv,Dh,TK", [(1, 4000, 8, 2, 128, 128), (1, 16383, 4, 1, 64, 256), (2, 1023, 8, 8, 64, 16), (40, 130, 16, 4, 128, 16), (300, 33, 8, 8, 64, 48)])
 def test_contexts_in_parts_and_in_one(B, pos0, Hq, Hkv, Dh, TK):
     """One sequence of a long context is split over the GPU; many sequences of a short one are not."""

@@ -89,10 +89,10 @@ def test_bytes_of_tiles_and_scratch():
     for B in (1, 3, 64, 1000):
         sizes = [tb.k_attn_q4_scratch_bytes(cfg(B=b, max_len=16384, TK=256), 1) for b in range(1, B + 1)]
         assert sizes == sorted(sizes)
-    # from 128 queries on the keys and values fit as bf16, a whole number of 64 positions of them
+    # from 32 queries on the keys and values fit as bf16, a whole number of 64 positions of them
     for max_len in (65536, 65500):
-        assert tb.k_attn_q4_scratch_bytes(cfg(max_len=max_len, TK=1024), 128) == 2 * 4 * 2 * 65536 * 64 * 2
-    assert tb.k_attn_q4_scratch_bytes(cfg(max_len=65536, TK=1024), 127) < 1 << 24
+        assert tb.k_attn_q4_scratch_bytes(cfg(max_len=max_len, TK=1024), 32) == 2 * 4 * 2 * 65536 * 64 * 2
+    assert tb.k_attn_q4_scratch_bytes(cfg(max_len=65536, TK=1024), 31) < 1 << 24
 
 
 def move(src, dst, c=None, form=tb.KV_Q4, B=4, length=40, tiles=2, kt=None):
