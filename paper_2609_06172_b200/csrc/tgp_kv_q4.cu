@@ -805,7 +805,7 @@ uint32_t rows_of_block(const tgp_model_cfg *c, uint32_t q_len) { return (uint64_
 // 2000 keys, 32 heads over 8 x 128, 32 queries 24.5 / 30.9, 64 39.5 / 31.7, 127 74.9 / 33.7; 64 heads, 8 sequences, 127 366 / 99; 24 of 500 365 / 104; one of 8000, 8 heads x 128, 127 30.9 / 60.4).
 // The codes' weights keep fp16's eleven bits, the others' bf16's eight: unpacking has to gain a tenth.
 bool reads_codes(const tgp_model_cfg *c, uint32_t B, uint32_t q_len, uint32_t kvlen) {
-    if (q_len < UNPACK_FROM) return true;
+    if (q_len < UNPACK_FROM || (uint64_t)B * c->Hkv > 65535u) return true;             // (the unpacking's grid)
     const float wide = c->Dh == 128 ? 1.f : 0.f, chunks = (float)kvlen / 32.f, blocks = (float)kvlen / 64.f, pages = (float)B * (float)c->Hkv;
     const float units = pages * (float)(((uint64_t)q_len * (c->Hq / c->Hkv) + 15) / 16), ctas = (float)B * (float)c->Hq * (float)((q_len + 127) / 128);
     const float codes = 4.6f + 0.035f * chunks + 1.02e-3f * units * (chunks + 12.f) * (0.65f + 0.35f * wide);
