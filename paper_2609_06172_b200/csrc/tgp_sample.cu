@@ -323,8 +323,8 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             __syncthreads();
         }
     };
-    const double u = (double)a.u[b];
-    auto draw = [&](u64 sum) { return min(u > 0.0 ? (u64)fmin(u * (double)sum, 9.0e18) : 0ull, sum - 1); };
+    const double u = fmin(fmax((double)a.u[b], 0.0), 1.0);          // (a NaN is 0); of a row's 2^19 weights of 2^44 at most it is 2^63 at most
+    auto draw = [&](u64 sum) { return min((u64)(u * (double)sum), sum - 1); };
     auto share = [&](u64 sum) { return max(1ull, min(sum, (u64)ceil((double)top_p * (double)sum))); };            // top_p of it
 
     // ---- top-k by the list of what is not below the k-th largest of the threads' maxima ----

@@ -157,3 +157,24 @@ def test_rows_that_do_not_begin_on_16_bytes():
 def test_largest_vocabulary():
     rng = np.random.default_rng(12)
     check(rng.standard_normal((2, tb.SAMPLE_MAX_V)) * 2, rng.random(2), top_p=[0.9, 1.0])
+
+
+@pytest.mark.parametrize("V", [tb.SAMPLE_MAX_V, 511591, 511590])
+@pytest.mark.parametrize("settings", [dict(), dict(top_p=0.99), dict(min_p=0.5), dict(top_k=520000), dict(top_k=2147483647, top_p=0.9999999)], ids=str)
+def test_flat_rows_of_the_largest_vocabulary(V, settings):
+    """Sums of weights beyond 2^62, up to 2^63: equal logits and infinite temperatures, random numbers up to 1 and above."""
+    rng = np.random.default_rng(13)
+    u = np.float32([0.0, 0.5, 0.9758, 0.98, 0.99, 0.9999, 0.99999994])
+    equal = np.full((len(u), V), 1.25, np.float32)
+    check(equal, u, **settings)
+    x = rng.standard_normal((3, V)).astype(np.float32)
+    check(x, [0.98, 0.99, 0.99999994], temperature=float("inf"), **settings)
+    assert list(run(equal[:4], [1.0, 2.0, np.inf, np.nan], **settings)) == [sample.sample(equal[0], 1.0, **{n: float(np.float32(s)) if n != "top_k" else s for n, s in settings.items()})] * 3 + [0]
+
+
+def test_a_flat_row_of_a_large_vocabulary_is_drawn_evenly():
+    """Of the largest vocabulary at a high temperature, by evenly spaced random numbers."""
+    rng = np.random.default_rng(14)
+    x = rng.standard_normal(tb.SAMPLE_MAX_V).astype(np.float32)
+    u = np.float32((np.arange(8) + 0.5) / 8)
+    check(np.tile(x, (8, 1)), u, temperature=1e3)
