@@ -1299,6 +1299,7 @@ __global__ void __launch_bounds__(256) tgp_argmax_kernel(const float *logits, in
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
     // (the wait stands before the first access to the first CTA's memory: only then is that CTA known to run, however short this part is)
+    __syncwarp();
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const float *row = logits + (size_t)(blockIdx.x / parts) * V;
@@ -1337,6 +1338,7 @@ __global__ void __launch_bounds__(256) tgp_argmax_kernel(const float *logits, in
         if (threadIdx.x == 0) { out[blockIdx.x] = (int32_t)idx; if (out2) out2[blockIdx.x] = (int32_t)idx; }
         return;
     }
+    __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (threadIdx.x == 0) {                                    // to slot `rank` of the cluster's first CTA
         uint32_t rv, ri;
@@ -1425,6 +1427,7 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) tgp_route_small_kernel(const
     uint32_t rank, parts;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+    __syncwarp();
     if (parts > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     const uint32_t per = (M + parts - 1) / parts, m0 = rank * per, mine = m0 < M ? min(per, M - m0) : 0u;       // this CTA's tokens
     uint4 w[U];

@@ -22,10 +22,12 @@
 #include "tgp.h"
 #include "tgp_kernels.h"
 #include "tgp_launch.cuh"
+#include "tgp_sm100.cuh"
 
 namespace {
 
 using namespace tgp_launch;
+using tgp_sm100::cluster_arrive; using tgp_sm100::cluster_sync_all; using tgp_sm100::cluster_wait;
 
 constexpr int THREADS = 512, NW = THREADS / 32;
 constexpr uint32_t BINS = 2048, CLUSTER_MAX = 8, LIST = 2048, OCTAVE = 512;
@@ -54,13 +56,6 @@ struct Shared {
     uint32_t key_lo, key_hi;
 };
 
-__device__ __forceinline__ void cluster_sync() {
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_arrive() { __syncwarp(); asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t in_cta(const void *p, uint32_t rank) {
     uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
@@ -239,7 +234,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             for (int o = NW / 2; o; o >>= 1) { const float om = __shfl_xor_sync(0xffffffffu, m, o); const uint32_t oi = __shfl_xor_sync(0xffffffffu, at, o); merge(om, oi); }
             if (lane < parts) { put32(reinterpret_cast<uint32_t *>(&sh.top[rank]), lane, __float_as_uint(m)); put32(&sh.top_i[rank], lane, at); }          // to every CTA
         }
-        cluster_sync();
+        cluster_sync_all();
         m = -INFINITY; at = 0;
         for (uint32_t p = 0; p < parts; ++p) merge(sh.top[p], sh.top_i[p]);
         r.top = m; best = at;
@@ -284,12 +279,12 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         __syncthreads();
         const uint32_t n = sh.listed;
         if (tid < parts) put32(&sh.counts[rank], tid, n);
-        cluster_sync();
+        cluster_sync_all();
         uint32_t before = 0, all = 0;
         for (uint32_t p = 0; p < parts; ++p) { if (p < rank) before += sh.counts[p]; all += sh.counts[p]; }
         if (rank && all <= LIST) for (uint32_t i = tid; i < n; i += THREADS) put64(&sh.list[before + i], 0, sh.list[i]);
         if (tid == 0) sh.listed = 0;
-        cluster_sync();
+        cluster_sync_all();
         return all;
     };
     // ---- tokens whose key is in [key_lo, key_hi], which are those of numbers, as a list in the first CTA ----
@@ -332,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         // (bins of eight: a histogram of 256, which every CTA adds up for itself)
         constexpr uint32_t EIGHT = BINS / 8;
         if (mine >= r.low) atomicAdd(&sh.cnt[r.bin(mine) / 8], 1u);
-        cluster_sync();
+        cluster_sync_all();
         uint32_t n = 0, c[CLUSTER_MAX];
         if (tid < EIGHT) {
 #pragma unroll
@@ -452,7 +447,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             add(bin, r.weight(x));
         });
         }
-        cluster_sync();
+        cluster_sync_all();
         for (uint32_t i = rank * THREADS + tid; i < BINS; i += parts * THREADS) {
             uint32_t n = 0;
             u64 w = 0;
@@ -464,7 +459,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             put32(&sh.all_cnt[i], 0, n);
             put64(&sh.all_w[i], 0, w);
         }
-        cluster_sync();
+        cluster_sync_all();
         if (rank == 0) {                                         // four bins a thread: sums of the threads before, then the bin where the need is met
             constexpr uint32_t PER = BINS / THREADS;
             uint32_t n = 0;
@@ -498,7 +493,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
                 }
             }
         }
-        cluster_sync();
+        cluster_sync_all();
     };
 
     auto narrow = [&](bool by_weight, u64 need) {
@@ -615,7 +610,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
         u64 w; uint32_t t;
         segment(lo, hi, w, t);
         if (lane == 0) { put64(&sh.seg_w[rank * NW + warp], 0, w); put32(&sh.seg_t[rank * NW + warp], 0, t); }
-        cluster_sync();
+        cluster_sync_all();
     }
     if (rank == 0 && warp == 0) {                                // four segments a lane: ties before them, then weight before them
         constexpr uint32_t PER = CLUSTER_MAX * NW / 32;
@@ -642,7 +637,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
             seen += t[i];
         }
     }
-    cluster_sync();
+    cluster_sync_all();
     if (summed && rank) bounds();
     // ---- the CTA of the segment: its warps take a sixteenth of it each, then the one into which the rest of the target falls goes through its part ----
     if (sh.seg / NW != rank) return;

@@ -97,3 +97,19 @@ def test_tiles_of_the_paired_products_are_the_fastest_measured(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-o", str(tmp_path / "rows"), str(src)], check=True)
     rows = [int(r) for r in subprocess.run([str(tmp_path / "rows")], capture_output=True, text=True, check=True).stdout.split()]
     assert len(rows) == len(FASTEST) and all(r in best for r, best in zip(rows, FASTEST.values())), dict(zip(FASTEST, rows))
+
+
+def test_a_warp_is_together_where_it_reaches_a_cluster_barrier():
+    """The .aligned forms are undefined for a warp whose lanes are on different paths, and what brings them together behind a branch or a loop is __syncwarp(), not
+    the order in which a compiler happens to lay out the code."""
+    seen = 0
+    for f in sorted(os.listdir(CSRC)):
+        if not f.endswith((".cu", ".cuh")):
+            continue
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, f)).read())
+        for m in re.finditer(r'asm volatile\("barrier\.cluster\.(arrive|wait)[^;"]*;"', text):
+            before = re.sub(r"if \(parts > 1\)\s*$", "", text[:m.start()].rstrip()).rstrip()
+            together = before.endswith("__syncwarp();") or (m.group(1) == "wait" and re.search(r'asm volatile\("barrier\.cluster\.arrive[^;"]*;" ::: "memory"\);$', before))
+            assert together, (f, text[:m.start()].count("\n") + 1)
+            seen += 1
+    assert seen >= 10
