@@ -113,3 +113,53 @@ def test_a_warp_is_together_where_it_reaches_a_cluster_barrier():
             assert together, (f, text[:m.start()].count("\n") + 1)
             seen += 1
     assert seen >= 10
+
+
+def device_functions():
+    """{file: {name: body without comments}} of the __device__ functions that the kernels of a file can call: its own and the headers'."""
+    own = {}
+    for f in sorted(os.listdir(CSRC)):
+        if not f.endswith((".cu", ".cuh")):
+            continue
+        text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, f)).read())
+        for m in re.finditer(r"__device__\s+(?:__forceinline__\s+)?(?:static\s+)?[\w:&*]+[ *&]+(\w+)\s*\(([^(){};]|\([^()]*\))*\)\s*\{", text):
+            depth, at = 1, m.end()
+            while depth:
+                depth += {"{": 1, "}": -1}.get(text[at], 0)
+                at += 1
+            own.setdefault(f, {}).setdefault(m.group(1), text[m.end():at])
+    shared = {n: b for f, fs in own.items() if f.endswith(".cuh") for n, b in fs.items()}
+    return {f: {**shared, **fs} for f, fs in own.items()}
+
+
+def inlined(body, functions, depth=6):
+    """The body with the bodies of the functions that it calls behind their calls."""
+    if not depth:
+        return body
+    def call(m):
+        f = functions.get(m.group(1))
+        return m.group(0) if f is None else "{" + inlined(f, {n: b for n, b in functions.items() if n != m.group(1)}, depth - 1) + "}" + m.group(0)
+    return re.sub(r"\b(\w+)(?:<[^<>;(){}]*>)?\(", call, body)
+
+
+def touches_others_only_between_barriers(body):
+    waits = [m.start() for m in re.finditer(r"barrier\.cluster\.wait", body)]
+    uses = [m.start() for m in re.finditer(r"mapa\.shared::cluster", body)]
+    return bool(waits) and waits[0] < uses[0] and waits[-1] > uses[-1]
+
+
+FUNCTIONS = device_functions()
+INLINED = [(f, k, text) for f, k, text in ((f, k, inlined(b, FUNCTIONS.get(f, {}))) for f, k, b in KERNELS) if "mapa.shared::cluster" in text]
+
+
+def test_kernels_that_reach_other_ctas_through_functions_are_found():
+    assert {"tgp_sample_kernel", "tgp_attn_q4_kernel", "tgp_argmax_kernel", "tgp_wstream_tc_kernel"} <= {k for _, k, _ in INLINED}
+
+
+@pytest.mark.parametrize("f,name,body", INLINED, ids=lambda v: v if isinstance(v, str) and len(v) < 60 else "")
+def test_functions_of_a_kernel_touch_other_ctas_only_between_cluster_barriers(f, name, body):
+    """The same order where a kernel's functions hold the accesses and the barriers; a barrier fewer at either end would be noticed."""
+    assert touches_others_only_between_barriers(body), (f, name)
+    uses, wait = [m.start() for m in re.finditer(r"mapa\.shared::cluster", body)], "barrier.cluster.wait"
+    assert not touches_others_only_between_barriers(body[:uses[0]].replace(wait, "") + body[uses[0]:]), (f, name)
+    assert not touches_others_only_between_barriers(body[:uses[-1]] + body[uses[-1]:].replace(wait, "")), (f, name)
