@@ -814,6 +814,16 @@ bool reads_codes(const tgp_model_cfg *c, uint32_t B, uint32_t q_len, uint32_t kv
 }
 
 uint64_t unpacked_rows(uint32_t kvlen) { return ((uint64_t)kvlen + 63) / 64 * 64; }
+uint64_t unpacked_bytes(const tgp_model_cfg *c, uint32_t kvlen) { return 2 * (uint64_t)c->Hkv * unpacked_rows(kvlen) * c->Dh * sizeof(bf16); }     // of a sequence
+
+// The part of the scratch array that holds an unpacked cache: of all sequences if that is no more than UNPACK_MOST, else of as many as fit (one at least), and a call takes
+// them group by group.  Bytes in bf16 are 3.6 times those of the tiles, which are small because memory is short; a group of 4 GB fills the GPU (64 heads over 8 x 128, 131072 keys: eight
+// sequences, at 32 queries 512 CTAs).
+constexpr uint64_t UNPACK_MOST = 4ull << 30;
+uint64_t unpacked_capacity(const tgp_model_cfg *c) {
+    const uint64_t one = unpacked_bytes(c, c->max_len);
+    return one * std::max<uint64_t>(1, std::min<uint64_t>(c->B, UNPACK_MOST / one));
+}
 
 int launch_unpack(const UnpackArgs &a, const tgp_model_cfg *c, uint32_t B, cudaStream_t st) {
     const dim3 grid(std::min<uint64_t>(((uint64_t)a.count * (c->Dh / 16) + 255) / 256, 1u << 20), B * c->Hkv, 2);
@@ -860,7 +870,7 @@ int tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64
     if (!bytes || !q4_geometry(cfg) || !cfg->B || !q_len || q_len > cfg->max_len) return TGP_E_INVAL;
     const uint64_t rb = rows_of_block(cfg, q_len);                // two partial results for each CTA of a wave; keys and values as bf16
     *bytes = stretch_bytes(cfg->B) + 2ull * wave((uint32_t)rb) * rb * (cfg->Dh + 4) * sizeof(float);
-    if (q_len >= UNPACK_FROM) *bytes = std::max(*bytes, 2 * (uint64_t)cfg->B * cfg->Hkv * unpacked_rows(cfg->max_len) * cfg->Dh * sizeof(bf16));
+    if (q_len >= UNPACK_FROM) *bytes = std::max(*bytes, unpacked_capacity(cfg));
     return TGP_OK;
 }
 
@@ -886,18 +896,29 @@ int tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, ui
     // more rows: keys and values once as bf16, exactly what the cache stands for, and the attention over a bf16 cache of one tile
     if ((uint64_t)B * cfg->Hkv > 65535u || q_len > 65535u * 256 || (uint64_t)q_len * G > (1u << 27)) return TGP_E_TOO_LARGE;
     const uint64_t ld = unpacked_rows(kvlen);
-    bf16 *kb = (bf16 *)scratch_dev, *vb = kb + (uint64_t)B * cfg->Hkv * ld * cfg->Dh;
-    UnpackArgs u{kb, vb, nullptr, cfg->Hkv, cfg->TK, kvlen, 0, (uint32_t)ld, pos0, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), tiles};
-    if (int rc = launch_unpack(u, cfg, B, st)) return rc;
-    tgp_model_cfg one = *cfg;
-    one.TK = (uint32_t)ld;
-    TgpTilePtrs whole{};
-    whole.k[0] = kb; whole.v[0] = vb;
-    // (tgpk_attn() would take the mma.sync kernel below 128 queries: 92 us for 32 of the three sequences above)
-    if (int rc = q_len < 128 ? tgpk_attn_prefill_tc5(qb, whole, ob, &one, B, q_len, pos0, st) : tgpk_attn(qb, whole, 1, ob, &one, B, q_len, pos0, nullptr, st)) return rc;
-    const dim3 grid(B * cfg->Hkv, (q_len + 255) / 256);
-    const NanArgs n{(bf16 *)ob, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, tiles};
-    return cfg->Dh == 64 ? launch(tgp_attn_q4_nan_kernel<64>, grid, dim3(256), 0, st, 1, n) : launch(tgp_attn_q4_nan_kernel<128>, grid, dim3(256), 0, st, 1, n);
+    const uint32_t fit = (uint32_t)std::min<uint64_t>(B, unpacked_capacity(cfg) / unpacked_bytes(cfg, kvlen)), groups = (B + fit - 1) / fit, most = (B + groups - 1) / groups;
+    for (uint32_t b0 = 0; b0 < B; b0 += most) {
+        const uint32_t n = std::min(most, B - b0);
+        TgpTilePtrs part{};                                       // the group's pages, queries and outputs
+        for (uint32_t t = 0; t <= (kvlen - 1) / cfg->TK; ++t) {
+            part.k[t] = (uint8_t *)tiles.k[t] + b0 * cfg->Hkv * page_bytes(cfg->Dh, cfg->TK);
+            part.v[t] = (uint8_t *)tiles.v[t] + b0 * cfg->Hkv * page_bytes(cfg->Dh, cfg->TK);
+        }
+        const bf16 *q = (const bf16 *)qb + (uint64_t)b0 * q_len * cfg->Hq * cfg->Dh;
+        bf16 *o = (bf16 *)ob + (uint64_t)b0 * q_len * cfg->Hq * cfg->Dh, *kb = (bf16 *)scratch_dev, *vb = kb + (uint64_t)n * cfg->Hkv * ld * cfg->Dh;
+        UnpackArgs u{kb, vb, nullptr, cfg->Hkv, cfg->TK, kvlen, 0, (uint32_t)ld, pos0, ldexpf(1.f, k_exp), ldexpf(1.f, v_exp), part};
+        if (int rc = launch_unpack(u, cfg, n, st)) return rc;
+        tgp_model_cfg one = *cfg;
+        one.TK = (uint32_t)ld;
+        TgpTilePtrs whole{};
+        whole.k[0] = kb; whole.v[0] = vb;
+        // (tgpk_attn() would take the mma.sync kernel below 128 queries: 92 us for 32 of the three sequences above)
+        if (int rc = q_len < 128 ? tgpk_attn_prefill_tc5(q, whole, o, &one, n, q_len, pos0, st) : tgpk_attn(q, whole, 1, o, &one, n, q_len, pos0, nullptr, st)) return rc;
+        const dim3 grid(n * cfg->Hkv, (q_len + 255) / 256);
+        const NanArgs nan{o, cfg->Hq, cfg->Hkv, G, cfg->TK, q_len, pos0, part};
+        if (int rc = cfg->Dh == 64 ? launch(tgp_attn_q4_nan_kernel<64>, grid, dim3(256), 0, st, 1, nan) : launch(tgp_attn_q4_nan_kernel<128>, grid, dim3(256), 0, st, 1, nan)) return rc;
+    }
+    return TGP_OK;
 }
 
 }  // extern "C"

@@ -389,6 +389,46 @@ def test_offsets_that_pass_32_bits():
     assert np.array_equal(f32(vb)[1898, :, 0], want)
 
 
+@pytest.mark.parametrize("B,S,Hq,Dh", [(9, 128, 16, 128), (11, 64, 64, 128), (17, 130, 16, 64)])
+def test_a_cache_that_is_unpacked_in_groups_of_sequences(B, S, Hq, Dh):
+    """Sequences of 131072 positions, more than the scratch array holds as bf16: each group's outputs are those of a call of its own, with a NaN in one of its values."""
+    n, Hkv, TK = 131072, 8, 2048
+    c, pos0 = config(Hq, Hkv, Dh, B, n, TK), n - S
+    g = torch.Generator(DEV).manual_seed(B)
+    tiles = []
+    for _ in range(2):
+        t = torch.randint(0, 256, (n // TK, B, Hkv, TK * Dh * 9 // 16), dtype=torch.uint8, device=DEV, generator=g)
+        t[..., TK * Dh // 2:] = torch.randint(0x28, 0x38, t[..., TK * Dh // 2:].shape, dtype=torch.uint8, device=DEV, generator=g)
+        tiles.append(t)
+    tiles[1][(n - S // 2) // TK, B - 1, 3, TK * Dh // 2 + (n - S // 2) % TK * Dh // 16 + 1] = 0x7f      # seen by the last sequence's later queries
+    qb = torch.randn(B * S, Hq * Dh, device=DEV, generator=g).bfloat16()
+    ob = torch.full((B * S + 1, Hq * Dh), 7.0, dtype=torch.bfloat16, device=DEV)
+    s, nbytes = scratch_for(c, S)
+    fit = nbytes // (2 * Hkv * n * Dh * 2)
+    pages = lambda b: [[t[b:].data_ptr() for t in side] for side in tiles]                             # noqa: E731
+    assert 1 < fit < B
+    tb.k_attn_q4(qb, list(tiles[0]), list(tiles[1]), ob, c, B, S, pos0, 0, 0, None, s)
+    groups = -(-B // fit)
+    most = -(-B // groups)
+    want = torch.empty_like(ob[:B * S])
+    for b in range(0, B, most):
+        m = min(most, B - b)
+        tb.k_attn_q4(qb[b * S:], *pages(b), want[b * S:], c, m, S, pos0, 0, 0, None, s)
+    torch.cuda.synchronize()
+    assert (s[nbytes:] == 77).all() and (ob[B * S] == 7).all()
+    nan = torch.zeros(B, S, Hq, Dh, dtype=torch.bool, device=DEV)
+    nan[B - 1, S - S // 2:, 3 * (Hq // Hkv):4 * (Hq // Hkv), 16:32] = True
+    assert torch.equal(torch.isnan(ob[:B * S]), nan.view(B * S, -1))
+    assert torch.equal(ob[:B * S].nan_to_num(), want.nan_to_num())
+    # and the last queries as single ones, which read the codes: |V| is below 3 on average, of which the weights' rounding to bf16 moves an output by half a step, as the
+    # outputs' own roundings do, of less than that
+    single = torch.empty(1, Hq * Dh, dtype=torch.bfloat16, device=DEV)
+    one, _ = scratch_for(c, 1)
+    for b in (0, most, B - 2):
+        tb.k_attn_q4(qb[(b + 1) * S - 1:], *pages(b), single, c, 1, 1, n - 1, 0, 0, None, one)
+        assert (single[0].float() - ob[(b + 1) * S - 1].float()).abs().max() <= 2 * HALF_BF16 * 3
+
+
 def test_two_calls_at_once_on_two_streams():
     c = config(32, 8, 128, 2, 4096, 128)
     rng = np.random.default_rng(7)

@@ -95,6 +95,16 @@ def test_bytes_of_tiles_and_scratch():
     assert tb.k_attn_q4_scratch_bytes(cfg(max_len=65536, TK=1024), 31) < 1 << 24
 
 
+def test_scratch_for_an_unpacked_cache_is_limited():
+    """4 GiB for as many sequences as fit, one sequence's where that is more; what fits entirely takes what it takes."""
+    long = dict(Hq=64, Hkv=8, Dh=128, max_len=131072, TK=2048)
+    one = 2 * 8 * 131072 * 128 * 2                         # 512 MiB
+    for B, sequences in ((1, 1), (7, 7), (8, 8), (9, 8), (64, 8), (1000, 8)):
+        assert tb.k_attn_q4_scratch_bytes(cfg(**long, B=B), 32) == tb.k_attn_q4_scratch_bytes(cfg(**long, B=B), 131072) == sequences * one
+    for B in (1, 5):
+        assert tb.k_attn_q4_scratch_bytes(cfg(Hq=64, Hkv=32, Dh=128, max_len=1 << 20, TK=1 << 14, B=B), 64) == 2 * 32 * (1 << 20) * 128 * 2
+
+
 def move(src, dst, c=None, form=tb.KV_Q4, B=4, length=40, tiles=2, kt=None):
     tb.k_kv_move([A] * tiles if kt is None else kt, [A] * tiles, src, dst, c or cfg(), form, B, length)
 
