@@ -445,8 +445,8 @@ int  tgp_k_attn_decode_static(const void *qb, void *const *k_tiles, void *const 
 #define TGP_Q4_EXP_MAX 32
 /* Bytes of one tile for cfg->B sequences: B * Hkv * TK * (Dh / 2 + Dh / 16). */
 int  tgp_k_kv_q4_tile_bytes(const tgp_model_cfg *cfg, uint64_t *bytes);
-/* tgp_k_rope_kv() for tiles in 4 bits.  The rotated values are rounded to bf16 from exact sums of the products (tgp_k_rope_kv() rounds between, so a value may
- * differ from its in the last bit).  Of 16 dimensions of a key or value, as bf16, the scale is the largest magnitude * 2^-exp / 6 and a code the value *
+/* tgp_k_rope_kv() for tiles in 4 bits.  The rotated values are the exact sums of the products, rounded to fp32 and then to bf16 (tgp_k_rope_kv() rounds in
+ * between, so a value may differ from its in the last bit).  Of 16 dimensions of a key or value, as bf16, the scale is the largest magnitude * 2^-exp / 6 and a code the value *
  * 2^-exp / scale, both rounded to the nearest (ties to even) and to the largest number where they are beyond it.  A group that
  * holds an infinity or a NaN gets a scale that is NaN. */
 int  tgp_k_rope_kv_q4(const float *q32, const float *k32, const float *v32, void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles,

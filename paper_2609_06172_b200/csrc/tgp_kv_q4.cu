@@ -69,8 +69,9 @@ __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32
 
 // ---- append ---------------------------------------------------------------------------------------------------------------------
 
-// x * c + y * s, rounded once: the products' own roundings are found by fused multiply-adds and the sum's by the difference of what it should be, and
-// added back.  The cache's values then do not depend on the order of a multiplication and an addition, at a border of two 4-bit codes least of all.
+// x * c + y * s, rounded to fp32 once (and to bf16 by the caller): the products' own roundings are found by fused multiply-adds and the sum's by the difference of what it
+// should be (Knuth's sum of two numbers), and added back.  The cache's values then do not depend on the order of a multiplication and an addition, at a border of two
+// 4-bit codes least of all.
 __device__ __forceinline__ float two_products(float x, float c, float y, float s) {
     const float p = __fmul_rn(x, c), q = __fmul_rn(y, s), sum = __fadd_rn(p, q);
     const float t = __fsub_rn(sum, p), lost = __fadd_rn(__fsub_rn(p, __fsub_rn(sum, t)), __fsub_rn(q, t));

@@ -149,6 +149,21 @@ def test_rotation_is_that_of_exact_sums():
     check_append(c, 1, 40, 0, 0, 0, q.reshape(40, -1).astype(np.float32), rng.standard_normal((40, 128)).astype(np.float32), rng.standard_normal((40, 128)).astype(np.float32))
 
 
+def test_rotation_rounds_to_fp32_and_then_to_bf16():
+    """Sums that fp32 rounds to the middle of two bf16 numbers go to the even one, whichever side they came from; those that it does not, to the nearer."""
+    c = config(Hq=2, Hkv=1, Dh=64, B=1, max_len=16, TK=16)
+    rest = np.array([2.0 ** -30, -2.0 ** -30, 2.0 ** -24, -2.0 ** -24, 2.0 ** -23, -2.0 ** -23, 0, 2.0 ** -60])
+    one = np.resize([1 + 2.0 ** -8, 1 + 3 * 2.0 ** -8], 32)              # the middles between 1, 1 + 2^-7 and 1 + 2^-6
+    row = np.concatenate((one, np.repeat(rest, 4))).astype(np.float32)
+    cos, sin = (torch.full((16, 32), x, device=DEV) for x in (1.0, -1.0))
+    x = torch.from_numpy(np.tile(row, 4)).to(DEV)
+    qb, tiles = torch.empty(1, 128, dtype=torch.bfloat16, device=DEV), [torch.zeros(tb.k_kv_q4_tile_bytes(c), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    tb.k_rope_kv_q4(x[:128], x[128:192], x[192:], qb, tiles[:1], tiles[1:], cos, sin, c, 1, 1, 0)
+    got = f32(qb).reshape(2, 64)
+    assert np.array_equal(got[0], got[1]) and np.array_equal(got[0], kv_q4.rotate(row, np.float32(1), np.float32(-1)))
+    assert list(got[0, :4]) == [1, 1 + 2.0 ** -6] * 2 and list(got[0, 16:24]) == [1 + 2.0 ** -7, 1 + 2.0 ** -6] * 2 + [1, 1 + 2.0 ** -7] * 2
+
+
 # ---- attention ----
 
 def run_attn(c, B, S, pos0, q, kt, vt, k_exp=0, v_exp=0, pos=None, stream=None):
