@@ -480,7 +480,8 @@ int  tgp_k_argmax(const float *logits, int32_t *out, uint32_t B, uint32_t V, voi
 /* out[b] = a token drawn from row b of logits [B, V] by the random number u_dev[b] in [0, 1).  Tokens are ordered by logit, the lower index
  * first of equals, and weigh w = exp((logit - max) / temperature).  Kept are the first top_k; of these the shortest beginning whose weight is at
  * least top_p of theirs (one token at least); of these the tokens with w >= min_p, the first token in any case.  The result is the lowest token, in the
- * order of the indices, at which the sum of the kept weights exceeds u times the whole.  Weights are rounded to 2^-44.
+ * order of the indices, at which the sum of the kept weights exceeds u times the whole.  Weights are rounded to 2^-44; a
+ * token whose weight rounds to 0 is never drawn.
  * The settings are device arrays [B], each may be NULL: temperature (NULL: 1; a row's 0, negative or NaN: the first token, as tgp_k_argmax(); below
  * 2^-120: that),
  * top_k (NULL, or 0 and less, or V and more: off), top_p (NULL, or 1 and more, or NaN: off; 0 and less: the first token), min_p (NULL, or

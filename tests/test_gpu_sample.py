@@ -1,7 +1,7 @@
 """Sampling on the GPU against plain 64-bit arithmetic, row by row: every filter, equal logits, settings and random numbers at their ends, rows of one CTA and of several.
 
-A weight is off by half a unit of 2^-44 at most (2^-45 of the largest) and by a few of the last bits of its exponential, so a sum over V tokens is off by V * 2^-45: below 1e-8
-at the sizes here, of a sum of 1 at least.  A token may differ from the oracle's only where a border of the cut or the draw lies so near, which for
+A weight is off by half a unit of 2^-44 at most (2^-45 of the largest) and by a few of the last bits of its exponential, so a sum over V tokens is off by V * 2^-45: 4e-9
+at 128256 tokens and 1.5e-8 at the largest vocabulary, of a sum of 1 at least.  A token may differ from the oracle's only where a border of the cut or the draw lies so near, which for
 the seeds here none does, or where numbers are equal by construction, which both sides hold exactly."""
 import numpy as np
 import pytest
@@ -178,3 +178,14 @@ def test_a_flat_row_of_a_large_vocabulary_is_drawn_evenly():
     x = rng.standard_normal(tb.SAMPLE_MAX_V).astype(np.float32)
     u = np.float32((np.arange(8) + 0.5) / 8)
     check(np.tile(x, (8, 1)), u, temperature=1e3)
+
+
+@pytest.mark.parametrize("V", [9000, 128256, tb.SAMPLE_MAX_V])
+@pytest.mark.parametrize("below", [31.1, 31.3, 33.5])
+def test_a_tail_at_the_end_of_the_weights(V, below):
+    """One token before all others, which round to one unit of 2^-44 or to nothing: by V * 2^-45 at most, less than any random number below 1 tells."""
+    x = np.full((4, V), -below, np.float32)
+    x[:, V // 3] = 0
+    for settings in (dict(), dict(top_p=0.9999999)):
+        check(x, [1e-7, 0.5, 0.9999, 0.99999994], **settings)
+    assert list(run(x[:2], [0.0, 1.0])) == ([0, V - 1] if below < 31.2 else [V // 3] * 2)
