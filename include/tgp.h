@@ -457,9 +457,11 @@ int  tgp_k_kv_unpack_q4(void *const *k_tiles, void *const *v_tiles, uint32_t n_t
                         uint32_t q_len, uint32_t pos0, int k_exp, int v_exp, const int32_t *pos_dev, void *stream);
 /* tgp_k_attn() over tiles in 4 bits, on what they stand for.  scratch_dev: tgp_k_attn_q4_scratch_bytes() for this q_len, not shared with a
  * call that may run at the same time: some megabytes below 32 queries; from there on the keys and values of all sequences up to max_len as bf16, or,
- * where that is more than 4 GiB, of as many sequences as that holds (one at least), which are then taken in turn.  Up to 31 queries, and more where they leave most of the GPU free, read the codes themselves; for
- * others, keys and values are unpacked into the scratch first and the kernels of tgp_k_attn() run on them.  A NaN in a position that a query does
- * not see does not reach its output. */
+ * where that is more than 4 GiB, of as many sequences as that holds (one at least), which are then taken in turn.  Up to 31 queries read the codes themselves, and more
+ * where that is expected to take less time; for others, keys and values are unpacked into the scratch first and the kernels of tgp_k_attn() run on them.  The two
+ * round differently: softmax weights are fp16 numbers where codes are read (half a step is 2^-11 of a weight), bf16 numbers where they are unpacked (2^-8, as in
+ * tgp_k_attn()), and where codes are read a query is fp16, too, scaled by a power of two of its largest number: numbers of less than 2^-17 of that are off by
+ * 2^-25 of it.  A NaN in a position that a query does not see does not reach its output. */
 int  tgp_k_attn_q4(const void *qb, void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, void *ob, const tgp_model_cfg *cfg, uint32_t B,
                    uint32_t q_len, uint32_t pos0, int k_exp, int v_exp, const int32_t *pos_dev, void *scratch_dev, void *stream);
 int  tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint64_t *bytes);

@@ -3,7 +3,8 @@
 // A page - one sequence and KV head of a tile - is TK rows of DH / 2 bytes of codes, two e2m1 numbers per byte with the lower dimension in the
 // lower half, and behind them TK rows of DH / 16 bytes of scales in e4m3, one for 16 dimensions.  An element stands for code * scale * 2^exp.
 // A code has two significant bits and a scale four, so code * scale is exact in fp16 and bf16, and what the kernels multiply is what the cache
-// stands for, without a rounding of its own: the only ones are the two when a position is appended, and those of the softmax weights.
+// stands for, without a rounding of its own.  Roundings are those of a position that is appended (fp32, bf16, scale and code), of the softmax weights (fp16 where the codes are read,
+// bf16 where the cache is unpacked for the kernels over bf16), and, where the codes are read, of a query's small numbers.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -335,7 +336,9 @@ __device__ __forceinline__ void attend_unit(const AttnQ4Args &a, uint8_t *q4_sm,
 #pragma unroll
     for (int i = 0; i < STAGES<DH, U> - 1; ++i) request();
 
-    // ---- the rows of Q: fp16 has fewer exponents than bf16, so each row is scaled to [1, 2) by a power of two, which its scores get back ----
+    // ---- the rows of Q: fp16 has fewer exponents than bf16, so each row is scaled to [1, 2) by a power of two, which its scores get back.  Numbers down to 2^-17 of the largest
+    // keep their bits, smaller ones are off by 2^-25 of it: what an fp32 sum loses next to a product of the largest, but more where the keys are zero there.  (Codes as bf16
+    // instead take another conversion and multiplication for two of them, a second fp16 part of Q as many MMAs again) ----
     uint32_t qf[NT][KS][2];
     float fix[NT][2];                                             // of the rows 2c and 2c + 1, which this lane's scores belong to
     uint32_t lim[NT][2];                                          // the last key that these rows see

@@ -284,6 +284,24 @@ def test_queries_of_any_size(std_q):
         check_attn(config(8, 2, 128, 2, 700, 64), 2, S, 600, std_q=std_q)
 
 
+@pytest.mark.parametrize("above,S,pos0", [(10, 1, 200), (17, 1, 200), (17, 5, 90), (18, 1, 200), (18, 5, 90)])
+def test_queries_whose_numbers_are_far_apart(above, S, pos0):
+    """One dimension of each query is 2^above times the others, and zero in the keys.  As fp16, scaled by the largest, the others are exact down to 2^-17 of it; below they
+    are off by 2^-25 of it, a score d by as much of the sum of |k|, and its weight by a factor of exp(d), as the sum of the weights."""
+    c, n = config(8, 2, 64, 2, 256, 32), pos0 + S
+    rng = np.random.default_rng(above)
+    (kh, _), (vh, vt) = random_tiles(rng, c, 8, 0), random_tiles(rng, c, 8, 0)
+    kh[..., 5:32 * 32:32] &= 0xf0                          # codes of dimension 10
+    q = rng.choice([-1, 1], (2, S, 8, 64)) * (1 + rng.integers(0, 128, (2, S, 8, 64)) / 128)
+    q[..., 10] = 2.0 ** above
+    got = run_attn(c, 2, S, pos0, q, [torch.from_numpy(t).to(DEV) for t in kh], vt)
+    K, V = decoded(kh, c, 0), decoded(vh, c, 0)
+    assert not K[..., 10].any()
+    for b in range(2):
+        d = 2.0 ** (above - 25) * np.abs(K[b, :, :n]).sum(-1).max() / 8 if above > 17 else 0.0
+        within(got[b], *kv_q4.attention(q[b], K[b], V[b], pos0), HALF_FP16 + np.expm1(2 * d) if d else HALF_FP16)
+
+
 def test_scores_that_rise_with_every_key():
     """The largest score so far is always the last: the reference moves again and again."""
     def change(q, kh, vh):
