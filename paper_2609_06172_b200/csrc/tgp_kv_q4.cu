@@ -104,9 +104,9 @@ struct AppendArgs {
 };
 
 // A thread takes four neighbouring dimensions of a head and their partners half a head away, as in tgp_rope_kv_vec_kernel: 16-byte loads, and the
-// four threads of a group of 16 dimensions are neighbours.  Meant to run at HBM's rate: 8192 positions of 64 + 2 x 8 heads of 128 take 100 us, 5.1 TB/s (513 MB),
-// with the issue slots 78 % busy: a rotated value costs 13 instructions, three without the exact sum.  (An estimate with an error bound first, the exact sum where the bound
-// does not settle the rounding, would leave no warp of 256 values without such a one.)  Eight single tokens: 3.9 us, which is the launch.
+// four threads of a group of 16 dimensions are neighbours.  8192 positions of 64 + 2 x 8 heads of 128 take 93 us with a cold L2, 4.9 TB/s
+// (with the read back right behind it 100 us, 5.1 TB/s of 513 MB), with the issue slots 78 % busy: a rotated value costs 13 instructions, three without the exact sum.  (An estimate with an error bound first, the exact sum where the bound
+// does not settle the rounding, would leave no warp of 256 values without such a one.)  Eight single tokens, read back: 3.9 us, which is the launches.
 template <int DH>
 __global__ void __launch_bounds__(256) tgp_rope_kv_q4_kernel(const AppendArgs a) {
     pdl_enter();
@@ -162,8 +162,9 @@ struct UnpackArgs {
     TgpTilePtrs tiles;
 };
 
-// A thread takes a group of 16 dimensions: 8 bytes of codes and a scale, 32 bytes of bf16.  Bound by what it writes: 8192 positions of 2 x 8 heads of 128 (9 MB of codes,
-// 34 MB of bf16) 13 us, alone with a cold L2.
+// A thread takes a group of 16 dimensions: 8 bytes of codes and a scale, 32 bytes of bf16.  8192 positions of 2 x 8 heads of 128 (9 MB of codes, 34 MB of bf16) take
+// 13 us with a cold L2, 3.3 TB/s, twice what HBM needs: a thread's 9 bytes are all that it has requested while it waits (memory is what warps wait for most,
+// 58 % of the issue slots are busy).
 template <int DH>
 __global__ void __launch_bounds__(256) tgp_kv_unpack_q4_kernel(const UnpackArgs a) {
     pdl_enter();
@@ -239,10 +240,12 @@ __global__ void __launch_bounds__(256) tgp_attn_q4_nan_kernel(const NanArgs a) {
 // Row r of a chunk stands for key (r % 2) * 4 + r / 2, and row r + 8 for the key 8 further on: the four keys of a lane's V are then
 // c, c + 4, c + 8, c + 12, and each of those loads reads four neighbouring rows.
 // S leaves the MMA with a key per lane row, P enters the next with a key per register pair: two 8 x 8 transposes (movmatrix) of P in fp16.
-// Bound by instructions, not by HBM: 16 keys of 128 dimensions (2.3 KB of K and V) take about 290 of a warp's, most of them conversions and the products with the scales, and
-// the issue slots are 61 % busy.  24 sequences of 12001 keys, 64 heads over 8 x 128: 71 us, 4.7 TB/s (333 MB; HBM would take 52); 61 of up to 2501 keys at positions of their own, 32 heads over
-// 8: 27.6 us (13); one of 701 keys: 4.2 us, a launch and its ramp.  Scales after the MMAs instead of on the codes would need an MMA per group of 16 dimensions with sums of its own; 128 registers
-// and four CTAs an SM are faster than five, which spill.
+// Bound by the chain of a warp's steps - conversion, S, vote, exponentials, transpose, O, chunk after chunk - at four warps a scheduler: 16 keys of 128 dimensions (2.3 KB of K and
+// V) take about 290 instructions, most of them conversions and the products with the scales, which the issue slots (61 % busy) would do in half of the time; a warp waits for its
+// own last instruction's result or for the pipe of the conversions twice as long as it issues.  Calls in a row, whose cache may lie in L2 / behind an L2 flush: 24 sequences of 12001 keys, 64 heads over 8 x 128
+// 71 / 86 us (333 MB, which HBM would move in 51); 61 of up to 2501 keys at positions of their own, 32 heads over 8 27.5 / 37 (12; 41 us when the host waits for each call); one of 701 keys 4.1 / 10, a launch and
+// its ramp.  Scales after the MMAs instead of on the codes would need an MMA per group of 16 dimensions with sums of its own; 128 registers and four CTAs an SM are faster than five, which
+// spill (with 16 rows three CTAs of 168 registers, where chunks of 32 keys of 128 dimensions spill 8 to 20 bytes).
 struct AttnQ4Args {
     const bf16 *qb; bf16 *ob; float *scratch; const int32_t *pos;
     uint32_t Hq, Hkv, G, TK, q_len, pos0, rows, row_blocks, parts, per_part, chunk, B;      // chunk: keys of one, 16 or 32; per_part: chunks
