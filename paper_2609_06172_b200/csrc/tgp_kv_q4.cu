@@ -104,9 +104,9 @@ struct AppendArgs {
 };
 
 // A thread takes four neighbouring dimensions of a head and their partners half a head away, as in tgp_rope_kv_vec_kernel: 16-byte loads, and the
-// four threads of a group of 16 dimensions are neighbours.  8192 positions of 64 + 2 x 8 heads of 128 take 93 us with a cold L2, 4.9 TB/s
-// (with the read back right behind it 100 us, 5.1 TB/s of 513 MB), with the issue slots 78 % busy: a rotated value costs 13 instructions, three without the exact sum.  (An estimate with an error bound first, the exact sum where the bound
-// does not settle the rounding, would leave no warp of 256 values without such a one.)  Eight single tokens, read back: 3.9 us, which is the launches.
+// four threads of a group of 16 dimensions are neighbours.  8192 positions of 64 + 2 x 8 heads of 128 (479 MB) take 93 us with a cold L2, 5.1 TB/s,
+// with the issue slots 78 % busy (100 us with the read back right behind it): a rotated value costs 13 instructions, three without the exact sum.  (An estimate with an error bound
+// first, the exact sum where the bound does not settle the rounding, would leave no warp of 256 values without such a one.)  Eight single tokens, read back: 3.9 us, which is the launches.
 template <int DH>
 __global__ void __launch_bounds__(256) tgp_rope_kv_q4_kernel(const AppendArgs a) {
     pdl_enter();
