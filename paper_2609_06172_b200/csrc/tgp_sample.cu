@@ -14,7 +14,7 @@
 //   where a list would be too long (equal logits, a large top-k): further histograms, each 2048 times finer in the logits' bits, down to one value;
 //   the draw: sums of the kept weights by warp, in the order of the tokens, and the one segment that the random number falls into once more.
 // Bound by instructions, not by the 4 B V bytes (5.1 us at 64 x 128256): us at 1 x 32000 and 64 x 128256: the maximum alone 2.9 and 6.0 (5.5 TB/s), no filter 7.8 and 26 (one sum of weights
-// more: nine operations in fp64 and a conversion for each token that can be drawn), top-k of 50 11.1 and 19 (two passes that compute no weights), top-p of 0.9 21 and 61 (a weight and two atomics per
+// more: nine operations in fp64 and a conversion for each token that can be drawn), top-k of 50 11.1 and 19 (two passes that compute no weights), top-p of 0.9 21 and 62 (a weight and two atomics per
 // token, then the weights of those above the bin once more); a top-k of 900 sorts its list, 34 and 60.  Eight CTAs per row where that fits two to an SM (four at 64 rows; eight there are
 // slower).  A weight with a table of 32 entries, without bank conflicts, and two more terms: 28 instead of 26.
 #include <cuda_runtime.h>
@@ -94,12 +94,13 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
 struct Row {
-    float top, step, low;                                        // the maximum; 64 / temperature; what is below weighs nothing (and is no NaN, nor -inf)
+    float top, half, step, low;                                  // the maximum, and half of it; 128 / temperature; what is below weighs nothing (and is no NaN, nor -inf)
     double top64, rate;                                          // the maximum (0 where it is infinite); OCTAVE * log2(e) / temperature
     const double *octave;
-    // bin of a logit that is no NaN and above -inf; those of BINS - 1 weigh nothing.  (Rounded by what 2^23 leaves of the fraction, without a conversion.)
+    // bin of a logit that is no NaN and above -inf; those of BINS - 1 weigh nothing.  (Half of the difference: the whole may be more than fp32 holds.  Rounded by what 2^23 leaves of the
+    // fraction, without a conversion.)
     __device__ __forceinline__ uint32_t bin(float x) const {
-        const float z = x == top ? 0.f : fminf((top - x) * step, (float)(BINS - 1));            // (fminf: a NaN, infinity times 0, is BINS - 1)
+        const float z = x == top ? 0.f : fminf(fmaf(x, -0.5f, half) * step, (float)(BINS - 1));            // (fminf: a NaN, infinity times 0, is BINS - 1)
         return __float_as_uint(z + 8388608.f) & (BINS - 1);
     }
     // The weight of a logit not below `low` (of others: any number): with t = OCTAVE log2(e) (x - top) / temperature = n + f, |f| <= 1/2, it is 2^(n / OCTAVE)
@@ -248,7 +249,8 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_sample_kernel(const SampleArgs
     }
     const double inv = 1.0 / (double)fmaxf(temperature, 7.52316384526264e-37f);        // 2^-120: bins are told in fp32
     r.rate = inv * (OCTAVE * 1.4426950408889634074);
-    r.step = (float)(64.0 * inv);
+    r.step = (float)(128.0 * inv);
+    r.half = 0.5f * r.top;
     r.top64 = (double)r.top;
     r.low = r.top == INFINITY ? INFINITY : fmaxf((float)(r.top64 - 33.0 / inv), -3.402823466e38f);
     r.octave = sh.octave;

@@ -189,3 +189,14 @@ def test_a_tail_at_the_end_of_the_weights(V, below):
     for settings in (dict(), dict(top_p=0.9999999)):
         check(x, [1e-7, 0.5, 0.9999, 0.99999994], **settings)
     assert list(run(x[:2], [0.0, 1.0])) == ([0, V - 1] if below < 31.2 else [V // 3] * 2)
+
+
+@pytest.mark.parametrize("temperature", [1.0, 3e37, 1e38, 3.4e38, float("inf")])
+@pytest.mark.parametrize("settings", [dict(), dict(top_k=30), dict(top_k=1000), dict(top_k=5500), dict(top_p=0.6), dict(top_p=0.95), dict(top_k=5000, top_p=0.9), dict(min_p=0.01)], ids=str)
+def test_logits_whose_difference_is_no_number_of_fp32(temperature, settings):
+    """The largest and the lowest logits lie further apart than fp32 reaches, and are as likely where the temperature is high enough."""
+    rng = np.random.default_rng(15)
+    top = np.finfo(np.float32).max
+    x = np.stack([rng.choice([top, -top, 0.0, 1e38, -2e38], 6000), rng.choice([top, -top], 6000), np.where(np.arange(6000) == 4321, top, -top), rng.uniform(-1, 1, 6000) * top])
+    for u in (0.0, 0.3, 0.7, 0.99999994):
+        check(x, [u] * 4, temperature=temperature, **settings)
