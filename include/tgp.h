@@ -439,6 +439,7 @@ int  tgp_k_attn_decode_static(const void *qb, void *const *k_tiles, void *const 
  * 2^(exp - 3) and 2^(exp + 11)).  A scale that is NaN makes its group NaN, in every call.
  * In the calls below Dh is 64 or 128, TK a multiple of 16, B <= cfg->B, pos0 + q_len <= cfg->max_len, at most 64 tiles; tiles and the other
  * device arrays, but for pos_dev, begin on 16 bytes; tile arrays are host arrays, and tiles that hold none of the call's positions may be NULL.
+ * Beyond a grid's size - B * Hkv above 65535 in tgp_k_kv_unpack_q4(), B above 65535 in tgp_k_attn_q4() - a call returns TGP_E_TOO_LARGE.
  * pos_dev, if not NULL, gives each sequence a position of its own and is for single tokens (q_len == 1): int32 [B] on the device, the
  * position of sequence b's new token, at most pos0.  A sequence whose entry lies outside [0, pos0] is idle: nothing of it is read or
  * appended, and its attention output is zero.  As pos_dev is read by the kernels, a captured step may be replayed with other positions. */

@@ -61,6 +61,13 @@ def test_calls_on_4_bit_tiles_refuse(call):
     call(B=0), call(S=0, pos0=0)                           # nothing to do
 
 
+def test_batches_beyond_a_grid_are_refused():
+    refused(tb.E_TOO_LARGE, unpack, cfg(B=32768), B=32768)              # 65536 pages
+    refused(tb.E_TOO_LARGE, attn, cfg(B=65536), B=65536)
+    refused(tb.E_TOO_LARGE, attn, cfg(B=65536), B=65536, S=40)
+    refused(tb.E_TOO_LARGE, append, cfg(B=1 << 30), B=1 << 30, S=2)
+
+
 def test_missing_and_misaligned_arguments():
     for kw in (dict(q=None), dict(o=None), dict(scratch=None), dict(q=A + 2), dict(o=A + 8), dict(scratch=A + 4)):
         refused(tb.E_INVAL, attn, **kw)
