@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(256) tgp_attn_q4_nan_kernel(const NanArgs a) {
 // Bound by the chain of a warp's steps - conversion, S, vote, exponentials, transpose, O, chunk after chunk - at four warps a scheduler: 16 keys of 128 dimensions (2.3 KB of K and
 // V) take about 290 instructions, most of them conversions and the products with the scales, which the issue slots (61 % busy) would do in half of the time; a warp waits for its
 // own last instruction's result or for the pipe of the conversions twice as long as it issues.  Calls in a row, whose cache may lie in L2 / behind an L2 flush: 24 sequences of 12001 keys, 64 heads over 8 x 128
-// 71 / 86 us (333 MB, which HBM would move in 51); 61 of up to 2501 keys at positions of their own, 32 heads over 8 27.5 / 37 (12; 41 us when the host waits for each call); one of 701 keys 4.1 / 10, a launch and
+// 71 / 84 - 86 us (333 MB, which HBM would move in 51); 61 of up to 2501 keys at positions of their own, 32 heads over 8 27.5 - 29 / 37 (12; 41 us when the host waits for each call); one of 701 keys 4.1 / 10, a launch and
 // its ramp.  Scales after the MMAs instead of on the codes would need an MMA per group of 16 dimensions with sums of its own; 128 registers and four CTAs an SM are faster than five, which
 // spill (with 16 rows three CTAs of 168 registers, where chunks of 32 keys of 128 dimensions spill 8 to 20 bytes).
 struct AttnQ4Args {

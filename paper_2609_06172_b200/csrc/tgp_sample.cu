@@ -13,7 +13,7 @@
 //   else top-p: a histogram of the weights over 2047 bins of 1 / 64 in (max - logit) / temperature tells the bin in which t lies; its tokens are such a list;
 //   where a list would be too long (equal logits, a large top-k): further histograms, each 2048 times finer in the logits' bits, down to one value;
 //   the draw: sums of the kept weights by warp, in the order of the tokens, and the one segment that the random number falls into once more.
-// Bound by instructions, not by the 4 B V bytes (5.1 us at 64 x 128256): us at 1 x 32000 and 64 x 128256: the maximum alone 2.9 and 6.0 (5.5 TB/s), no filter 7.8 and 26 (one sum of weights
+// Bound by instructions, not by the 4 B V bytes (5.0 us at 64 x 128256): us at 1 x 32000 and 64 x 128256: the maximum alone 2.9 and 6.0 (5.5 TB/s), no filter 7.8 and 26 (one sum of weights
 // more: nine operations in fp64 and a conversion for each token that can be drawn), top-k of 50 11.1 and 19 (two passes that compute no weights), top-p of 0.9 21 and 62 (a weight and two atomics per
 // token, then the weights of those above the bin once more); a top-k of 900 sorts its list, 34 and 60.  Eight CTAs per row where that fits two to an SM (four at 64 rows; eight there are
 // slower).  A weight with a table of 32 entries, without bank conflicts, and two more terms: 28 instead of 26.
