@@ -379,7 +379,7 @@ int  tgp_k_attn_select(int impl);
  * of query heads); 1 forces the CUDA-core kernels.  The tensor-core kernel rounds P to bf16 for the second product; while the
  * batch's context adds up to less than 256 chunks it multiplies what that leaves over with V too, all 24 bits of P.  Process-wide. */
 int  tgp_k_attn_decode_select(int impl);
-/* Error word of the tcgen05 attention kernel: 0, or which bounded wait ran out first (1 for S, 2 for P V, 3 for a K/V
+/* Error word of the tcgen05 attention kernels (over KV tiles and over pages): 0, or which bounded wait ran out first (1 for S, 2 for P V, 3 for a K/V
  * load, 4 for the hand-over between the softmax warps and the MMA warp), or 5 if shared memory was not 1024-byte
  * aligned.  A CTA that gives up stores nothing.  Synchronous. */
 int  tgp_k_attn_status(int *error_code);
@@ -476,6 +476,42 @@ int  tgp_k_attn_q4_scratch_bytes(const tgp_model_cfg *cfg, uint32_t q_len, uint6
 #define TGP_KV_Q4   1u
 int  tgp_k_kv_move(void *const *k_tiles, void *const *v_tiles, uint32_t n_tiles, const int32_t *src, const int32_t *dst, uint32_t n,
                    const tgp_model_cfg *cfg, uint32_t form, uint32_t B, uint32_t len, void *stream);
+/* ---- a KV cache in pages, for batches whose sequences differ in length ------------------------------------------------
+ * (No counterpart in the paper: what a program that serves requests needs between a step's products.)
+ * A page holds TK = cfg->TK positions of one sequence and all KV heads: bf16 [Hkv, TK, Dh].  The n_pages pages of a layer are one array of keys and one of values.  table int32
+ * [B, W], W = ceil(max_len / TK), lists the pages of each sequence: position p is row p % TK of page table[b][p / TK].  All layers of a model may share a table.  A step's
+ * rows lie one sequence behind the other: rows start[b] ... start[b + 1] - 1 of its T rows are sequence b's, at its last positions before end[b] (start int32 [B + 1], end int32 [B]).  All
+ * of this lies on the device and is read by the kernels, so a captured step may be replayed with other lengths and tables.
+ * In the calls below B <= cfg->B and B <= TGP_PAGED_MAX_B, n_pages * TK < 2^31; arrays of int32 and fp32 that are read one number at a time begin on 4 bytes, others on 16.
+ * No two arrays of a call may overlap unless it says so. */
+#define TGP_PAGED_MAX_B 4096u
+/* Pages and places of a step.  Sequence b keeps its first len[b] positions and adds add[b]: its table row then lists ceil((len + add) / TK) pages.  held int32 [B] is how many it lists before and
+ * after the call.  Pages beyond that go back - a sequence that has ended has len = add = 0, one whose drafted tokens were refused a len below what it had - and their
+ * entries become -1; pages that it lacks are taken.  free int32 [n_pages] is the stack of free pages, *n_free of them, the last one the first to go.  Pages go back before any is taken,
+ * sequence by sequence and in the order of the table, the first on top: a step that is taken back leaves the stack as it was.  Entries of the stack above *n_free keep what they hold.
+ * A sequence is served unless it asks for pages and those before it and it ask for more than there are, or for positions and those before it and it ask for more than T (those that are not served
+ * counted too); else it gets neither pages nor rows in this step, and keeps what it has.  A sequence with len < 0, add < 0 or len + add > max_len keeps what it has and gets nothing.  A page belongs to
+ * one sequence at most.
+ * Written: start [B + 1] and end [B] as above, end[b] = len[b] + rows of b; slot [T] and pos [T], of each row the place page * TK + position % TK and the position, -1 in rows behind
+ * the last sequence's.  Every argument is a device array. */
+int  tgp_k_page_plan(const int32_t *len_dev, const int32_t *add_dev, int32_t *table_dev, int32_t *held_dev, int32_t *free_dev, int32_t *n_free_dev, int32_t *start_dev, int32_t *end_dev,
+                     int32_t *slot_dev, int32_t *pos_dev, const tgp_model_cfg *cfg, uint32_t B, uint32_t n_pages, uint32_t T, void *stream);
+/* tgp_k_rope_kv() for pages: row t of q32, k32, v32 [T, H*Dh] is rotated by position pos[t] and rounded as there - the same bits -, its key and value put into place slot[t].  A row
+ * whose place is outside the pages, or whose position is outside [0, max_len), is left out: nothing of it is read or written.  No two rows may have the same place.  Dh is 64 or 128. */
+int  tgp_k_rope_kv_paged(const float *q32, const float *k32, const float *v32, void *qb, void *k_pages, void *v_pages, const float *cos_dev, const float *sin_dev, const int32_t *slot_dev,
+                         const int32_t *pos_dev, const tgp_model_cfg *cfg, uint32_t T, uint32_t n_pages, void *stream);
+/* Attention of a step's rows over the pages: single tokens, drafted tokens and prompts in one call.  The row at position p sees the positions j <= p - with window > 0 those of them with
+ * j > p - window or j < sinks -: o = softmax(q K^T / sqrt(Dh)) V, bf16 [T, Hq*Dh].  q_max and kv_max are bounds of the rows of a sequence and of end[b]; a sequence beyond them, or with end[b] less
+ * than its rows, is idle: its rows of o are zero.  Rows of no sequence keep what they hold, and with start outside [0, T] or falling a sequence has no rows.  A position whose table entry lies outside [0, n_pages)
+ * is not seen; a row that sees nothing is zero.  Entries of positions that no row sees (before a window, behind the sequence) are not read as pages.  What the pages hold in positions that a row does not
+ * see does not reach it, NaN or not.  Dh is 64 or 128, TK a multiple of 16, at most 128 query heads share a KV head; kv_max <= max_len.
+ * Softmax weights are rounded to bf16 (half a step is 2^-8 of a weight), sums are fp32.  Sequences of up to 16 rows * query heads per KV head (32 where q_max has more than 16) are split
+ * over the GPU by their lengths, prompts go to the tcgen05 kernel; a row's bits may depend on the lengths of the other sequences (how a context is split), and not on anything else.
+ * scratch_dev: tgp_k_attn_paged_scratch_bytes() for at least these arguments, of any contents, not shared with a call that may run at the same time; between two calls that share it other use is fine.
+ * B * Hkv * ceil(kv_max / 16) and n_pages * TK * Hkv have to stay below 2^31 (TGP_E_TOO_LARGE). */
+int  tgp_k_attn_paged(const void *qb, const void *k_pages, const void *v_pages, void *ob, const int32_t *table_dev, const int32_t *start_dev, const int32_t *end_dev, const tgp_model_cfg *cfg,
+                      uint32_t B, uint32_t T, uint32_t q_max, uint32_t kv_max, uint32_t n_pages, uint32_t window, uint32_t sinks, void *scratch_dev, void *stream);
+int  tgp_k_attn_paged_scratch_bytes(const tgp_model_cfg *cfg, uint32_t B, uint32_t T, uint32_t q_max, uint32_t kv_max, uint64_t *bytes);
 /* a = bf16(silu(g) * u), g/u fp32 [M, F]. */
 int  tgp_k_swiglu(const float *g32, const float *u32, void *ab, uint64_t n_elems, void *stream);
 /* out[b] = argmax_j logits[b, j], lowest index on ties. */
@@ -493,6 +529,20 @@ int  tgp_k_argmax(const float *logits, int32_t *out, uint32_t B, uint32_t V, voi
 #define TGP_SAMPLE_MAX_V (1u << 19)
 int  tgp_k_sample(const float *logits, const float *u_dev, int32_t *out, uint32_t B, uint32_t V, const float *temperature_dev, const int32_t *top_k_dev,
                   const float *top_p_dev, const float *min_p_dev, void *stream);
+
+/* Verification of drafted tokens.  The rows of a step (start int32 [B + 1], as above) were fed tokens [T]: of a sequence its last token and those that a draft proposed behind it.  Row r holds the target's
+ * logits [T, V] behind its token, and judges the token of row r + 1, d, unless it is its sequence's last: with p = softmax(logits / temperature), q = softmax(draft_logits / temperature) of row r, d is taken if
+ * u[r] * q(d) < p(d).  The first that is not is replaced by a token of the distribution max(p - q, 0), normalised; if all are taken, a token of p of the last row follows.  A token of a
+ * distribution is the lowest, in the order of the indices, at which its sum exceeds u_draw[b] of the whole.  draft_logits NULL: q(d) = 1 (a draft that proposes without drawing).  Where nothing is left of p - q
+ * the token is one of p.
+ * out [T]: in the rows of a sequence the tokens that it goes on with - those taken and the one drawn -, then -1; n_out [B]: how many (0 for a sequence without rows, or whose rows do not lie in [0, T)).  Rows of no
+ * sequence keep what they hold.  What stays in the cache are the rows fed with tokens that hold: length before the step + n_out.
+ * temperature fp32 [B] or NULL (1); a row's 0, negative or NaN: d is taken if it is the row's likeliest token (the lowest of equals), which also is the token that follows.  Logits of -inf and NaN
+ * weigh nothing (so filters may be applied to both by -inf); a row of nothing else takes no token and gives token 0.  A drafted token outside [0, V) is not taken.  u and u_draw are limited to [0, 1].  Weights and sums are in 64 bits, weights
+ * of less than 2^-1000 of a row's largest are 0.  draft_logits of a sequence's last row are not read.  scratch_dev: tgp_k_verify_scratch_bytes(), not shared with a call that may run at the same time.  T <= 32767, V <= TGP_SAMPLE_MAX_V. */
+int  tgp_k_verify(const float *logits, const float *draft_logits, const int32_t *tokens_dev, const int32_t *start_dev, const float *u_dev, const float *u_draw_dev, int32_t *out_dev, int32_t *n_out_dev,
+                  uint32_t B, uint32_t T, uint32_t V, const float *temperature_dev, void *scratch_dev, void *stream);
+int  tgp_k_verify_scratch_bytes(uint32_t T, uint32_t V, uint64_t *bytes);
 
 #ifdef __cplusplus
 }

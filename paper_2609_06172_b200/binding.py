@@ -29,6 +29,7 @@ X_TAIL = 0x100
 (K_EMBED, K_G1, K_WQ, K_WK, K_WV, K_WO, K_G2, K_WG, K_WU, K_WD, K_GF, K_LM, K_ROUTER, K_KTILE, K_VTILE) = range(15)
 KV_BF16, KV_Q4 = 0, 1
 SAMPLE_MAX_V = 1 << 19
+PAGED_MAX_B = 4096
 TAP_H, TAP_HF, TAP_Q, TAP_KTILE, TAP_VTILE, TAP_O, TAP_A = range(7)
 
 
@@ -138,6 +139,12 @@ _SIGS = {
     "tgp_k_attn_q4": [_P, C.POINTER(_P), C.POINTER(_P), _U32, _P, C.POINTER(ModelCfg), _U32, _U32, _U32, C.c_int, C.c_int, _P, _P, _P],
     "tgp_k_attn_q4_scratch_bytes": [C.POINTER(ModelCfg), _U32, C.POINTER(_U64)],
     "tgp_k_kv_move": [C.POINTER(_P), C.POINTER(_P), _U32, C.POINTER(_I32), C.POINTER(_I32), _U32, C.POINTER(ModelCfg), _U32, _U32, _U32, _P],
+    "tgp_k_page_plan": [_P] * 10 + [C.POINTER(ModelCfg), _U32, _U32, _U32, _P],
+    "tgp_k_rope_kv_paged": [_P] * 10 + [C.POINTER(ModelCfg), _U32, _U32, _P],
+    "tgp_k_attn_paged": [_P] * 7 + [C.POINTER(ModelCfg)] + [_U32] * 7 + [_P, _P],
+    "tgp_k_attn_paged_scratch_bytes": [C.POINTER(ModelCfg), _U32, _U32, _U32, _U32, C.POINTER(_U64)],
+    "tgp_k_verify": [_P] * 8 + [_U32, _U32, _U32, _P, _P, _P],
+    "tgp_k_verify_scratch_bytes": [_U32, _U32, C.POINTER(_U64)],
     "tgp_k_sample": [_P, _P, _P, _U32, _U32, _P, _P, _P, _P, _P],
 }
 
@@ -180,7 +187,8 @@ def _load_fastcall(l):
     except ImportError:
         return
     _fastcall.bind(tuple(C.cast(getattr(l, "tgp_k_" + n), C.c_void_p).value for n in ("embed", "rmsnorm", "gemm", "gemm_group", "rope_kv", "attn", "swiglu", "argmax",
-                                                                                                         "rope_kv_q4", "kv_unpack_q4", "attn_q4", "kv_move", "sample")),
+                                                                                                         "rope_kv_q4", "kv_unpack_q4", "attn_q4", "kv_move", "sample",
+                                                                                                         "page_plan", "rope_kv_paged", "attn_paged", "verify")),
                    ModelCfg, np.ndarray)
     _fast = _fastcall
 
@@ -715,3 +723,54 @@ def k_sample(logits, u, out, B, V, temperature=None, top_k=None, top_p=None, min
         rc = lib().tgp_k_sample(_ptr(logits), _ptr(u), _ptr(out), B, V, _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(stream))
     if rc:
         raise TgpError(rc, "tgp_k_sample")
+
+
+def k_page_plan(length, add, table, held, free, n_free, start, end, slot, pos, cfg, B, n_pages, T, stream=None):
+    """Pages given back and taken, and the places of a step's T rows: sequence b keeps length[b] positions and adds add[b].  Everything but the numbers is a device array."""
+    rc = _fast.page_plan(length, add, table, held, free, n_free, start, end, slot, pos, cfg, B, n_pages, T, stream)
+    if rc is None:
+        rc = lib().tgp_k_page_plan(_ptr(length), _ptr(add), _ptr(table), _ptr(held), _ptr(free), _ptr(n_free), _ptr(start), _ptr(end), _ptr(slot), _ptr(pos), C.byref(cfg), B, n_pages, T,
+                                   _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_page_plan")
+
+
+def k_rope_kv_paged(q32, k32, v32, qb, k_pages, v_pages, cos, sin, slot, pos, cfg, T, n_pages, stream=None):
+    rc = _fast.rope_kv_paged(q32, k32, v32, qb, k_pages, v_pages, cos, sin, slot, pos, cfg, T, n_pages, stream)
+    if rc is None:
+        rc = lib().tgp_k_rope_kv_paged(_ptr(q32), _ptr(k32), _ptr(v32), _ptr(qb), _ptr(k_pages), _ptr(v_pages), _ptr(cos), _ptr(sin), _ptr(slot), _ptr(pos), C.byref(cfg), T, n_pages,
+                                       _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_rope_kv_paged")
+
+
+def k_attn_paged(qb, k_pages, v_pages, ob, table, start, end, cfg, B, T, q_max, kv_max, n_pages, window=0, sinks=0, scratch=None, stream=None):
+    """scratch: k_attn_paged_scratch_bytes(cfg, B, T, q_max, kv_max) of device memory, needed by every call."""
+    rc = _fast.attn_paged(qb, k_pages, v_pages, ob, table, start, end, cfg, B, T, q_max, kv_max, n_pages, window, sinks, scratch, stream)
+    if rc is None:
+        rc = lib().tgp_k_attn_paged(_ptr(qb), _ptr(k_pages), _ptr(v_pages), _ptr(ob), _ptr(table), _ptr(start), _ptr(end), C.byref(cfg), B, T, q_max, kv_max, n_pages, window, sinks,
+                                    _ptr(scratch), _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_attn_paged")
+
+
+def k_attn_paged_scratch_bytes(cfg, B, T, q_max, kv_max):
+    n = _U64()
+    _k(lib().tgp_k_attn_paged_scratch_bytes(C.byref(cfg), B, T, q_max, kv_max, C.byref(n)), "tgp_k_attn_paged_scratch_bytes")
+    return n.value
+
+
+def k_verify(logits, draft_logits, tokens, start, u, u_draw, out, n_out, B, T, V, temperature=None, scratch=None, stream=None):
+    """scratch: k_verify_scratch_bytes(T, V) of device memory, needed by every call; draft_logits None: the draft proposes without drawing."""
+    rc = _fast.verify(logits, draft_logits, tokens, start, u, u_draw, out, n_out, B, T, V, temperature, scratch, stream)
+    if rc is None:
+        rc = lib().tgp_k_verify(_ptr(logits), _ptr(draft_logits), _ptr(tokens), _ptr(start), _ptr(u), _ptr(u_draw), _ptr(out), _ptr(n_out), B, T, V, _ptr(temperature), _ptr(scratch),
+                                _ptr(stream))
+    if rc:
+        raise TgpError(rc, "tgp_k_verify")
+
+
+def k_verify_scratch_bytes(T, V):
+    n = _U64()
+    _k(lib().tgp_k_verify_scratch_bytes(T, V, C.byref(n)), "tgp_k_verify_scratch_bytes")
+    return n.value

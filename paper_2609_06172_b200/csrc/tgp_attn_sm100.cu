@@ -57,23 +57,6 @@ struct TArgs {
     int32_t krow[TGP_MAX_TILES], vrow[TGP_MAX_TILES];       // first row of each KV tile in the map over all tiles
 };
 
-// MN-major operand in the same swizzled storage: 64 contiguous elements (128 B) of the MN dimension per row, rows are
-// K; the next 64 MN elements start `lbo` bytes further (leading byte offset), the next 8 K rows 1024 bytes further.
-__device__ __forceinline__ uint64_t umma_desc_mn(uint32_t smem_addr, uint32_t lbo) {
-    return (uint64_t)((smem_addr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-
-// byte offset of 16-byte chunk c (0..7) of row r inside a [rows x 128 B] tile with the 128-byte swizzle
-__device__ __forceinline__ uint32_t sw128(uint32_t r, uint32_t c) { return r * 128u + ((c ^ (r & 7u)) << 4); }
-
-__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-// two fp32 values per instruction (sm_100 packed arithmetic) and the three-input maximum
-__device__ __forceinline__ uint64_t pack2(float lo, float hi) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
-__device__ __forceinline__ void unpack2(uint64_t r, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(x), "l"(y), "l"(z)); return d; }
-__device__ __forceinline__ uint64_t add2(uint64_t x, uint64_t y) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(x), "l"(y)); return d; }
-__device__ __forceinline__ float max3(float x, float y, float z) { float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(x), "f"(y), "f"(z)); return d; }
-
 // SPLIT: two CTAs of a cluster share the queries, each with half of the key blocks, for grids that leave SMs without a second CTA or without one: the chain of
 // key blocks is half as long.  They exchange what they have of half of the dimensions through shared memory, with the sums and exponent references, and
 // each stores the other half.
@@ -484,5 +467,5 @@ int tgpk_attn_status_clear() { const int z = 0; return cudaMemcpyToSymbol(g_attn
 extern "C" int tgp_k_attn_status(int *error_code) {
     if (!error_code) return TGP_E_INVAL;
     if (cudaMemcpyFromSymbol(error_code, g_attn_tc_error, sizeof(int)) != cudaSuccess) return TGP_E_CUDA;
-    return TGP_OK;
+    return *error_code ? TGP_OK : tgpk_attn_paged_status(error_code);
 }

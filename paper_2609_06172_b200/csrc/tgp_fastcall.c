@@ -28,6 +28,13 @@ static struct {
     int (*attn_q4)(const void *, void *const *, void *const *, uint32_t, void *, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, int, int, const int32_t *, void *, void *);
     int (*kv_move)(void *const *, void *const *, uint32_t, const int32_t *, const int32_t *, uint32_t, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, void *);
     int (*sample)(const float *, const float *, int32_t *, uint32_t, uint32_t, const float *, const int32_t *, const float *, const float *, void *);
+    int (*page_plan)(const int32_t *, const int32_t *, int32_t *, int32_t *, int32_t *, int32_t *, int32_t *, int32_t *, int32_t *, int32_t *, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t,
+                     void *);
+    int (*rope_kv_paged)(const float *, const float *, const float *, void *, void *, void *, const float *, const float *, const int32_t *, const int32_t *, const tgp_model_cfg *, uint32_t,
+                         uint32_t, void *);
+    int (*attn_paged)(const void *, const void *, const void *, void *, const int32_t *, const int32_t *, const int32_t *, const tgp_model_cfg *, uint32_t, uint32_t, uint32_t, uint32_t, uint32_t,
+                      uint32_t, uint32_t, void *, void *);
+    int (*verify)(const float *, const float *, const int32_t *, const int32_t *, const float *, const float *, int32_t *, int32_t *, uint32_t, uint32_t, uint32_t, const float *, void *, void *);
 } lib;
 static PyObject *s_data_ptr, *s_cuda_stream, *cfg_type, *array_type;
 
@@ -269,7 +276,52 @@ static PyObject *f_sample(PyObject *self, PyObject *const *a, Py_ssize_t nargs) 
     CALL(rc, lib.sample(logits, u, out, B, V, t, k, p, m, st));
 }
 
-#define ENTRIES 13
+/* the first n arguments as addresses, or as numbers */
+static int all_addresses(PyObject *const *a, int n, void **out) {
+    for (int i = 0; i < n; ++i) if (!address(a[i], &out[i])) return 0;
+    return 1;
+}
+static int all_numbers(PyObject *const *a, int n, uint32_t *out) {
+    for (int i = 0; i < n; ++i) if (!u32(a[i], &out[i])) return 0;
+    return 1;
+}
+
+static PyObject *f_page_plan(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *p[10], *st;
+    uint32_t n[3];
+    tgp_model_cfg cfg;
+    ARGS(15);
+    if (!all_addresses(a, 10, p) || !config(a[10], &cfg) || !all_numbers(a + 11, 3, n) || !address(a[14], &st)) return not_mine();
+    CALL(rc, lib.page_plan(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], &cfg, n[0], n[1], n[2], st));
+}
+
+static PyObject *f_rope_kv_paged(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *p[10], *st;
+    uint32_t n[2];
+    tgp_model_cfg cfg;
+    ARGS(14);
+    if (!all_addresses(a, 10, p) || !config(a[10], &cfg) || !all_numbers(a + 11, 2, n) || !address(a[13], &st)) return not_mine();
+    CALL(rc, lib.rope_kv_paged(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], &cfg, n[0], n[1], st));
+}
+
+static PyObject *f_attn_paged(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *p[7], *scratch, *st;
+    uint32_t n[7];
+    tgp_model_cfg cfg;
+    ARGS(17);
+    if (!all_addresses(a, 7, p) || !config(a[7], &cfg) || !all_numbers(a + 8, 7, n) || !address(a[15], &scratch) || !address(a[16], &st)) return not_mine();
+    CALL(rc, lib.attn_paged(p[0], p[1], p[2], p[3], p[4], p[5], p[6], &cfg, n[0], n[1], n[2], n[3], n[4], n[5], n[6], scratch, st));
+}
+
+static PyObject *f_verify(PyObject *self, PyObject *const *a, Py_ssize_t nargs) {
+    void *p[8], *t, *scratch, *st;
+    uint32_t n[3];
+    ARGS(14);
+    if (!all_addresses(a, 8, p) || !all_numbers(a + 8, 3, n) || !address(a[11], &t) || !address(a[12], &scratch) || !address(a[13], &st)) return not_mine();
+    CALL(rc, lib.verify(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], n[0], n[1], n[2], t, scratch, st));
+}
+
+#define ENTRIES 17
 /* bind(addresses of the entry points in the order of `lib`, type of the model configuration, type of numpy's arrays) */
 static PyObject *f_bind(PyObject *self, PyObject *args) {
     PyObject *points, *cfg, *array;
@@ -289,7 +341,7 @@ static PyObject *f_bind(PyObject *self, PyObject *args) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))f_##name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {{"bind", f_bind, METH_VARARGS, NULL}, FAST(embed), FAST(rmsnorm), FAST(gemm), FAST(gemm_group), FAST(rope_kv), FAST(attn), FAST(swiglu), FAST(argmax),
-                                FAST(rope_kv_q4), FAST(kv_unpack_q4), FAST(attn_q4), FAST(kv_move), FAST(sample), {NULL, NULL, 0, NULL}};
+                                FAST(rope_kv_q4), FAST(kv_unpack_q4), FAST(attn_q4), FAST(kv_move), FAST(sample), FAST(page_plan), FAST(rope_kv_paged), FAST(attn_paged), FAST(verify), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__fastcall(void) {

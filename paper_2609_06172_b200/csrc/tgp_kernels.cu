@@ -2861,7 +2861,8 @@ int tgp_k_wait_test(uint64_t limit_ns, int withhold_step) {
     if (!limit_ns) { limit_ns = 2000000000ull; withhold_step = -1; }
     if (limit_ns < 100000ull || withhold_step < -1) return TGP_E_INVAL;
     int rc = tgpk_gemm_wait_test(limit_ns, withhold_step);
-    return rc ? rc : tgpk_attn_wait_test(limit_ns, withhold_step);
+    if (!rc) rc = tgpk_attn_wait_test(limit_ns, withhold_step);
+    return rc ? rc : tgpk_attn_paged_wait_test(limit_ns, withhold_step);
 }
 
 int tgp_k_status_clear(void) {
@@ -2869,7 +2870,8 @@ int tgp_k_status_clear(void) {
     const unsigned long long z = 0;
     if (cudaMemcpyToSymbol(g_embed_error, &z, sizeof(z)) != cudaSuccess) return TGP_E_CUDA;
     int rc = tgpk_gemm_status_clear();
-    return rc ? rc : tgpk_attn_status_clear();
+    if (!rc) rc = tgpk_attn_status_clear();
+    return rc ? rc : tgpk_attn_paged_status_clear();
 }
 
 int tgp_k_rmsnorm(const float *x_dev, uint32_t ldx, const void *g_dev, void *h_dev, uint32_t M, uint32_t d, float eps, void *stream) {

@@ -98,6 +98,9 @@ int tgp_rope_tables_upload(uint32_t Dh, uint32_t max_len, float base, float *cos
 // reset of the tensor-core kernels' error words (tgp_gemm_sm100.cu, tgp_attn_sm100.cu)
 int tgpk_gemm_status_clear();
 int tgpk_attn_status_clear();
+// the same of the attention over pages (tgp_attn_paged_sm100.cu), and its error word
+int tgpk_attn_paged_status_clear();
+int tgpk_attn_paged_status(int *error_code);
 // name of the kernel the last tgpk_gemm / tgpk_gemm_group / tgpk_gemm_tc call of this thread launched
 extern thread_local const char *tgpk_last_gemm_kernel;
 // set while the caller vouches that this thread's kernel launches are all that is enqueued on their streams (see tgp_k_gemm_chain)
@@ -105,6 +108,7 @@ extern thread_local bool tgpk_chain_ok;
 // test hooks of the tensor-core kernels' bounded waits (see tgp_k_wait_test)
 int tgpk_gemm_wait_test(unsigned long long limit_ns, int withhold_step);
 int tgpk_attn_wait_test(unsigned long long limit_ns, int withhold_step);
+int tgpk_attn_paged_wait_test(unsigned long long limit_ns, int withhold_step);
 // products of M <= 2 rows with the activations computed on the fly: mode 1 the RMSNorm of x (row stride ldx, gain, eps),
 // mode 2 SwiGLU of (g32, u32); bit-identical to the separate kernels followed by tgpk_gemm_group()
 int tgpk_gemm_group_fused(int mode, const float *x, uint32_t ldx, const void *gain, float eps, const float *g32, const float *u32, uint32_t count,
