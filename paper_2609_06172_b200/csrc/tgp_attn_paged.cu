@@ -25,14 +25,17 @@ using namespace tgp_launch;
 typedef __nv_bfloat16 bf16;
 typedef unsigned long long u64;
 
-constexpr uint32_t KEYS = 16, WARPS = 4, STAGES = 3, GROUP = 1024;          // GROUP: sequences of a launch, whose counts lie in shared memory
+constexpr uint32_t KEYS = 16, WARPS = 4, STAGES = 3, GROUP = 512;          // GROUP: sequences of a launch, which lie in shared memory
 constexpr uint32_t MIN_STRETCH = 2 * WARPS;                                  // chunks
+constexpr float LIFT = 16.f;
+constexpr uint32_t ONES = 0x3f803f80u;                                       // two bf16
 // A counter is a number of arrivals only with this in its upper half: a NaN that no arithmetic gives, so whatever else the memory held, partials of an earlier call among
 // it, counts as 0.  The last arrival puts 0 back.
 constexpr u64 COUNTS = 0xffa5c3d1ull << 32;
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, uint32_t src_bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
+__device__ __forceinline__ void cp_async16_or_zeros(uint32_t dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void ldsm_x4(uint32_t addr, uint32_t &r0, uint32_t &r1, uint32_t &r2, uint32_t &r3) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3) : "r"(addr));
@@ -45,31 +48,46 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-// two weights as bf16, and what they are then
-__device__ __forceinline__ uint32_t rounded2(float &a, float &b) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    a = __low2float(h); b = __high2float(h);
-    return *reinterpret_cast<const uint32_t *>(&h);
-}
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t *>(&h); }
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
+
+// How many have arrived at a counter, this one included.  What the CTA has written before its last barrier is seen by who arrives later.
+__device__ __forceinline__ uint32_t arrive(u64 *counter) {
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    u64 was = atomicAdd(counter, 1ull);
+    // Not a number of arrivals yet: the first that replaces it is the first to have arrived.  Others may have added to it meanwhile; they have seen so, too, and arrive here.
+    while ((was & ~0xffffffffull) != COUNTS) {
+        const u64 now = atomicAdd(counter, 0ull);
+        if ((now & ~0xffffffffull) == COUNTS) was = atomicAdd(counter, 1ull);
+        else if (atomicCAS(counter, now, COUNTS + 1) == now) was = COUNTS;
+    }
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    return (uint32_t)was + 1;
+}
 
 template <int DH> __host__ __device__ constexpr uint32_t stage_bytes() { return 2 * KEYS * DH * 2; }
 template <int DH, int MT> __host__ __device__ constexpr uint32_t q_bytes() { return MT > 1 ? MT * 16 * DH * 2 : 0; }
-template <int DH, int MT> __host__ __device__ constexpr uint32_t fixed_smem() { return WARPS * STAGES * stage_bytes<DH>() + q_bytes<DH, MT>() + WARPS * 16 * 2 * 4 + 64; }
+template <int DH, int MT> __host__ __device__ constexpr uint32_t fixed_smem() { return WARPS * STAGES * stage_bytes<DH>() + q_bytes<DH, MT>() + WARPS * 16 * 2 * 4 + 64 + 256; }
 template <int DH, int MT> __host__ __device__ constexpr uint32_t slot_floats() { return MT * 16 * (DH + 2); }
 
-struct FewArgs { TgpPagedAttn a; float *parts; u64 *counters; };
+struct FewArgs {
+    TgpPagedAttn a; float *parts; u64 *counters;
+    uint32_t magic, shift;                                                  // a chunk's page: chunk * magic >> shift (chunks are below 2^27)
+    uint32_t per_token;                                                     // a row's token: row * per_token >> 16 (rows are below 32)
+    __device__ __forceinline__ uint32_t page_of_chunk(uint32_t chunk) const { return (uint32_t)((u64)chunk * magic >> shift); }
+};
 
 template <int DH, int MT>
 __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) tgp_attn_paged_few_kernel(const FewArgs f) {
     pdl_enter();
     const TgpPagedAttn &a = f.a;
-    extern __shared__ __align__(128) uint8_t few_sm[];
+    extern __shared__ __align__(16) uint8_t few_raw[];
+    uint8_t *few_sm = few_raw + (-(uint32_t)__cvta_generic_to_shared(few_raw) & 255u);       // stages begin on 256 bytes
     constexpr uint32_t ROW = DH * 2, CPR = ROW / 16, KV_BYTES = KEYS * ROW, STAGE = stage_bytes<DH>();
     uint8_t *q_sm = few_sm + WARPS * STAGES * STAGE;
     float *ml = reinterpret_cast<float *>(q_sm + q_bytes<DH, MT>());       // [WARPS][16][2]: maxima and sums of the warps' partials
     uint32_t *shared_u = reinterpret_cast<uint32_t *>(ml + WARPS * 16 * 2);
-    uint32_t *upto = shared_u + 16;                                         // [B] chunks of the sequences up to this one, all KV heads
+    uint4 *seqs = reinterpret_cast<uint4 *>(shared_u + 16);                 // [B] first row, rows, length, and chunks of the sequences up to this one, all KV heads
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
 
     // ---- the line of all chunks ----
@@ -78,8 +96,9 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         for (uint32_t i0 = 0; i0 < a.B; i0 += WARPS * 32) {
             const uint32_t i = i0 + tid;
             uint32_t mine = 0;
+            TgpPagedSeq s{0, 0, 0, false};
             if (i < a.B) {
-                const TgpPagedSeq s = tgp_paged_seq(a, a.b0 + i);
+                s = tgp_paged_seq(a, a.b0 + i);
                 if (s.n && !s.idle && s.n * a.G <= a.few) mine = tgp_paged_keys<KEYS>(a, s.end - s.n, s.end - 1).chunks * a.Hkv;
                 else if (s.n && s.idle)                                     // rows of idle sequences are zero
                     for (u64 e = blockIdx.x; e < (u64)s.n * a.Hq * DH / 8; e += gridDim.x) reinterpret_cast<uint4 *>(a.o + (size_t)s.first * a.Hq * DH)[e] = make_uint4(0, 0, 0, 0);
@@ -92,24 +111,25 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             uint32_t all = 0;
 #pragma unroll
             for (uint32_t w = 0; w < WARPS; ++w) { if (w < warp) x += shared_u[w]; all += shared_u[w]; }
-            if (i < a.B) upto[i] = before + x;
+            if (i < a.B) seqs[i] = make_uint4(s.first, s.n, s.end, before + x);
             before += all;
             __syncthreads();
         }
     }
-    const uint32_t N = a.B ? upto[a.B - 1] : 0;
-    const uint32_t ctas = min(gridDim.x, (N + MIN_STRETCH - 1) / MIN_STRETCH);
+    const uint32_t N = seqs[a.B - 1].w, ctas = min(gridDim.x, (N + MIN_STRETCH - 1) / MIN_STRETCH);
     if (blockIdx.x >= ctas) return;
-    auto stretch = [&](uint32_t cta) { return (uint32_t)((u64)N * cta / ctas); };
+    const uint32_t each_cta = N / ctas, longer = N - each_cta * ctas;       // the first `longer` stretches have a chunk more
+    auto stretch = [&](uint32_t cta) { return cta * each_cta + min(cta, longer); };
     const uint32_t line_lo = stretch(blockIdx.x), line_hi = stretch(blockIdx.x + 1);
 
     // an item: a (sequence, KV head) and its place in the line
     struct Item { uint32_t b, hk, lo, hi; TgpPagedSeq s; TgpPagedKeys k; };
     auto enter = [&](Item &it, uint32_t g) {                                // the item of chunk g, whose sequence is it.b or a later one
-        while (upto[it.b] <= g) ++it.b;
-        it.s = tgp_paged_seq(a, a.b0 + it.b);
+        uint4 q = seqs[it.b];
+        while (q.w <= g) q = seqs[++it.b];
+        it.s = TgpPagedSeq{q.x, q.y, q.z, false};
         it.k = tgp_paged_keys<KEYS>(a, it.s.end - it.s.n, it.s.end - 1);
-        const uint32_t seq_lo = upto[it.b] - it.k.chunks * a.Hkv;
+        const uint32_t seq_lo = q.w - it.k.chunks * a.Hkv;
         it.hk = (g - seq_lo) / it.k.chunks;
         it.lo = seq_lo + it.hk * it.k.chunks;
         it.hi = it.lo + it.k.chunks;
@@ -117,63 +137,79 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     Item ahead, now;
     {
         uint32_t lo = 0, hi = a.B - 1;                                      // the first sequence that ends behind line_lo
-        while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (upto[mid] > line_lo) hi = mid; else lo = mid + 1; }
+        while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (seqs[mid].w > line_lo) hi = mid; else lo = mid + 1; }
         ahead.b = lo;
     }
     enter(ahead, line_lo);
     now = ahead;
 
-    // ---- staging: this warp's chunks are line_lo + warp, + WARPS, ... ----
+    // ---- staging: this warp's chunks are line_lo + warp, + WARPS, ...; lane l copies the 16-byte pieces i * 32 + l of a chunk's keys and of its values, piece j of a row to place
+    // j ^ (row & 7).  (What differs between the pieces of a lane is a constant, added or exclusive-ored: every stage begins on 256 bytes.) ----
     const uint32_t stages = (uint32_t)__cvta_generic_to_shared(few_sm) + warp * STAGES * STAGE;
-    uint32_t issued = 0, next = line_lo + warp;                             // chunks asked for, and the next one to ask for
-    auto page_of = [&](const Item &it, uint32_t g) {
-        const uint32_t i = it.k.chunk(g - it.lo) * KEYS / a.P;
-        return i < a.W ? a.table[(size_t)(a.b0 + it.b) * a.W + i] : -1;
-    };
-    int32_t page_next = -1;                                                 // of the next chunk to ask for: the table is read one chunk ahead
-    if (next < line_hi) {
+    constexpr uint32_t RPI = 32 / CPR;                                      // rows that a warp's pieces cover
+    const uint32_t put = (lane / CPR) * ROW + ((lane % CPR ^ lane / CPR) << 4);
+    uint32_t next = line_lo + warp;                                         // the next chunk to ask for
+    // The table's entries of the warp's next 32 chunks of an item are read together, a lane each, a chunk ahead of the first one's copy.
+    int32_t pages = -1;
+    uint32_t pages_at = 0;                                                  // chunk of lane 0's
+    auto read_pages = [&]() {
+        if (next >= line_hi) return;
         if (next >= ahead.hi) enter(ahead, next);
-        page_next = page_of(ahead, next);
-    }
+        else if (next - pages_at < 32 * WARPS) return;
+        pages_at = next;
+        const uint32_t g = next + lane * WARPS, i = f.page_of_chunk(ahead.k.chunk(g - ahead.lo));
+        pages = g < ahead.hi && i < a.W ? a.table[(size_t)(a.b0 + ahead.b) * a.W + i] : -1;
+    };
+    pages_at = next - 32 * WARPS;
+    read_pages();
     uint32_t present = 0;                                                   // a bit per stage: its page is one of the cache's
-    auto issue = [&]() {
+    auto issue = [&](uint32_t stage) {
         if (next < line_hi) {
-            const uint32_t key0 = ahead.k.chunk(next - ahead.lo) * KEYS, stage = issued % STAGES;
-            const bool there = (uint32_t)page_next < a.n_pages;
+            const uint32_t chunk = ahead.k.chunk(next - ahead.lo), key0 = chunk * KEYS;
+            const int32_t page = __shfl_sync(0xffffffffu, pages, (next - pages_at) / WARPS);
+            const bool there = (uint32_t)page < a.n_pages;
             present = there ? present | 1u << stage : present & ~(1u << stage);
-            const size_t at = (((size_t)(there ? page_next : 0) * a.Hkv + ahead.hk) * a.P + key0 % a.P) * ROW;
-            const uint8_t *kg = reinterpret_cast<const uint8_t *>(a.k) + at, *vg = reinterpret_cast<const uint8_t *>(a.v) + at;
-            const uint32_t base = stages + stage * STAGE;
+            if (there) {
+                const size_t at = (((size_t)page * a.Hkv + ahead.hk) * a.P + (key0 - f.page_of_chunk(chunk) * a.P)) * ROW + lane * 16;
+                const uint8_t *kg = reinterpret_cast<const uint8_t *>(a.k) + at, *vg = reinterpret_cast<const uint8_t *>(a.v) + at;
+                const uint32_t base = stages + stage * STAGE + put;
+                if (key0 + KEYS <= ahead.s.end && (key0 >= ahead.k.low || key0 + KEYS <= a.sinks)) {
 #pragma unroll
-            for (uint32_t i = 0; i < KEYS * CPR / 32; ++i) {
-                const uint32_t idx = i * 32 + lane, row = idx / CPR, j = idx % CPR, key = key0 + row;
-                const uint32_t dst = row * ROW + ((j ^ (row & 7)) << 4);
-                // keys that no row sees are zeros, not read
-                const uint32_t bytes = there && key < ahead.s.end && (key >= ahead.k.low || key < a.sinks) ? 16u : 0u;
-                cp_async16(base + dst, kg + (size_t)row * ROW + j * 16, bytes);
-                cp_async16(base + KV_BYTES + dst, vg + (size_t)row * ROW + j * 16, bytes);
+                    for (uint32_t i = 0; i < KEYS * CPR / 32; ++i) {
+                        const uint32_t dst = (base ^ (i * RPI % 8) << 4) + i * 512;
+                        cp_async16(dst, kg + i * 512);
+                        cp_async16(dst + KV_BYTES, vg + i * 512);
+                    }
+                } else {                                                    // keys that no row sees are zeros, not read
+#pragma unroll
+                    for (uint32_t i = 0; i < KEYS * CPR / 32; ++i) {
+                        const uint32_t key = key0 + i * RPI + lane / CPR, dst = (base ^ (i * RPI % 8) << 4) + i * 512;
+                        const uint32_t bytes = key < ahead.s.end && (key >= ahead.k.low || key < a.sinks) ? 16u : 0u;
+                        cp_async16_or_zeros(dst, kg + i * 512, bytes);
+                        cp_async16_or_zeros(dst + KV_BYTES, vg + i * 512, bytes);
+                    }
+                }
             }
-            ++issued;
             next += WARPS;
-            if (next < line_hi) {
-                if (next >= ahead.hi) enter(ahead, next);
-                page_next = page_of(ahead, next);
-            }
+            read_pages();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
 #pragma unroll
-    for (uint32_t s = 0; s < STAGES - 1; ++s) issue();
+    for (uint32_t s = 0; s < STAGES - 1; ++s) issue(s);
 
-    uint32_t done = 0;                                                      // chunks this warp has been through
+    // what a lane reads of a stage with ldmatrix, up to constants: of the keys as they lie, of the values transposed
+    const uint32_t k_get = (lane & 7) * ROW + ((lane >> 3 ^ (lane & 7)) << 4), v_get = KV_BYTES + ((lane >> 3 & 1) * 8 + (lane & 7)) * ROW + ((lane >> 4 ^ (lane & 7)) << 4);
+    const uint32_t q_get = (uint32_t)__cvta_generic_to_shared(q_sm) + (lane & 15) * ROW + ((lane >> 4 ^ (lane & 7)) << 4);
+    uint32_t done = 0, stage = 0;                                           // chunks this warp has been through; the stage of the next one
     for (uint32_t seg_lo = line_lo; seg_lo < line_hi;) {                    // the CTA's part of an item
         if (seg_lo >= now.hi) enter(now, seg_lo);
         const uint32_t seg_hi = min(line_hi, now.hi), rows = now.s.n * a.G, first_pos = now.s.end - now.s.n;
         const bf16 *q_item = a.q + ((size_t)now.s.first * a.Hq + now.hk * a.G) * DH;
-        auto q_row = [&](uint32_t row) { const uint32_t t = row / a.G; return q_item + ((size_t)t * a.Hq + (row - t * a.G)) * DH; };
+        auto token_of = [&](uint32_t row) { return row * f.per_token >> 16; };
+        auto q_row = [&](uint32_t row) { const uint32_t t = token_of(row); return q_item + ((size_t)t * a.Hq + (row - t * a.G)) * DH; };
         // ---- Q: in registers (one tile), or in shared memory, rows as wide as the keys' ----
         uint32_t qf[MT == 1 ? DH / 16 : 1][4];
-        const uint32_t q_u = (uint32_t)__cvta_generic_to_shared(q_sm);
         if constexpr (MT == 1) {
             const bf16 *q0 = q_row(min(r, rows - 1)) + 2 * c, *q1 = q_row(min(r + 8, rows - 1)) + 2 * c;
 #pragma unroll
@@ -191,28 +227,24 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             }
             __syncthreads();
         }
-        float o[MT][DH / 8][4], m[MT][2], l[MT][2];
+        // The reference m of a row's exponents follows its maximum where that is more than 2^LIFT above it: weights and sums are floating point, and are as exact anywhere.  So a chunk
+        // asks one question of all rows, and O is hardly ever multiplied.  (It starts from the least number, not from -inf: scores of -inf weigh nothing then, in whichever chunk they are met.)
+        float o[MT][DH / 8][4], m[MT][2], l[MT][4];                         // l: the sums of the rounded weights, of rows r (0) and r + 8 (2), by a product with ones
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            // (from the least number, not from -inf: scores of -inf weigh nothing then, in whichever chunk they are met)
             m[t][0] = m[t][1] = -FLT_MAX;
-            l[t][0] = l[t][1] = 0.f;
+            l[t][0] = l[t][1] = l[t][2] = l[t][3] = 0.f;
 #pragma unroll
             for (int j = 0; j < DH / 8; ++j) o[t][j][0] = o[t][j][1] = o[t][j][2] = o[t][j][3] = 0.f;
         }
-        uint32_t pos[MT][2];                                                // positions of this lane's rows (of the tile's last row where there is none)
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) pos[t][e] = first_pos + min(t * 16 + r + 8 * e, rows - 1) / a.G;
+        auto pos_of = [&](int t, int e) { return first_pos + token_of(min(t * 16 + r + 8 * e, rows - 1)); };      // of this lane's rows (of the last row where there is none)
 
-        for (uint32_t g = line_lo + warp + done * WARPS; g < seg_hi; g += WARPS, ++done) {
-            issue();
+        for (uint32_t g = line_lo + warp + done * WARPS; g < seg_hi; g += WARPS, ++done, stage = stage + 1 == STAGES ? 0 : stage + 1) {
+            issue(stage == 0 ? STAGES - 1 : stage - 1);
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
             __syncwarp();
-            const uint32_t stage = done % STAGES, key0 = now.k.chunk(g - now.lo) * KEYS;
-            const uint32_t kb = stages + stage * STAGE, vb = kb + KV_BYTES;
             if (!(present >> stage & 1)) continue;                          // (the stage is refilled behind the next chunk's barrier)
+            const uint32_t key0 = now.k.chunk(g - now.lo) * KEYS, at = stages + stage * STAGE;
             // whole: every row sees every key
             const bool whole = key0 + KEYS - 1 <= first_pos && (!a.window || now.s.end - 1 - key0 < a.window || key0 + KEYS <= a.sinks);
             // ---- S = Q K^T ----
@@ -225,79 +257,78 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             for (int kp = 0; kp < DH / 32; ++kp) {
                 uint32_t b[2][4];
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    const uint32_t row = nt * 8 + (lane & 7), j = kp * 4 + (lane >> 3);
-                    ldsm_x4(kb + row * ROW + ((j ^ (row & 7)) << 4), b[nt][0], b[nt][1], b[nt][2], b[nt][3]);
-                }
+                for (int nt = 0; nt < 2; ++nt) ldsm_x4((at + k_get ^ kp << 6) + nt * 8 * ROW, b[nt][0], b[nt][1], b[nt][2], b[nt][3]);
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         uint32_t x0, x1, x2, x3;
                         if constexpr (MT == 1) { x0 = qf[2 * kp + e][0]; x1 = qf[2 * kp + e][1]; x2 = qf[2 * kp + e][2]; x3 = qf[2 * kp + e][3]; }
-                        else {
-                            const uint32_t row = t * 16 + (lane & 15), j = (2 * kp + e) * 2 + (lane >> 4);
-                            ldsm_x4(q_u + row * ROW + ((j ^ (row & 7)) << 4), x0, x1, x2, x3);
-                        }
+                        else ldsm_x4((q_get ^ (2 * kp + e) << 5) + t * 16 * ROW, x0, x1, x2, x3);
 #pragma unroll
                         for (int nt = 0; nt < 2; ++nt) mma_bf16(s[t][nt], x0, x1, x2, x3, b[nt][2 * e], b[nt][2 * e + 1]);
                     }
             }
             // ---- weights: this lane's keys are 2c, 2c + 1, 8 + 2c, 9 + 2c of rows r and r + 8 ----
-            uint32_t pa[MT][4];
-            float grow[MT][2];
-            bool grows = false;
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float &x = s[t][nt][2 * e + i];
-                            x *= a.sl2;
-                            if (!whole && !tgp_paged_sees(a, pos[t][e], key0 + nt * 8 + 2 * c + i)) x = -INFINITY;
-                            top = fmaxf(top, x);
-                        }
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    grow[t][e] = fmaxf(m[t][e], top);
-                    grows |= grow[t][e] > m[t][e];
-                }
-            }
-            if (__any_sync(0xffffffffu, grows)) {
+            if (!whole) {
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        const float alpha = ex2(m[t][e] - grow[t][e]);       // (the first time: of zeros)
-                        m[t][e] = grow[t][e];
-                        l[t][e] *= alpha;
+                        const uint32_t pos = pos_of(t, e);
 #pragma unroll
-                        for (int j = 0; j < DH / 8; ++j) { o[t][j][2 * e] *= alpha; o[t][j][2 * e + 1] *= alpha; }
+                        for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) if (!tgp_paged_sees(a, pos, key0 + nt * 8 + 2 * c + i)) s[t][nt][2 * e + i] = -INFINITY;
                     }
             }
+            float x[MT][2][4], top = -INFINITY;
+            auto exponents = [&]() {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[t][nt][i] = fmaf(s[t][nt][i], a.sl2, -m[t][i >> 1]);
+            };
+            exponents();
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt)
+                for (int nt = 0; nt < 2; ++nt) top = fmaxf(top, fmaxf(fmaxf(x[t][nt][0], x[t][nt][1]), fmaxf(x[t][nt][2], x[t][nt][3])));
+            if (__any_sync(0xffffffffu, top > LIFT)) {
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
-                        float &x = s[t][nt][2 * e], &y = s[t][nt][2 * e + 1];
-                        x = ex2(x - m[t][e]);
-                        y = ex2(y - m[t][e]);
-                        pa[t][2 * nt + e] = rounded2(x, y);
-                        l[t][e] += x + y;                                   // (of this lane's keys: the four lanes of a row meet at the end)
+                        float best = fmaxf(fmaxf(s[t][0][2 * e], s[t][0][2 * e + 1]), fmaxf(s[t][1][2 * e], s[t][1][2 * e + 1]));
+                        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+                        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2)) * a.sl2;
+                        if (!(best > m[t][e])) best = m[t][e];
+                        const float alpha = ex2(m[t][e] - best);             // (the first time: of zeros)
+                        m[t][e] = best;
+                        l[t][2 * e] *= alpha;
+#pragma unroll
+                        for (int j = 0; j < DH / 8; ++j) { o[t][j][2 * e] *= alpha; o[t][j][2 * e + 1] *= alpha; }
                     }
+                exponents();
+            }
+            uint32_t pa[MT][4];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) pa[t][2 * nt + e] = bf16x2(ex2(x[t][nt][2 * e]), ex2(x[t][nt][2 * e + 1]));
+                mma_bf16(l[t], pa[t][0], pa[t][1], pa[t][2], pa[t][3], ONES, ONES);
+            }
             // ---- O += P V ----
             // Where some rows see a key and others do not, a value that is no number must not reach the others as 0 x inf: then each row adds up what it sees.
             bool each = false;
             if (!whole && now.s.n > 1) {
                 for (uint32_t i = lane; i < KEYS * CPR; i += 32) {
                     uint32_t w0, w1, w2, w3;
-                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3) : "r"(vb + i * 16));
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w0), "=r"(w1), "=r"(w2), "=r"(w3) : "r"(at + KV_BYTES + i * 16));
                     each |= not_finite2(w0) || not_finite2(w1) || not_finite2(w2) || not_finite2(w3);
                 }
                 each = __any_sync(0xffffffffu, each);
@@ -305,9 +336,8 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             if (!each) {
 #pragma unroll
                 for (int jp = 0; jp < DH / 16; ++jp) {
-                    const uint32_t row = ((lane >> 3) & 1) * 8 + (lane & 7), j = 2 * jp + (lane >> 4);
                     uint32_t v0, v1, v2, v3;
-                    ldsm_x4_t(vb + row * ROW + ((j ^ (row & 7)) << 4), v0, v1, v2, v3);
+                    ldsm_x4_t(at + v_get ^ jp << 5, v0, v1, v2, v3);
 #pragma unroll
                     for (int t = 0; t < MT; ++t) {
                         mma_bf16(o[t][2 * jp], pa[t][0], pa[t][1], pa[t][2], pa[t][3], v0, v1);
@@ -322,16 +352,14 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
                     for (int t = 0; t < MT; ++t)
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
-                            const float w0 = __shfl_sync(0xffffffffu, key < 8 ? s[t][0][2 * e] : s[t][1][2 * e], from), w1 = __shfl_sync(0xffffffffu, key < 8 ? s[t][0][2 * e + 1] : s[t][1][2 * e + 1], from);
-                            const float w = key & 1 ? w1 : w0;
-                            if (!tgp_paged_sees(a, pos[t][e], key0 + key)) continue;
+                            const uint32_t two = __shfl_sync(0xffffffffu, key < 8 ? pa[t][e] : pa[t][2 + e], from);
+                            const float w = __uint_as_float(key & 1 ? two & 0xffff0000u : two << 16);
+                            const bool sees = tgp_paged_sees(a, pos_of(t, e), key0 + key);
 #pragma unroll
                             for (int j = 0; j < DH / 8; ++j) {
                                 uint32_t v;
-                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(vb + key * ROW + ((j ^ (key & 7)) << 4) + 4 * c));
-                                const __nv_bfloat162 h = *reinterpret_cast<const __nv_bfloat162 *>(&v);
-                                o[t][j][2 * e] += w * __low2float(h);
-                                o[t][j][2 * e + 1] += w * __high2float(h);
+                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at + KV_BYTES + key * ROW + ((j ^ (key & 7)) << 4) + 4 * c));
+                                if (sees) { o[t][j][2 * e] += w * __uint_as_float(v << 16); o[t][j][2 * e + 1] += w * __uint_as_float(v & 0xffff0000u); }
                             }
                         }
                 }
@@ -341,25 +369,24 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         // ---- the four warps' partials: outputs go to the stage that each has free (the two behind it are under way), one tile at a time ----
         const bool complete = seg_lo == now.lo && seg_hi == now.hi;
         float *slot = f.parts + ((size_t)blockIdx.x * 2 + (seg_lo == line_lo ? 0 : 1)) * slot_floats<DH, MT>();
-        float *mine = reinterpret_cast<float *>(few_sm + (size_t)(warp * STAGES + (done + STAGES - 1) % STAGES) * STAGE);
-        auto finish = [&](uint32_t row, uint32_t d, float2 v, float sum) {  // (a row that sees nothing is zero; a NaN stays one)
-            const uint32_t t = row / a.G;
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const __nv_bfloat162 h = sum == 0.f ? __floats2bfloat162_rn(0.f, 0.f) : __floats2bfloat162_rn(v.x * inv, v.y * inv);
-            *reinterpret_cast<__nv_bfloat162 *>(a.o + ((size_t)(now.s.first + t) * a.Hq + now.hk * a.G + (row - t * a.G)) * DH + d) = h;
+        float *mine = reinterpret_cast<float *>(few_sm + (size_t)(warp * STAGES + (stage == 0 ? STAGES - 1 : stage - 1)) * STAGE);
+        auto finish = [&](uint32_t row, uint32_t d, float4 v, float sum) {  // (a row that sees nothing is zero; a NaN stays one)
+            const uint32_t t = token_of(row);
+            const float inv = 1.f / sum;
+            uint2 two = make_uint2(bf16x2(v.x * inv, v.y * inv), bf16x2(v.z * inv, v.w * inv));
+            if (sum == 0.f) two = make_uint2(0u, 0u);
+            *reinterpret_cast<uint2 *>(a.o + ((size_t)(now.s.first + t) * a.Hq + now.hk * a.G + (row - t * a.G)) * DH + d) = two;
         };
+        auto add = [](float4 &v, float w, const float4 &x) { v.x += w * x.x; v.y += w * x.y; v.z += w * x.z; v.w += w * x.w; };
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             if (t && t * 16 >= rows) break;
             __syncwarp();
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float sum = l[t][e];
-                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
                 const uint32_t row = r + 8 * e;
                 if (t * 16 + row < rows) {
-                    if (c == 0) { ml[(warp * 16 + row) * 2] = m[t][e]; ml[(warp * 16 + row) * 2 + 1] = sum; }
+                    if (c == 0) { ml[(warp * 16 + row) * 2] = m[t][e]; ml[(warp * 16 + row) * 2 + 1] = l[t][2 * e]; }
 #pragma unroll
                     for (int j = 0; j < DH / 8; ++j) *reinterpret_cast<float2 *>(mine + row * DH + ((j * 8 + 2 * c) ^ (row & 7) * 8)) = make_float2(o[t][j][2 * e], o[t][j][2 * e + 1]);
                 }
@@ -368,24 +395,26 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             if (lane == 0) shared_u[warp] = (uint32_t)(reinterpret_cast<uint8_t *>(mine) - few_sm);
             __syncthreads();
             const uint32_t tile_rows = min(16u, rows - t * 16);
-            for (uint32_t i = tid; i < tile_rows * DH / 2; i += WARPS * 32) {
-                const uint32_t row = i / (DH / 2), d = i % (DH / 2) * 2;
-                float M = -FLT_MAX, sum = 0.f;
-                float2 v = make_float2(0.f, 0.f);
+            const float *theirs[WARPS];
 #pragma unroll
-                for (uint32_t w = 0; w < WARPS; ++w) M = fmaxf(M, ml[(w * 16 + row) * 2]);
+            for (uint32_t w = 0; w < WARPS; ++w) theirs[w] = reinterpret_cast<const float *>(few_sm + shared_u[w]);
+            for (uint32_t i = tid; i < tile_rows * DH / 4; i += WARPS * 32) {
+                const uint32_t row = i / (DH / 4), d = i % (DH / 4) * 4;
+                float2 x[WARPS];
+                float M = -FLT_MAX, sum = 0.f;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (uint32_t w = 0; w < WARPS; ++w) { x[w] = *reinterpret_cast<const float2 *>(ml + (w * 16 + row) * 2); M = fmaxf(M, x[w].x); }
 #pragma unroll
                 for (uint32_t w = 0; w < WARPS; ++w) {
-                    const float2 x = *reinterpret_cast<const float2 *>(reinterpret_cast<const float *>(few_sm + shared_u[w]) + row * DH + (d ^ (row & 7) * 8));
-                    const float wgt = ex2(ml[(w * 16 + row) * 2] - M);      // (a warp without a chunk: any weight of zeros)
-                    sum += wgt * ml[(w * 16 + row) * 2 + 1];
-                    v.x += wgt * x.x; v.y += wgt * x.y;
+                    const float wgt = ex2(x[w].x - M);                      // (a warp without a chunk: any weight of zeros)
+                    sum += wgt * x[w].y;
+                    add(v, wgt, *reinterpret_cast<const float4 *>(theirs[w] + row * DH + (d ^ (row & 7) * 8)));
                 }
                 if (complete) finish(t * 16 + row, d, v, sum);
                 else {
-                    float *to = slot + (size_t)(t * 16 + row) * (DH + 2);
-                    if (d == 0) { to[0] = M; to[1] = sum; }
-                    *reinterpret_cast<float2 *>(to + 2 + d) = v;
+                    if (d == 0) *reinterpret_cast<float2 *>(slot + MT * 16 * DH + (t * 16 + row) * 2) = make_float2(M, sum);
+                    *reinterpret_cast<float4 *>(slot + (t * 16 + row) * DH + d) = v;
                 }
             }
             __syncthreads();
@@ -394,43 +423,54 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         if (!complete) {
             const uint32_t item = (a.b0 + now.b) * a.Hkv + now.hk;
             // CTAs of the item's first and last chunk
-            auto cta_of = [&](uint32_t g) {
-                uint32_t x = (uint32_t)(((u64)g * ctas) / N);
-                while (x + 1 < ctas && stretch(x + 1) <= g) ++x;
-                while (stretch(x) > g) --x;
-                return x;
-            };
+            auto cta_of = [&](uint32_t g) { return g < longer * (each_cta + 1) ? g / (each_cta + 1) : longer + (g - longer * (each_cta + 1)) / each_cta; };
             const uint32_t c0 = cta_of(now.lo), c1 = cta_of(now.hi - 1), parts = c1 - c0 + 1;
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                u64 *counter = f.counters + item, old = *(volatile u64 *)counter, seen, to;
-                do {
-                    seen = old;
-                    to = (seen & 0xffffffff00000000ull) == COUNTS ? seen + 1 : COUNTS + 1;
-                    if ((uint32_t)to == parts) to = COUNTS;
-                    old = atomicCAS(counter, seen, to);
-                } while (old != seen);
-                shared_u[8] = to == COUNTS;
-                __threadfence();
-            }
+            if (tid == 0) shared_u[8] = arrive(f.counters + item) == parts;
             __syncthreads();
             if (shared_u[8]) {
-                for (uint32_t i = tid; i < rows * DH / 2; i += WARPS * 32) {
-                    const uint32_t row = i / (DH / 2), d = i % (DH / 2) * 2;
-                    float M = -FLT_MAX, sum = 0.f;
-                    float2 v = make_float2(0.f, 0.f);
-                    for (uint32_t p = 0; p < parts; ++p) {
-                        const uint32_t cta = c0 + p;
-                        const float *from = f.parts + ((size_t)cta * 2 + (stretch(cta) >= now.lo ? 0 : 1)) * slot_floats<DH, MT>() + (size_t)row * (DH + 2);
-                        const float pm = __ldcg(from), pl = __ldcg(from + 1);
-                        const float2 x = __ldcg(reinterpret_cast<const float2 *>(from + 2 + d));
-                        const float M2 = fmaxf(M, pm), w_old = ex2(M - M2), w_new = ex2(pm - M2);
-                        M = M2;
-                        sum = sum * w_old + pl * w_new;
-                        v.x = v.x * w_old + x.x * w_new; v.y = v.y * w_old + x.y * w_new;
+                if (tid == 0) f.counters[item] = COUNTS;
+                // a partial: [rows][DH] outputs, [rows][2] maxima and sums
+                auto part = [&](uint32_t p) { const uint32_t cta = c0 + p; return f.parts + ((size_t)cta * 2 + (stretch(cta) >= now.lo ? 0 : 1)) * slot_floats<DH, MT>(); };
+                auto ml_of = [&](const float *from, uint32_t row) { return __ldcg(reinterpret_cast<const float2 *>(from + MT * 16 * DH + row * 2)); };
+                auto four_of = [&](const float *from, uint32_t row, uint32_t d) { return __ldcg(reinterpret_cast<const float4 *>(from + row * DH + d)); };
+                constexpr uint32_t SOME = 4, ROWS = DH == 128 ? 3 : 1;     // partials, and pieces of four dimensions, that a thread asks for at a time
+                for (uint32_t i0 = tid; i0 < rows * DH / 4; i0 += WARPS * 32 * ROWS) {
+                    float M[ROWS], sum[ROWS];
+                    float4 v[ROWS];
+#pragma unroll
+                    for (uint32_t k = 0; k < ROWS; ++k) { M[k] = -FLT_MAX; sum[k] = 0.f; v[k] = make_float4(0.f, 0.f, 0.f, 0.f); }
+                    for (uint32_t p0 = 0; p0 < parts; p0 += SOME) {
+                        float2 y[ROWS][SOME];
+                        float4 x[ROWS][SOME];
+#pragma unroll
+                        for (uint32_t p = 0; p < SOME; ++p) {
+                            const float *from = part(min(p0 + p, parts - 1));
+#pragma unroll
+                            for (uint32_t k = 0; k < ROWS; ++k) {
+                                const uint32_t i = i0 + k * WARPS * 32, row = i / (DH / 4), d = i % (DH / 4) * 4;
+                                y[k][p] = make_float2(-FLT_MAX, 0.f);
+                                x[k][p] = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (p0 + p < parts && row < rows) { y[k][p] = ml_of(from, row); x[k][p] = four_of(from, row, d); }
+                            }
+                        }
+#pragma unroll
+                        for (uint32_t k = 0; k < ROWS; ++k) {
+                            float best = M[k];
+#pragma unroll
+                            for (uint32_t p = 0; p < SOME; ++p) best = fmaxf(best, y[k][p].x);
+                            const float old = ex2(M[k] - best);
+                            M[k] = best;
+                            sum[k] *= old;
+                            v[k].x *= old; v[k].y *= old; v[k].z *= old; v[k].w *= old;
+#pragma unroll
+                            for (uint32_t p = 0; p < SOME; ++p) { const float w = ex2(y[k][p].x - best); sum[k] += w * y[k][p].y; add(v[k], w, x[k][p]); }
+                        }
                     }
-                    finish(row, d, v, sum);
+#pragma unroll
+                    for (uint32_t k = 0; k < ROWS; ++k) {
+                        const uint32_t i = i0 + k * WARPS * 32, row = i / (DH / 4);
+                        if (row < rows) finish(row, i % (DH / 4) * 4, v[k], sum[k]);
+                    }
                 }
             }
             __syncthreads();
@@ -445,12 +485,12 @@ template <int DH, int MT> uint32_t few_ctas() { return (uint32_t)tgpk_sms() * (D
 
 template <int DH, int MT>
 int launch_few(FewArgs f, cudaStream_t st) {
-    if (!tgpk_allow_smem<tgp_attn_paged_few_kernel<DH, MT>>(fixed_smem<DH, MT>() + GROUP * 4, true)) return TGP_E_CUDA;
+    if (!tgpk_allow_smem<tgp_attn_paged_few_kernel<DH, MT>>(fixed_smem<DH, MT>() + GROUP * 16, true)) return TGP_E_CUDA;
     const uint32_t B = f.a.B;
     for (uint32_t b0 = 0; b0 < B; b0 += GROUP) {
         f.a.b0 = b0;
         f.a.B = std::min(GROUP, B - b0);
-        if (int rc = launch(tgp_attn_paged_few_kernel<DH, MT>, dim3(few_ctas<DH, MT>()), dim3(WARPS * 32), fixed_smem<DH, MT>() + f.a.B * 4, st, 1, f)) return rc;
+        if (int rc = launch(tgp_attn_paged_few_kernel<DH, MT>, dim3(few_ctas<DH, MT>()), dim3(WARPS * 32), fixed_smem<DH, MT>() + f.a.B * 16, st, 1, f)) return rc;
     }
     return TGP_OK;
 }
@@ -487,6 +527,13 @@ extern "C" int tgp_k_attn_paged(const void *qb, const void *k_pages, const void 
     FewArgs f{};
     f.a = TgpPagedAttn{(const bf16 *)qb, (const bf16 *)k_pages, (const bf16 *)v_pages, (bf16 *)ob, table_dev, start_dev, end_dev, cfg->Hq, cfg->Hkv, G, cfg->TK,
                        cfg->max_len / cfg->TK + (cfg->max_len % cfg->TK != 0), B, T, q_max, kv_max, n_pages, window, window ? sinks : 0, 0, 1.4426950408889634f / sqrtf((float)cfg->Dh), 0};
+    // with s bits for the chunks of a page, ceil(2^(27 + s) / chunks) is off by less than 2^s / 2^(27 + s) of what it multiplies
+    const uint32_t chunks = cfg->TK / KEYS;
+    uint32_t s = 0;
+    while ((1u << s) < chunks) ++s;
+    f.shift = 27 + s;
+    f.magic = (uint32_t)(((1ull << f.shift) + chunks - 1) / chunks);
+    f.per_token = (65536 + G - 1) / G;
     f.counters = (u64 *)scratch_dev;
     f.parts = (float *)((uint8_t *)scratch_dev + counter_bytes(cfg, B));
     // one tile of 16 rows where all sequences fit it, else two; sequences of more rows are the other kernel's
