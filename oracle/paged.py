@@ -74,7 +74,7 @@ def softmax(x, t):
         return np.zeros(len(x))
     top = x[real].max()
     with np.errstate(invalid="ignore", over="ignore"):
-        w = np.where(~real, 0.0, np.where(x == top, 1.0, np.exp((x - top) / t)))
+        w = np.where(~real, 0.0, np.where(x == top, 1.0, np.exp((x - top) / t) if top < np.inf else 0.0))
     return w / w.sum()
 
 

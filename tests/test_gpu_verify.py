@@ -113,7 +113,7 @@ def test_logits_that_are_infinite_or_no_numbers():
     x[16:20, [5, 99, 100]] = np.inf
     y[20:24, 50] = np.inf
     x[24:28] = 3e38 * np.sign(x[24:28])
-    for t in (None, np.full(9, 0.3), np.full(9, 1e-30), np.full(9, 1e30), np.zeros(9)):
+    for t in (None, np.full(9, 0.3), np.full(9, 1e-30), np.full(9, 1e30), np.full(9, np.inf), np.zeros(9)):
         for u in (0.01, 0.5):
             check(x, y, tokens, n, np.full(36, u), rng.random(9), t)
             check(x, None, tokens, n, np.full(36, u), rng.random(9), t)
@@ -152,14 +152,18 @@ def test_rows_that_do_not_lie_in_the_arrays():
     x, y, tokens = drafts(rng, [3, 3, 3], 700)
     u, v = rng.random(9), rng.random(3)
     good, n_good = run(x, y, tokens, [0, 3, 6, 9], u, v)
-    for start, lost in (([-1, 3, 6, 9], [0]), ([0, 3, 6, 10], [2]), ([0, 3, 3, 3], [1, 2]), ([0, 3, 6, 2], [2])):
+    for start, lost in (([-1, 3, 6, 9], [0]), ([0, 3, 6, 10], [2]), ([0, 3, 3, 3], [1, 2]), ([0, 3, 6, 2], [2]), ([0, 2 ** 31 - 1, 3, 6], [0, 1])):
         out, n_out = run(x, y, tokens, start, u, v)
         for b in range(3):
             rows = slice(3 * b, 3 * b + 3)
             if b in lost:
-                assert n_out[b] == 0 and (out[rows] == -7).all()
+                assert n_out[b] == 0
+            elif start[1] == 2 ** 31 - 1:                  # the third sequence has the rows of the second
+                assert n_out[b] >= 1 and out[3] >= 0 and (out[:3] == -7).all() and (out[6:] == -7).all()
             else:
                 assert n_out[b] == n_good[b] and np.array_equal(out[rows], good[rows])
+        if start[1] != 2 ** 31 - 1:
+            assert all((out[3 * b:3 * b + 3] == -7).all() for b in lost)
 
 
 def test_a_captured_call():
