@@ -29,10 +29,6 @@ constexpr uint32_t KEYS = 16, WARPS = 4, STAGES = 3, GROUP = 512;          // GR
 constexpr uint32_t MIN_STRETCH = 2 * WARPS;                                  // chunks
 constexpr float LIFT = 16.f;
 constexpr uint32_t ONES = 0x3f803f80u;                                       // two bf16
-// A counter is a number of arrivals only with this in its upper half: a NaN that no arithmetic gives, so whatever else the memory held, partials of an earlier call among
-// it, counts as 0.  The last arrival puts 0 back.
-constexpr u64 COUNTS = 0xffa5c3d1ull << 32;
-
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void cp_async16_or_zeros(uint32_t dst, const void *src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -51,27 +47,13 @@ __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32
 __device__ __forceinline__ uint32_t bf16x2(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); return *reinterpret_cast<const uint32_t *>(&h); }
 __device__ __forceinline__ bool not_finite2(uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; }
 
-// How many have arrived at a counter, this one included.  What the CTA has written before its last barrier is seen by who arrives later.
-__device__ __forceinline__ uint32_t arrive(u64 *counter) {
-    asm volatile("fence.acq_rel.gpu;" ::: "memory");
-    u64 was = atomicAdd(counter, 1ull);
-    // Not a number of arrivals yet: the first that replaces it is the first to have arrived.  Others may have added to it meanwhile; they have seen so, too, and arrive here.
-    while ((was & ~0xffffffffull) != COUNTS) {
-        const u64 now = atomicAdd(counter, 0ull);
-        if ((now & ~0xffffffffull) == COUNTS) was = atomicAdd(counter, 1ull);
-        else if (atomicCAS(counter, now, COUNTS + 1) == now) was = COUNTS;
-    }
-    asm volatile("fence.acq_rel.gpu;" ::: "memory");
-    return (uint32_t)was + 1;
-}
-
 template <int DH> __host__ __device__ constexpr uint32_t stage_bytes() { return 2 * KEYS * DH * 2; }
 template <int DH, int MT> __host__ __device__ constexpr uint32_t q_bytes() { return MT > 1 ? MT * 16 * DH * 2 : 0; }
 template <int DH, int MT> __host__ __device__ constexpr uint32_t fixed_smem() { return WARPS * STAGES * stage_bytes<DH>() + q_bytes<DH, MT>() + WARPS * 16 * 2 * 4 + 64 + 256; }
 template <int DH, int MT> __host__ __device__ constexpr uint32_t slot_floats() { return MT * 16 * (DH + 2); }
 
 struct FewArgs {
-    TgpPagedAttn a; float *parts; u64 *counters;
+    TgpPagedAttn a; float *parts; u64 *counters; uint32_t *tiles;           // tiles: the other kernel's counter, which begins at 0
     uint32_t magic, shift;                                                  // a chunk's page: chunk * magic >> shift (chunks are below 2^27)
     uint32_t per_token;                                                     // a row's token: row * per_token >> 16 (rows are below 32)
     __device__ __forceinline__ uint32_t page_of_chunk(uint32_t chunk) const { return (uint32_t)((u64)chunk * magic >> shift); }
@@ -90,6 +72,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     uint4 *seqs = reinterpret_cast<uint4 *>(shared_u + 16);                 // [B] first row, rows, length, and chunks of the sequences up to this one, all KV heads
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
 
+    if (blockIdx.x == 0 && tid == 0) *f.tiles = 0;
     // ---- the line of all chunks ----
     {
         uint32_t before = 0;
@@ -425,10 +408,10 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             // CTAs of the item's first and last chunk
             auto cta_of = [&](uint32_t g) { return g < longer * (each_cta + 1) ? g / (each_cta + 1) : longer + (g - longer * (each_cta + 1)) / each_cta; };
             const uint32_t c0 = cta_of(now.lo), c1 = cta_of(now.hi - 1), parts = c1 - c0 + 1;
-            if (tid == 0) shared_u[8] = arrive(f.counters + item) == parts;
+            if (tid == 0) shared_u[8] = tgp_paged_arrive(f.counters + item) == parts;
             __syncthreads();
             if (shared_u[8]) {
-                if (tid == 0) f.counters[item] = COUNTS;
+                if (tid == 0) f.counters[item] = TGP_PAGED_COUNTS;
                 // a partial: [rows][DH] outputs, [rows][2] maxima and sums
                 auto part = [&](uint32_t p) { const uint32_t cta = c0 + p; return f.parts + ((size_t)cta * 2 + (stretch(cta) >= now.lo ? 0 : 1)) * slot_floats<DH, MT>(); };
                 auto ml_of = [&](const float *from, uint32_t row) { return __ldcg(reinterpret_cast<const float2 *>(from + MT * 16 * DH + row * 2)); };
@@ -497,8 +480,8 @@ int launch_few(FewArgs f, cudaStream_t st) {
 
 bool shapes_ok(const tgp_model_cfg *c) { return c && (c->Dh == 64 || c->Dh == 128) && c->Hkv && c->Hq && c->Hq % c->Hkv == 0 && c->Hq / c->Hkv <= 128 && c->TK && c->TK % 16 == 0 && c->max_len; }
 
-// bytes of the counters, and of the partials of a launch of few rows
-uint64_t counter_bytes(const tgp_model_cfg *c, uint32_t B) { return ((uint64_t)B * c->Hkv * 8 + 255) / 256 * 256; }
+// bytes of the counters - of each sequence and KV head, and one of tiles -, and of the partials of a launch of few rows
+uint64_t counter_bytes(const tgp_model_cfg *c, uint32_t B) { return (((uint64_t)B * c->Hkv + 1) * 8 + 255) / 256 * 256; }
 uint64_t part_bytes(const tgp_model_cfg *c) {
     const uint32_t ctas = c->Dh == 128 ? few_ctas<128, 1>() : few_ctas<64, 1>();
     return (uint64_t)ctas * 2 * 32 * (c->Dh + 2) * 4;
@@ -535,6 +518,7 @@ extern "C" int tgp_k_attn_paged(const void *qb, const void *k_pages, const void 
     f.magic = (uint32_t)(((1ull << f.shift) + chunks - 1) / chunks);
     f.per_token = (65536 + G - 1) / G;
     f.counters = (u64 *)scratch_dev;
+    f.tiles = (uint32_t *)(f.counters + (uint64_t)B * cfg->Hkv);
     f.parts = (float *)((uint8_t *)scratch_dev + counter_bytes(cfg, B));
     // one tile of 16 rows where all sequences fit it, else two; sequences of more rows are the other kernel's
     const bool one = (uint64_t)q_max * G <= 16;
@@ -542,5 +526,5 @@ extern "C" int tgp_k_attn_paged(const void *qb, const void *k_pages, const void 
     if (int rc = cfg->Dh == 64 ? (one ? launch_few<64, 1>(f, (cudaStream_t)stream) : launch_few<64, 2>(f, (cudaStream_t)stream))
                                : (one ? launch_few<128, 1>(f, (cudaStream_t)stream) : launch_few<128, 2>(f, (cudaStream_t)stream))) return rc;
     if ((uint64_t)q_max * G <= f.a.few) return TGP_OK;
-    return tgpk_attn_paged_many(f.a, cfg->Dh, (cudaStream_t)stream);
+    return tgpk_attn_paged_many(f.a, cfg->Dh, f.tiles, (cudaStream_t)stream);
 }

@@ -47,5 +47,23 @@ __device__ __forceinline__ TgpPagedKeys tgp_paged_keys(const TgpPagedAttn &a, ui
 // is the key at position j visible to the row at position p?
 __device__ __forceinline__ bool tgp_paged_sees(const TgpPagedAttn &a, uint32_t p, uint32_t j) { return j <= p && (!a.window || p - j < a.window || j < a.sinks); }
 
-// sequences of more than a.few rows * G, on tcgen05 (tgp_attn_paged_sm100.cu)
-int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, cudaStream_t st);
+// Counters in a scratch of any contents: a word is a number of arrivals only with this in its upper half - a NaN that no arithmetic gives, so whatever else the memory held, partials of an earlier call
+// among it, counts as 0.  The last arrival puts 0 back.
+constexpr unsigned long long TGP_PAGED_COUNTS = 0xffa5c3d1ull << 32;
+
+// How many have arrived at a counter, this one included.  What the CTA has written before its last barrier is seen by who arrives later.
+__device__ __forceinline__ uint32_t tgp_paged_arrive(unsigned long long *counter) {
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    unsigned long long was = atomicAdd(counter, 1ull);
+    // Not a number of arrivals yet: the first that replaces it is the first to have arrived.  Others may have added to it meanwhile; they have seen so, too, and arrive here.
+    while ((was & ~0xffffffffull) != TGP_PAGED_COUNTS) {
+        const unsigned long long now = atomicAdd(counter, 0ull);
+        if ((now & ~0xffffffffull) == TGP_PAGED_COUNTS) was = atomicAdd(counter, 1ull);
+        else if (atomicCAS(counter, now, TGP_PAGED_COUNTS + 1) == now) was = TGP_PAGED_COUNTS;
+    }
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
+    return (uint32_t)was + 1;
+}
+
+// sequences of more than a.few rows * G, on tcgen05 (tgp_attn_paged_sm100.cu); counter: a word that is 0
+int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, uint32_t *counter, cudaStream_t st);

@@ -36,7 +36,11 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, i
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
 }
 
-struct ManyArgs { TgpPagedAttn a; uint32_t tokens, piece; int none; };       // tokens of a CTA, rows of a piece, a row outside the maps
+struct ManyArgs { TgpPagedAttn a; uint32_t *counter; uint32_t tokens, piece; int none; bool wide; };        // tiles begun beyond the CTAs' first ones, 0 at the start; tokens of a tile, rows of a piece, a row outside the maps; output on 32 bytes
+
+// what a CTA works on: `tokens` tokens of a sequence and KV head, the first at row `row` and position `pos` (no tokens: the end)
+struct Tile { uint32_t row, pos, tokens, hk, b, missing; };
+constexpr uint32_t TILES = 4;                              // of which so many are known ahead
 
 template <int DH>
 __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -45,17 +49,21 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     constexpr int KB = DH / 64;                          // 64-wide blocks of the head dimension
     constexpr uint32_t Q_BYTES = KB * BQ * 128, KV_BYTES = KB * BKV * 128;
     uint8_t *Qs = smem, *Ks = Qs + Q_BYTES, *Vs = Ks + 2 * KV_BYTES;                            // K and V: two stages each
-    uint64_t *bar_k = reinterpret_cast<uint64_t *>(Vs + 2 * KV_BYTES);      // [2] K stage landed (stage 0's first use also carries Q)
+    uint64_t *bar_k = reinterpret_cast<uint64_t *>(Vs + 2 * KV_BYTES);      // [2] K stage landed (of a tile's first block also Q)
     uint64_t *bar_v = bar_k + 2;                                       // [2] V stage landed
     uint64_t *bar_s = bar_v + 2;                                       // S complete in TMEM (tensor core)
     uint64_t *bar_sfree = bar_s + 1;                                   // all 128 rows of S are in registers
-    uint64_t *bar_p = bar_sfree + 1;                                   // [2] all 128 rows of P_j (buffer j & 1) written, O rescaled where needed
-    uint64_t *bar_o = bar_p + 2;                                       // [2] P V_j complete (tensor core): P buffer j & 1 and the V stage are free
-    uint64_t *bar_kfree = bar_o + 2;                                   // [2] S_j complete: K stage j & 1 is free
-    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(bar_kfree + 2);
+    uint64_t *bar_p = bar_sfree + 1;                                   // [2] all 128 rows of P_i (buffer i & 1) written, O rescaled where needed
+    uint64_t *bar_o = bar_p + 2;                                       // [2] P V_i complete (tensor core): P buffer i & 1 and the V stage are free
+    uint64_t *bar_kfree = bar_o + 2;                                   // [2] S_i complete: K stage i & 1 is free, and with a tile's last block Q
+    uint64_t *bar_ofree = bar_kfree + 2;                               // O of a tile is in registers
+    uint64_t *bar_odd = bar_ofree + 1;                                 // `odd` of a tile is what it is going to be
+    uint64_t *bar_tile = bar_odd + 1;                                  // [TILES] a tile is known
+    uint64_t *bar_tfree = bar_tile + TILES;                            // [TILES] the seven warps that work on it have read it
+    Tile *tiles = reinterpret_cast<Tile *>(bar_tfree + TILES);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(tiles + TILES);
     volatile uint32_t *failed = tmem_slot + 1;                         // [0] a wait ran out; [1] never set
-    volatile uint32_t *odd = failed + 2;                               // a value that is no number was put to zero
-    uint32_t *place = tmem_slot + 4;                                   // this CTA's sequence and tile
+    volatile uint32_t *odd = failed + 2;                               // [2] (of tiles in turn) a value that is no number was put to zero
     const TgpPagedAttn &a = args.a;
 
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -67,9 +75,11 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     if (warp == 5 && elect_one()) {
         mbar_init(bar_k, 1); mbar_init(bar_k + 1, 1); mbar_init(bar_v, 1); mbar_init(bar_v + 1, 1);
         mbar_init(bar_s, 1); mbar_init(bar_sfree, 128); mbar_init(bar_p, 128); mbar_init(bar_p + 1, 128); mbar_init(bar_o, 1); mbar_init(bar_o + 1, 1); mbar_init(bar_kfree, 1); mbar_init(bar_kfree + 1, 1);
+        mbar_init(bar_ofree, 128); mbar_init(bar_odd, 1);
+        for (uint32_t i = 0; i < TILES; ++i) { mbar_init(bar_tile + i, 1); mbar_init(bar_tfree + i, 7); }
         failed[0] = 0;
         failed[1] = 0;
-        *odd = 0;
+        odd[0] = odd[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmQ) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&tmK) : "memory");
@@ -80,328 +90,420 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // not before the allocation: see tgp_sm100.cuh
     }
-    if (warp == 7) {
-        // ---- which tile: blockIdx.x counts the tiles of all sequences that are this kernel's, a sequence's last tile (the longest) first ----
-        asm volatile("griddepcontrol.wait;" ::: "memory");
-        uint32_t before = 0, b = 0xffffffffu, tile = 0;
-        for (uint32_t i0 = 0; i0 < a.B && b == 0xffffffffu; i0 += 32) {
-            const uint32_t i = i0 + lane;
-            uint32_t mine = 0;
-            if (i < a.B) {
-                const TgpPagedSeq s = tgp_paged_seq(a, i);
-                if (s.n && !s.idle && s.n * a.G > a.few) mine = (s.n + args.tokens - 1) / args.tokens;
-            }
-            uint32_t x = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-            const uint32_t hit = __ballot_sync(0xffffffffu, before + x > blockIdx.x);
-            if (hit) {
-                const int at = __ffs(hit) - 1;
-                b = i0 + at;
-                tile = before + __shfl_sync(0xffffffffu, x, at) - 1 - blockIdx.x;
-            }
-            before += __shfl_sync(0xffffffffu, x, 31);
-        }
-        if (lane == 0) { place[0] = b; place[1] = tile; }
-    }
+    // rows of Q behind the box's: zeros, so that they do not slow the softmax down
+    for (uint32_t i = args.tokens * a.G * KB * 8 + tid; i < BQ * KB * 8; i += THREADS)
+        *reinterpret_cast<uint4 *>(Qs + (i / 8 % KB) * (BQ * 128) + (i / (8 * KB)) * 128 + (i % 8) * 16) = make_uint4(0, 0, 0, 0);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t tmem_S = tmem_base, tmem_O = tmem_base + 64, tmem_P = tmem_base + 192;     // P: two buffers of 32 columns (bf16 pairs)
-    const uint32_t b = place[0], hk = blockIdx.y;
-    const bool live = b != 0xffffffffu;
-    const TgpPagedSeq seq = live ? tgp_paged_seq(a, b) : TgpPagedSeq{0, 1, 1, false};
-    const uint32_t t0 = place[1] * args.tokens, first_pos = seq.end - seq.n + t0, last_pos = min(first_pos + args.tokens, seq.end) - 1;      // tokens of the tile
-    const uint32_t tokens = last_pos - first_pos + 1, rows = tokens * a.G;
-    const TgpPagedKeys keys = tgp_paged_keys<BKV>(a, first_pos, last_pos);
-    const uint32_t nblk = live ? keys.chunks : 0, pieces = BKV / args.piece;
-    const int32_t *table = a.table + (size_t)(live ? b : 0) * a.W;
-    auto page_at = [&](uint32_t key) { const uint32_t i = key / a.P; return i < a.W ? (uint32_t)table[i] : 0xffffffffu; };
-
-    // is a page missing?  And rows behind the box's: zeros, so that they do not slow the softmax down
-    bool missing = false;
-    for (uint32_t i = tid; i < nblk * pieces; i += THREADS) {
-        const uint32_t key = keys.chunk(i / pieces) * BKV + i % pieces * args.piece;
-        missing |= key <= last_pos && page_at(key) >= a.n_pages;
-    }
-    for (uint32_t i = args.tokens * a.G * KB * 8 + tid; i < BQ * KB * 8; i += THREADS)
-        *reinterpret_cast<uint4 *>(Qs + (i / 8 % KB) * (BQ * 128) + (i / (8 * KB)) * 128 + (i % 8) * 16) = make_uint4(0, 0, 0, 0);
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    missing = __syncthreads_or(missing);
+    const uint32_t pieces = BKV / args.piece;
     auto give_up = [&](int code) { if (!*failed) { *failed = 1; atomicCAS(&g_attn_paged_error, 0, code); } };
+    auto wait = [&](uint64_t *bar, uint32_t parity, int code) {              // by a warp
+        const bool ok = mbar_wait(bar, parity, failed);
+        if (!ok) give_up(code);
+        return __all_sync(0xffffffffu, ok);
+    };
+    auto page_at = [&](const Tile &t, uint32_t key) { const uint32_t i = key / a.P; return i < a.W ? (uint32_t)a.table[(size_t)t.b * a.W + i] : 0xffffffffu; };
+    auto last_of = [&](const Tile &t) { return t.pos + t.tokens - 1; };
+    auto keys_of = [&](const Tile &t) { return tgp_paged_keys<BKV>(a, t.pos, last_of(t)); };
     // whole: every row sees every key of the block
-    auto whole = [&](uint32_t key0) { return key0 + BKV - 1 <= first_pos && (!a.window || last_pos - key0 < a.window || key0 + BKV <= a.sinks); };
-    // Registers move from the second warpgroup (three single-thread roles and an idle warp) to the softmax warpgroup:
+    auto whole = [&](const Tile &t, uint32_t key0) { return key0 + BKV - 1 <= t.pos && (!a.window || last_of(t) - key0 < a.window || key0 + BKV <= a.sinks); };
+    // the n-th tile of this CTA; false at the end
+    auto tile_at = [&](Tile &t, uint32_t n, bool &ok) {
+        ok = wait(bar_tile + n % TILES, n / TILES & 1, 4);
+        if (!ok) return false;
+        t = tiles[n % TILES];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_tfree + n % TILES);
+        return t.tokens != 0;
+    };
+    // Registers move from the second warpgroup (three single-thread roles and the warp that finds tiles) to the softmax warpgroup:
     // 128 * 64 + 128 * 192 is the 128 per thread the CTA is launched with.
     if (warp >= 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;" ::: "memory");
-        if (warp == 5 && nblk) {
+        if (warp == 7) {
+            // ======================= tiles: the first is the CTA's own, further ones are those that nobody has begun =======================
+            uint32_t all = 0;                                                // tiles of all sequences
+            for (uint32_t i0 = 0; i0 < a.B; i0 += 32) {
+                uint32_t mine = 0;
+                if (i0 + lane < a.B) { const TgpPagedSeq s = tgp_paged_seq(a, i0 + lane); if (s.n && !s.idle && s.n * a.G > a.few) mine = (s.n + args.tokens - 1) / args.tokens; }
+                all += __reduce_add_sync(0xffffffffu, mine);
+            }
+            const uint32_t items = all * a.Hkv;
+            bool ok = true;
+            for (uint32_t n = 0, item = blockIdx.x; ok; ++n) {
+                Tile t{0, 0, 0, 0, 0, 0};
+                const bool live = item < items;
+                if (live) {
+                    // A sequence's last tile (the longest) comes first, and the KV heads of a tile one after the other.
+                    const uint32_t at = item / a.Hkv;
+                    t.hk = item - at * a.Hkv;
+                    uint32_t before = 0;
+                    for (uint32_t i0 = 0; i0 < a.B; i0 += 32) {
+                        TgpPagedSeq s{0, 0, 0, false};
+                        uint32_t mine = 0;
+                        if (i0 + lane < a.B) { s = tgp_paged_seq(a, i0 + lane); if (s.n && !s.idle && s.n * a.G > a.few) mine = (s.n + args.tokens - 1) / args.tokens; }
+                        uint32_t x = mine;
+#pragma unroll
+                        for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+                        const uint32_t hit = __ballot_sync(0xffffffffu, before + x > at);
+                        if (hit) {
+                            const int from = __ffs(hit) - 1;
+                            const uint32_t t0 = (before + __shfl_sync(0xffffffffu, x, from) - 1 - at) * args.tokens, rows = __shfl_sync(0xffffffffu, s.n, from);
+                            t.b = i0 + from;
+                            t.row = __shfl_sync(0xffffffffu, s.first, from) + t0;
+                            t.pos = __shfl_sync(0xffffffffu, s.end, from) - rows + t0;
+                            t.tokens = min(args.tokens, rows - t0);
+                            break;
+                        }
+                        before += __shfl_sync(0xffffffffu, x, 31);
+                    }
+                    const TgpPagedKeys keys = keys_of(t);                    // is a page missing?
+                    uint32_t missing = 0;
+                    for (uint32_t i = lane; i < keys.chunks * pieces; i += 32) {
+                        const uint32_t key = keys.chunk(i / pieces) * BKV + i % pieces * args.piece;
+                        missing |= key <= last_of(t) && page_at(t, key) >= a.n_pages;
+                    }
+                    t.missing = __any_sync(0xffffffffu, missing);
+                }
+                if (n >= TILES && !(ok = wait(bar_tfree + n % TILES, n / TILES - 1 & 1, 4))) break;
+                if (lane == 0) { tiles[n % TILES] = t; mbar_arrive(bar_tile + n % TILES); }
+                __syncwarp();
+                if (!live) break;
+                uint32_t next = 0;
+                if (lane == 0) next = gridDim.x + atomicAdd(args.counter, 1u);
+                item = __shfl_sync(0xffffffffu, next, 0);
+            }
+        } else if (warp == 5) {
             // ======================= TMA warp =======================
-            // Two windows of 32 pieces each, a lane's piece in either: rows of the maps (args.none: zeros)
-            uint32_t nk = 0, nv = 0, window = 0;                             // K and V blocks asked for; the first window, which V is in
-            auto row_of = [&](uint32_t piece) {
-                const uint32_t j = piece / pieces;
-                if (j >= nblk) return args.none;
-                const uint32_t key = keys.chunk(j) * BKV + piece % pieces * args.piece;
-                if (key > last_pos) return args.none;
-                const uint32_t page = page_at(key);
-                return page < a.n_pages ? (int)((page * a.Hkv + hk) * a.P + key % a.P) : args.none;
+            // Places in the sequence of all blocks: of K, two blocks ahead, and of V.  Either has 32 pieces' rows of the maps in its lanes (args.none: zeros).
+            struct Cursor { Tile t; TgpPagedKeys keys; uint32_t n, j, i, base; int rows; bool live; };      // tile n, its block j, block i of all; lane 0's piece
+            bool ok = true;
+            auto fill = [&](Cursor &c) {
+                c.base = c.j * pieces;
+                const uint32_t piece = c.base + lane, j = piece / pieces;
+                c.rows = args.none;
+                if (j < c.keys.chunks) {
+                    const uint32_t key = c.keys.chunk(j) * BKV + piece % pieces * args.piece;
+                    if (key <= last_of(c.t)) { const uint32_t page = page_at(c.t, key); if (page < a.n_pages) c.rows = (int)((page * a.Hkv + c.t.hk) * a.P + key % a.P); }
+                }
             };
-            int here = row_of(lane), there = row_of(32 + lane);
-            auto load = [&](uint8_t *dst, const CUtensorMap *map, uint32_t j, uint64_t *bar, uint32_t more_bytes) {
+            auto enter = [&](Cursor &c, bool release) {
+                ok = wait(bar_tile + c.n % TILES, c.n / TILES & 1, 4);
+                if (!ok) { c.live = false; return; }
+                c.t = tiles[c.n % TILES];
+                __syncwarp();
+                if (release && lane == 0) mbar_arrive(bar_tfree + c.n % TILES);
+                c.live = c.t.tokens != 0;
+                c.j = 0;
+                if (c.live) { c.keys = keys_of(c.t); fill(c); }
+            };
+            auto load = [&](Cursor &c, uint8_t *dst, const CUtensorMap *map, uint64_t *bar, uint32_t more_bytes) {
                 if (elect_one()) mbar_expect_tx(bar, KV_BYTES + more_bytes);
+                __syncwarp();
                 for (uint32_t i = 0; i < pieces; ++i) {
-                    const uint32_t p = j * pieces + i;
-                    const int y = __shfl_sync(0xffffffffu, p / 32 == window ? here : there, p & 31);
+                    const int y = __shfl_sync(0xffffffffu, c.rows, c.j * pieces + i - c.base);
                     if (elect_one())
 #pragma unroll
                         for (uint32_t kb = 0; kb < KB; ++kb) tma_load_2d(dst + kb * (BKV * 128) + i * args.piece * 128, map, kb * 64, y, bar);
+                    __syncwarp();
                 }
+                ++c.i;
             };
-            auto next_k = [&](uint32_t more_bytes) { load(Ks + (nk & 1) * KV_BYTES, &tmK, nk, bar_k + (nk & 1), more_bytes); nk += 1; };
-            auto next_v = [&]() {
-                if (nv * pieces / 32 != window) { window += 1; here = there; there = row_of((window + 1) * 32 + lane); }
-                load(Vs + (nv & 1) * KV_BYTES, &tmV, nv, bar_v + (nv & 1), 0);
-                nv += 1;
+            auto step = [&](Cursor &c, bool release) {
+                if (++c.j == c.keys.chunks) { ++c.n; enter(c, release); }
+                else if ((c.j + 1) * pieces - c.base > 32) fill(c);
             };
-            next_k(KB * args.tokens * a.G * 128);                            // K_0 and, on the same barrier, Q
-            if (elect_one())
+            Cursor k{}, v{};
+            enter(k, false);
+            if (ok) enter(v, true);
+            auto load_k = [&]() {                                            // with a tile's first block Q is waited for, too
+                load(k, Ks + (k.i & 1) * KV_BYTES, &tmK, bar_k + (k.i & 1), k.j == 0 ? KB * args.tokens * a.G * 128 : 0);
+            };
+            auto load_q = [&](uint32_t i, const Tile &t) {
+                if (elect_one())
 #pragma unroll
-                for (uint32_t kb = 0; kb < KB; ++kb) tma_load_3d(Qs + kb * (BQ * 128), &tmQ, kb * 64, hk * a.G, seq.first + t0, bar_k);
-            if (1 < nblk) next_k(0);
-            next_v();
-            auto wait = [&](uint64_t *bar, uint32_t parity, int code) {
-                const bool ok = mbar_wait(bar, parity, failed);
-                if (!ok) give_up(code);
-                return __all_sync(0xffffffffu, ok);
+                    for (uint32_t kb = 0; kb < KB; ++kb) tma_load_3d(Qs + kb * (BQ * 128), &tmQ, kb * 64, t.hk * a.G, t.row, bar_k + (i & 1));
+                __syncwarp();
             };
             // test hook: the first CTA of the grid never loads this V block, so the wait for it runs out
-            const uint32_t withhold = (blockIdx.x | blockIdx.y) == 0 ? (uint32_t)g_withhold_step : 0xffffffffu;
-            for (uint32_t jb = 0; jb + 1 < nblk; ++jb) {
-                const uint32_t st = jb & 1;
-                if (jb + 1 == withhold) break;
-                if (jb + 2 < nblk) {                                         // K_jb+2 goes where K_jb is, once S_jb is complete
-                    if (!wait(bar_kfree + st, (jb >> 1) & 1, 1)) break;
-                    next_k(0);
+            const uint32_t withhold = blockIdx.x == 0 ? (uint32_t)g_withhold_step : 0xffffffffu;
+            uint32_t q_due = 0xffffffffu;                                    // the block whose Q is not asked for yet
+            Tile q_tile{};
+            // block i: K_i goes where K_i-2 was, once S_i-2 is complete, V_i-1 where V_i-3 was, once P V_i-3 is, and Q of block i where that of the tile before was, once S_i-1 is
+            for (uint32_t i = 0; ok; ++i) {
+                const bool more = k.live;
+                if (more) {
+                    if (i >= 2 && !(ok = wait(bar_kfree + (i & 1), (i - 2 >> 1) & 1, 1))) break;
+                    if (k.j == 0) { q_due = i; q_tile = k.t; }
+                    load_k();
+                    if (i == 0) { load_q(0, q_tile); q_due = 0xffffffffu; }
+                    step(k, false);
+                    if (!ok) break;
                 }
-                if (jb >= 1 && !wait(bar_o + (st ^ 1), ((jb - 1) >> 1) & 1, 2)) break;                 // V_jb+1 goes where V_jb-1 is
-                next_v();
+                if (i >= 1) {
+                    if (!v.live) break;
+                    if (v.i == withhold) break;
+                    if (v.i >= 2 && !(ok = wait(bar_o + (v.i & 1), (v.i - 2 >> 1) & 1, 2))) break;
+                    load(v, Vs + (v.i & 1) * KV_BYTES, &tmV, bar_v + (v.i & 1), 0);
+                    step(v, true);
+                    if (!ok) break;
+                }
+                if (q_due == i && i) {
+                    if (!(ok = wait(bar_kfree + (i - 1 & 1), (i - 1 >> 1) & 1, 1))) break;
+                    load_q(i, q_tile);
+                    q_due = 0xffffffffu;
+                }
             }
-            // every load asked for must have landed before the CTA may exit (bounded; `never` is never set)
+            // every load asked for must have landed before the CTA may exit (bounded; `never` is never set), and with a tile's first K that of the Q that it is waited for with
             volatile uint32_t *never = failed + 1;
+            if (q_due != 0xffffffffu && __all_sync(0xffffffffu, mbar_wait(bar_kfree + (q_due - 1 & 1), (q_due - 1 >> 1) & 1, never))) load_q(q_due, q_tile);
             for (uint32_t st = 0; st < 2; ++st) {
-                const uint32_t ck = (nk + 1 - st) >> 1, cv = (nv + 1 - st) >> 1;     // loads asked for into this stage
+                const uint32_t ck = (k.i + 1 - st) >> 1, cv = (v.i + 1 - st) >> 1;   // loads asked for into this stage
                 if (ck) mbar_wait(bar_k + st, (ck - 1) & 1, never);
                 if (cv) mbar_wait(bar_v + st, (cv - 1) & 1, never);
             }
         } else if (warp == 4) {
-            // ======================= S warp: one thread issues S_j = Q K_j^T =======================
+            // ======================= S warp: one thread issues S_i = Q K_i^T =======================
             constexpr uint32_t idesc_s = umma_idesc(BKV);
-            auto wait = [&](uint64_t *bar, uint32_t parity, int code) {
-                bool ok = mbar_wait(bar, parity, failed);
-                if (!ok) give_up(code);
-                return __all_sync(0xffffffffu, ok);
-            };
-            for (uint32_t jb = 0; jb < nblk; ++jb) {
-                if (jb >= 1 && !wait(bar_sfree, (jb - 1) & 1, 4)) break;         // S_jb-1 is in registers
-                if (!wait(bar_k + (jb & 1), (jb >> 1) & 1, 3)) break;            // K_jb (and Q with K_0) has landed
-                if (elect_one()) {
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint8_t *Kj = Ks + (jb & 1) * KV_BYTES;
+            Tile t;
+            bool ok = true;
+            for (uint32_t n = 0, i = 0; ok && tile_at(t, n, ok); ++n) {
+                const uint32_t nblk = keys_of(t).chunks;
+                for (uint32_t jb = 0; jb < nblk; ++jb, ++i) {
+                    if (i >= 1 && !(ok = wait(bar_sfree, (i - 1) & 1, 4))) break;        // S_i-1 is in registers
+                    if (!(ok = wait(bar_k + (i & 1), (i >> 1) & 1, 3))) break;           // K_i (and Q with a tile's first) has landed
+                    if (elect_one()) {
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint8_t *Ki = Ks + (i & 1) * KV_BYTES;
 #pragma unroll
-                    for (uint32_t kb = 0; kb < KB; ++kb) {
-                        const uint64_t dq = umma_desc(smem_u32(Qs + kb * (BQ * 128))), dk = umma_desc(smem_u32(Kj + kb * (BKV * 128)));
+                        for (uint32_t kb = 0; kb < KB; ++kb) {
+                            const uint64_t dq = umma_desc(smem_u32(Qs + kb * (BQ * 128))), dk = umma_desc(smem_u32(Ki + kb * (BKV * 128)));
 #pragma unroll
-                        for (uint32_t k = 0; k < 4; ++k) umma(tmem_S, dq + 2 * k, dk + 2 * k, idesc_s, (kb | k) != 0);
-                    }
-                    umma_commit(bar_s);
-                    umma_commit(bar_kfree + (jb & 1));                           // its completion also frees the K stage
-                }
-                __syncwarp();
-            }
-        } else if (warp == 6) {
-            // ======================= P V warp: one thread issues O += P_j V_j =======================
-            constexpr uint32_t idesc_o = umma_idesc(DH) | (1u << 16);           // bit 16: B operand is MN-major
-            auto wait = [&](uint64_t *bar, uint32_t parity, int code) {
-                bool ok = mbar_wait(bar, parity, failed);
-                if (!ok) give_up(code);
-                return __all_sync(0xffffffffu, ok);
-            };
-            for (uint32_t jb = 0; jb < nblk; ++jb) {
-                const uint32_t st = jb & 1, key0 = keys.chunk(jb) * BKV;
-                if (!wait(bar_v + st, (jb >> 1) & 1, 3)) break;
-                if (!whole(key0)) {
-                    // Values that no row sees, whatever the page holds there, are zeros; those that some rows see and that are no numbers too, and remembered.
-                    for (uint32_t i = lane; i < BKV * KB * 8; i += 32) {
-                        const uint32_t r = i / (KB * 8), kb = (i / 8) % KB, c = i % 8, key = key0 + r;
-                        const bool none = key > last_pos || (a.window && key < keys.low && key >= a.sinks);
-                        const bool every = key <= first_pos && (!a.window || last_pos - key < a.window || key < a.sinks);
-                        if (every) continue;
-                        uint4 *at = reinterpret_cast<uint4 *>(Vs + st * KV_BYTES + kb * (BKV * 128) + r * 128 + c * 16);
-                        uint32_t w[4] = {0u, 0u, 0u, 0u};
-                        if (!none) {
-                            const uint4 v = *at;
-                            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                            bool found = false;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                if ((w[e] & 0x7f80u) == 0x7f80u) { w[e] &= 0xffff0000u; found = true; }
-                                if ((w[e] & 0x7f800000u) == 0x7f800000u) { w[e] &= 0xffffu; found = true; }
-                            }
-                            if (!found) continue;
-                            *odd = 1;
+                            for (uint32_t k = 0; k < 4; ++k) umma(tmem_S, dq + 2 * k, dk + 2 * k, idesc_s, (kb | k) != 0);
                         }
-                        *at = make_uint4(w[0], w[1], w[2], w[3]);
+                        umma_commit(bar_s);
+                        umma_commit(bar_kfree + (i & 1));                            // its completion also frees the K stage
                     }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                if (!wait(bar_p + st, (jb >> 1) & 1, 4)) break;
-                if (elect_one()) {
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t dv = umma_desc_mn(smem_u32(Vs + st * KV_BYTES), BKV * 128);
+            }
+        } else if (warp == 6) {
+            // ======================= P V warp: one thread issues O += P_i V_i =======================
+            constexpr uint32_t idesc_o = umma_idesc(DH) | (1u << 16);           // bit 16: B operand is MN-major
+            Tile t;
+            bool ok = true;
+            for (uint32_t n = 0, i = 0; ok && tile_at(t, n, ok); ++n) {
+                const TgpPagedKeys keys = keys_of(t);
+                const uint32_t last_pos = last_of(t);
+                if (lane == 0) odd[n & 1] = 0;                                  // (the tile before the last is done with it: its O has been waited for)
+                __syncwarp();
+                for (uint32_t jb = 0; jb < keys.chunks; ++jb, ++i) {
+                    const uint32_t st = i & 1, key0 = keys.chunk(jb) * BKV;
+                    if (!(ok = wait(bar_v + st, (i >> 1) & 1, 3))) break;
+                    // Steps of 16 keys that no row sees are left out.  In the others, values that no row sees, whatever the page holds there, are zeros; those that some rows see and
+                    // others do not are looked at, and what is no number becomes zero and is remembered.
+                    uint32_t steps = 0xf;
+                    if (!whole(t, key0)) {
+                        // rows of the block: [head, from) and [past, 64) are nobody's (a window's: [0, head) are first positions).  Of the others, [near, far) are before some rows' windows and
+                        // [sure, past) behind some rows.
+                        auto clip = [&](uint32_t key) { return key <= key0 ? 0u : min(key - key0, BKV); };
+                        const uint32_t past = clip(last_pos + 1), from = min(past, clip(keys.low)), head = min(from, clip(a.sinks)), sure = max(from, min(past, clip(t.pos + 1)));
+                        const uint32_t near = max(from, min(past, clip(a.sinks))), far = a.window && last_pos >= a.window ? max(near, min(past, clip(last_pos - a.window + 1))) : near;
+                        auto rows_of = [&](uint32_t r0, uint32_t r1, auto &&f) {         // f of every 16 bytes of rows [r0, r1)
+                            for (uint32_t e = lane; e < (r1 - r0) * KB * 8 && r1 > r0; e += 32) f(reinterpret_cast<uint4 *>(Vs + st * KV_BYTES + (e / 8 % KB) * (BKV * 128) + (r0 + e / (KB * 8)) * 128 + e % 8 * 16));
+                        };
+                        auto zero = [&](uint4 *at) { *at = make_uint4(0u, 0u, 0u, 0u); };
+                        steps = 0;
+                        for (uint32_t k = 0; k < 4; ++k) if (16 * k < head || (16 * k + 16 > from && 16 * k < past)) steps |= 1u << k;
+                        // (of steps that are left out nothing is read)
+                        rows_of(past, min(BKV, (past + 15) / 16 * 16), zero);
+                        rows_of(head, min(from, (head + 15) / 16 * 16), zero);
+                        rows_of(max(head, from / 16 * 16), from, zero);
+                        uint32_t exponents = 0;                                  // a bit where a half word's exponent is all ones
+                        auto look = [&](uint4 *at) {
+                            const uint4 v = *at;
+                            exponents |= ((v.x & 0x7f807f80u) + 0x00800080u) | ((v.y & 0x7f807f80u) + 0x00800080u) | ((v.z & 0x7f807f80u) + 0x00800080u) | ((v.w & 0x7f807f80u) + 0x00800080u);
+                        };
+                        rows_of(near, far, look);
+                        rows_of(sure, past, look);
+                        if (__any_sync(0xffffffffu, (exponents & 0x80008000u) != 0)) {
+                            auto clean = [&](uint4 *at) {
+                                uint32_t w[4] = {at->x, at->y, at->z, at->w};
 #pragma unroll
-                    for (uint32_t k = 0; k < 4; ++k)                             // 16 keys per step: 8 columns of P, 2048 B of V rows
-                        umma_ts(tmem_O, tmem_P + st * 32 + 8 * k, dv + 128 * k, idesc_o, (jb | k) != 0);
-                    umma_commit(bar_o + st);
+                                for (int h = 0; h < 4; ++h) {
+                                    if ((w[h] & 0x7f80u) == 0x7f80u) w[h] &= 0xffff0000u;
+                                    if ((w[h] & 0x7f800000u) == 0x7f800000u) w[h] &= 0xffffu;
+                                }
+                                *at = make_uint4(w[0], w[1], w[2], w[3]);
+                            };
+                            rows_of(near, far, clean);
+                            __syncwarp();
+                            rows_of(sure, past, clean);
+                            if (lane == 0) odd[n & 1] = 1;
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    if (!(ok = wait(bar_p + st, (i >> 1) & 1, 4))) break;
+                    if (jb == 0 && n && !(ok = wait(bar_ofree, (n - 1) & 1, 4))) break;  // O of the tile before is in registers
+                    if (elect_one()) {
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t dv = umma_desc_mn(smem_u32(Vs + st * KV_BYTES), BKV * 128);
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k)                             // 16 keys per step: 8 columns of P, 2048 B of V rows
+                            if (steps >> k & 1) umma_ts(tmem_O, tmem_P + st * 32 + 8 * k, dv + 128 * k, idesc_o, jb != 0 || (steps & ((1u << k) - 1)) != 0);
+                        umma_commit(bar_o + st);
+                    }
+                    __syncwarp();
                 }
                 __syncwarp();
+                if (lane == 0) mbar_arrive(bar_odd);
             }
-            __syncwarp();
-            asm volatile("bar.arrive 1, 160;" ::: "memory");                 // `odd` is what it is going to be
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;" ::: "memory");
         // ======================= softmax warps: thread = row = TMEM lane =======================
         const uint32_t tok = tid / a.G;
-        const bool row_ok = tid < rows;
-        const uint32_t qpos = first_pos + min(tok, tokens - 1);              // padding rows take the last token's mask
         const uint32_t lane_addr = (warp * 32u) << 16;                       // this warp's quarter of the TMEM lanes
-        float m_ref = -FLT_MAX, lrow = 0.f;                                  // exponent reference and running sum of this row
-        auto wait = [&](uint64_t *bar, uint32_t parity, int code) {
-            bool ok = mbar_wait(bar, parity, failed);
-            if (!ok) give_up(code);
-            return __all_sync(0xffffffffu, ok);
-        };
+        Tile t;
         bool ok = true;
-        for (uint32_t jb = 0; jb < nblk; ++jb) {
-            const uint32_t key0 = keys.chunk(jb) * BKV;
-            if (!(ok = wait(bar_s, jb & 1, 1))) break;
-            float s[BKV];
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            tmem_ld64(tmem_S + lane_addr, s);
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            mbar_arrive(bar_sfree);
-            if (!whole(key0)) {
-                // hidden: behind the row, or before its window and none of the first positions
-                const uint32_t low = a.window && qpos >= a.window ? qpos - a.window + 1 : 0;
-#pragma unroll
-                for (uint32_t i = 0; i < BKV; ++i)
-                    if (key0 + i > qpos || (key0 + i < low && key0 + i >= a.sinks)) s[i] = -INFINITY;
-            }
-            if (missing) {
-                uint32_t there = 0;                                          // a bit per 16 keys (no page begins inside them)
-                for (uint32_t i = 0; i < 4; ++i) there |= (page_at(key0 + i * 16) < a.n_pages ? 1u : 0u) << i;
-#pragma unroll
-                for (uint32_t i = 0; i < BKV; ++i)
-                    if (!(there >> (i / 16) & 1)) s[i] = -INFINITY;
-            }
-            auto row_max = [&]() {                                           // of the scaled scores (scale > 0: max commutes with it)
-                float m0 = max3(s[0], s[1], s[2]), m1 = max3(s[3], s[4], s[5]);
-#pragma unroll
-                for (uint32_t i = 6; i + 3 < BKV; i += 4) { m0 = max3(m0, s[i], s[i + 1]); m1 = max3(m1, s[i + 2], s[i + 3]); }
-                return max3(m0, m1, fmaxf(s[BKV - 2], s[BKV - 1])) * a.sl2;
-            };
-            uint32_t w[BKV / 2];
-            auto exps = [&](float m) {                                       // w = exp2(S * scale - m) as bf16 pairs; returns their fp32 sum
-                const uint64_t sc2 = pack2(a.sl2, a.sl2), nm2 = pack2(-m, -m);
-                uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
-#pragma unroll
-                for (uint32_t i = 0; i < BKV / 2; ++i) {
-                    float x0, x1;
-                    unpack2(fma2(pack2(s[2 * i], s[2 * i + 1]), sc2, nm2), x0, x1);
-                    const float p0 = ex2(x0), p1 = ex2(x1);                  // a masked score is -inf: p = 0
-                    if (i & 1) acc1 = add2(acc1, pack2(p0, p1)); else acc0 = add2(acc0, pack2(p0, p1));
-                    __nv_bfloat162 pk = __floats2bfloat162_rn(p0, p1);       // .x = p0 in the lower half
-                    w[i] = *reinterpret_cast<uint32_t *>(&pk);
-                }
-                float l0, l1;
-                unpack2(add2(acc0, acc1), l0, l1);
-                return l0 + l1;
-            };
-            // The exponent reference m is the row max of block 0, moved only where a block's sum says that a score lies more than about 2^40 above it (or overflowed).  A row
-            // that sees nothing of block 0 has the lowest finite reference: its sums are 0, and the first finite score takes the slow path.
-            if (jb == 0) m_ref = fmaxf(row_max(), -FLT_MAX);
-            float lblk = exps(m_ref);
-            if (jb > 0 && __any_sync(0xffffffffu, !(lblk <= 0x1p40f))) {
-                if (!(ok = wait(bar_o + ((jb - 1) & 1), ((jb - 1) >> 1) & 1, 2))) break;           // P V_{j-1}: nothing is accumulating into O
-                const float m_new = fmaxf(m_ref, row_max()), alpha = ex2(m_ref - m_new);
-                m_ref = m_new;
-                lrow *= alpha;
+        for (uint32_t n = 0, i0 = 0; ok && tile_at(t, n, ok); ++n) {
+            const TgpPagedKeys keys = keys_of(t);
+            const uint32_t nblk = keys.chunks, qpos = t.pos + min(tok, t.tokens - 1);    // padding rows take the last token's mask
+            float m_ref = -FLT_MAX, lrow = 0.f;                              // exponent reference and running sum of this row
+            for (uint32_t jb = 0; jb < nblk; ++jb) {
+                const uint32_t i = i0 + jb, key0 = keys.chunk(jb) * BKV;
+                if (!(ok = wait(bar_s, i & 1, 1))) break;
+                float s[BKV];
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                tmem_ld64(tmem_S + lane_addr, s);
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                mbar_arrive(bar_sfree);
+                if (t.missing || !whole(t, key0)) {
+                    // a bit per key that is hidden: behind the row, or before its window and none of the first positions, or of no page
+                    auto below = [&](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };       // the first n keys of the block
+                    const uint32_t low = a.window && qpos >= a.window ? qpos - a.window + 1 : 0;
+                    uint64_t hidden = ~below((int)(qpos - key0) + 1) | (below((int)(low - key0)) & ~below((int)(min(a.sinks, 0x7fffffffu) - key0)));
+                    if (t.missing)
+                        for (uint32_t e = 0; e < 4; ++e) if (page_at(t, key0 + e * 16) >= a.n_pages) hidden |= 0xffffull << e * 16;       // (no page begins inside 16 keys)
+                    const uint32_t h0 = (uint32_t)hidden, h1 = (uint32_t)(hidden >> 32);
 #pragma unroll
-                for (uint32_t h = 0; h < DH / 32; ++h) {
-                    float v[32];
-                    uint32_t u[32];
-                    tmem_ld32(tmem_O + lane_addr + h * 32, v);
-#pragma unroll
-                    for (uint32_t i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i] * alpha);
-                    tmem_st32(tmem_O + lane_addr + h * 32, u);
+                    for (uint32_t e = 0; e < BKV; ++e)
+                        if ((e < 32 ? h0 : h1) >> (e % 32) & 1) s[e] = -INFINITY;
                 }
-                lblk = exps(m_ref);
-            }
-            lrow += lblk;
-            if (jb >= 2 && !(ok = wait(bar_o + (jb & 1), ((jb - 2) >> 1) & 1, 2))) break;      // P V_{j-2}: this P buffer is free
-            tmem_st32(tmem_P + (jb & 1) * 32 + lane_addr, w);
-            tmem_wait_st();
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            mbar_arrive(bar_p + (jb & 1));
-        }
-        // ---- the last P V; normalise and store this thread's row ----
-        if (ok && nblk) ok = wait(bar_o + ((nblk - 1) & 1), ((nblk - 1) >> 1) & 1, 2);
-        __syncwarp();
-        asm volatile("bar.sync 1, 160;" ::: "memory");                       // (the P V warp has left its loop, too, however it went)
-        if (ok && nblk) {
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const bool empty = lrow == 0.f;                                  // a row that sees nothing is zero
-            const float inv = 1.0f / lrow;
-            bf16 *dst = a.o + ((size_t)(seq.first + t0 + tok) * a.Hq + hk * a.G + (tid - tok * a.G)) * DH;
+                // The exponent reference m_ref is the row max of the tile's block 0, moved only where a block's sum says that a score lies more than about 2^40 above it (or overflowed).  A row
+                // that sees nothing of block 0 has the lowest finite reference: its sums are 0, and the first finite score moves it.  (Everything stands here once: with the exponentials and
+                // masks unrolled in several places, warps waited for instructions.)
+                uint32_t w[BKV / 2];
+                float lblk;
+                for (bool move = jb == 0;;) {
+                    if (move) {                                              // the row max of the scaled scores (scale > 0: max commutes with it)
+                        float m0 = max3(s[0], s[1], s[2]), m1 = max3(s[3], s[4], s[5]);
 #pragma unroll
+                        for (uint32_t e = 6; e + 3 < BKV; e += 4) { m0 = max3(m0, s[e], s[e + 1]); m1 = max3(m1, s[e + 2], s[e + 3]); }
+                        const float m_new = fmaxf(m_ref, max3(m0, m1, fmaxf(s[BKV - 2], s[BKV - 1])) * a.sl2), alpha = ex2(m_ref - m_new);
+                        m_ref = m_new;
+                        if (jb) {
+                            if (!(ok = wait(bar_o + (i - 1 & 1), (i - 1 >> 1) & 1, 2))) break;       // P V_{i-1}: nothing is accumulating into O
+                            lrow *= alpha;
+                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+                            for (uint32_t h = 0; h < DH / 32; ++h) {
+                                float v[32];
+                                uint32_t u[32];
+                                tmem_ld32(tmem_O + lane_addr + h * 32, v);
+#pragma unroll
+                                for (uint32_t e = 0; e < 32; ++e) u[e] = __float_as_uint(v[e] * alpha);
+                                tmem_st32(tmem_O + lane_addr + h * 32, u);
+                            }
+                        }
+                    }
+                    // w = exp2(S * scale - m) as bf16 pairs, and their fp32 sum
+                    const uint64_t sc2 = pack2(a.sl2, a.sl2), nm2 = pack2(-m_ref, -m_ref);
+                    uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
+#pragma unroll
+                    for (uint32_t e = 0; e < BKV / 2; ++e) {
+                        float x0, x1;
+                        unpack2(fma2(pack2(s[2 * e], s[2 * e + 1]), sc2, nm2), x0, x1);
+                        const float p0 = ex2(x0), p1 = ex2(x1);              // a masked score is -inf: p = 0
+                        if (e & 1) acc1 = add2(acc1, pack2(p0, p1)); else acc0 = add2(acc0, pack2(p0, p1));
+                        __nv_bfloat162 pk = __floats2bfloat162_rn(p0, p1);   // .x = p0 in the lower half
+                        w[e] = *reinterpret_cast<uint32_t *>(&pk);
+                    }
+                    float l0, l1;
+                    unpack2(add2(acc0, acc1), l0, l1);
+                    lblk = l0 + l1;
+                    if (move || !__any_sync(0xffffffffu, !(lblk <= 0x1p40f))) break;
+                    move = true;
+                }
+                if (!ok) break;
+                lrow += lblk;
+                if (i >= 2 && !(ok = wait(bar_o + (i & 1), (i - 2 >> 1) & 1, 2))) break;      // P V_{i-2}: this P buffer is free
+                tmem_st32(tmem_P + (i & 1) * 32 + lane_addr, w);
+                tmem_wait_st();
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                mbar_arrive(bar_p + (i & 1));
+            }
+            i0 += nblk;
+            // ---- the last P V; normalise and store this thread's row ----
+            ok = ok && wait(bar_o + (i0 - 1 & 1), (i0 - 1 >> 1) & 1, 2) && wait(bar_odd, n & 1, 2);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const bool empty = lrow == 0.f, row_ok = tid < t.tokens * a.G;   // a row that sees nothing is zero
+            const float inv = 1.0f / lrow;
+            bf16 *dst = a.o + ((size_t)(t.row + tok) * a.Hq + t.hk * a.G + (tid - tok * a.G)) * DH;
+#pragma unroll 1
             for (uint32_t h = 0; h < DH / 32; ++h) {
                 float v[32];
                 __syncwarp();
                 tmem_ld32(tmem_O + lane_addr + h * 32, v);
-                if (*odd) {                                                  // keys that some rows see and others do not: what was put to zero
-                    for (uint32_t jb = 0; jb < nblk; ++jb) {
-                        const uint32_t key0 = keys.chunk(jb) * BKV;
-                        if (whole(key0)) continue;
-                        for (uint32_t key = key0; key < key0 + BKV && key <= qpos; ++key) {
-                            const uint32_t page = page_at(key);
-                            if (page >= a.n_pages || !tgp_paged_sees(a, qpos, key) || (key <= first_pos && (!a.window || last_pos - key < a.window || key < a.sinks))) continue;
-                            const bf16 *from = a.v + (((size_t)page * a.Hkv + hk) * a.P + key % a.P) * DH + h * 32;
+                uint32_t w[16];
 #pragma unroll
-                            for (uint32_t i = 0; i < 32; ++i) {
-                                const float x = __bfloat162float(from[i]);
-                                if (!(fabsf(x) < INFINITY)) v[i] += x;
-                            }
+                for (uint32_t e = 0; e < 16; ++e) {
+                    __nv_bfloat162 pk = __floats2bfloat162_rn(v[2 * e] * inv, v[2 * e + 1] * inv);
+                    w[e] = empty ? 0u : *reinterpret_cast<uint32_t *>(&pk);
+                }
+                if (!row_ok) continue;
+                if (args.wide) {                                             // (whole sectors)
+#pragma unroll
+                    for (uint32_t c = 0; c < 2; ++c)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst + h * 32 + c * 16), "r"(w[8 * c]), "r"(w[8 * c + 1]), "r"(w[8 * c + 2]), "r"(w[8 * c + 3]),
+                                     "r"(w[8 * c + 4]), "r"(w[8 * c + 5]), "r"(w[8 * c + 6]), "r"(w[8 * c + 7]) : "memory");
+                } else {
+#pragma unroll
+                    for (uint32_t c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(dst + h * 32 + c * 8) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+                }
+            }
+            __syncwarp();
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            mbar_arrive(bar_ofree);
+            if (odd[n & 1] && row_ok) {                                      // keys that some rows see and others do not: what was put to zero is added now
+                const uint32_t last_pos = last_of(t);
+#pragma unroll 1
+                for (uint32_t jb = 0; jb < nblk; ++jb) {
+                    const uint32_t key0 = keys.chunk(jb) * BKV;
+                    if (whole(t, key0)) continue;
+#pragma unroll 1
+                    for (uint32_t key = key0; key < key0 + BKV && key <= qpos; ++key) {
+                        const uint32_t page = page_at(t, key);
+                        if (page >= a.n_pages || !tgp_paged_sees(a, qpos, key) || (key <= t.pos && (!a.window || last_pos - key < a.window || key < a.sinks))) continue;
+                        const bf16 *from = a.v + (((size_t)page * a.Hkv + t.hk) * a.P + key % a.P) * DH;
+#pragma unroll 1
+                        for (uint32_t e = 0; e < DH; ++e) {
+                            const float x = __bfloat162float(from[e]);
+                            if (!(fabsf(x) < INFINITY)) dst[e] = __float2bfloat16_rn(__bfloat162float(dst[e]) + x);
                         }
                     }
-                }
-#pragma unroll
-                for (uint32_t c = 0; c < 4; ++c) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i) {
-                        __nv_bfloat162 pk = __floats2bfloat162_rn(v[c * 8 + 2 * i] * inv, v[c * 8 + 2 * i + 1] * inv);
-                        w[i] = empty ? 0u : *reinterpret_cast<uint32_t *>(&pk);
-                    }
-                    if (row_ok) *reinterpret_cast<uint4 *>(dst + h * 32 + c * 8) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
         }
     }
+    __syncwarp();
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     if (warp == 4) {
@@ -410,7 +512,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     }
 }
 
-template <int DH> constexpr int smem_bytes() { return (DH / 64) * (BQ + 4 * BKV) * 128 + 256; }
+template <int DH> constexpr int smem_bytes() { return (DH / 64) * (BQ + 4 * BKV) * 128 + 512; }
 
 // bf16 map of [rows of a third dimension][heads][Dh] with boxes of [tokens][heads of a group][64] and the 128-byte swizzle
 bool tensor_map_q(CUtensorMap *map, const void *base, uint64_t T, uint64_t Hq, uint64_t Dh, uint32_t G, uint32_t tokens) {
@@ -430,18 +532,18 @@ int launch_many(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v
 
 }  // namespace
 
-int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, cudaStream_t st) {
-    ManyArgs args{a, BQ / a.G, BKV, 0};
+int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, uint32_t *counter, cudaStream_t st) {
+    ManyArgs args{a, counter, BQ / a.G, BKV, 0, reinterpret_cast<uintptr_t>(a.o) % 32 == 0};
     while (a.P % args.piece) args.piece /= 2;                                // (a page holds a multiple of 16 positions)
     const uint64_t rows = (uint64_t)a.n_pages * a.Hkv * a.P;
     args.none = (int)rows;
     CUtensorMap mq, mk, mv;
     if (!tensor_map_q(&mq, a.q, a.T, a.Hq, Dh, a.G, args.tokens) || !tensor_map_bf16_2d(&mk, a.k, rows, Dh, (uint64_t)Dh * 2, args.piece) ||
         !tensor_map_bf16_2d(&mv, a.v, rows, Dh, (uint64_t)Dh * 2, args.piece)) return TGP_E_CUDA;
-    // tiles: of T rows, and one more for each sequence that this kernel has
+    // tiles: of T rows, and one more for each sequence that this kernel has; two CTAs fit an SM
     const uint32_t least = a.few / a.G + 1, tiles = a.T / args.tokens + std::min(a.B, a.T / least);
-    if (a.Hkv > 65535) return TGP_E_TOO_LARGE;
-    return Dh == 64 ? launch_many<64>(mq, mk, mv, args, dim3(tiles, a.Hkv), st) : launch_many<128>(mq, mk, mv, args, dim3(tiles, a.Hkv), st);
+    const dim3 grid((uint32_t)std::min<uint64_t>((uint64_t)tiles * a.Hkv, 2 * (uint32_t)tgpk_sms()));
+    return Dh == 64 ? launch_many<64>(mq, mk, mv, args, grid, st) : launch_many<128>(mq, mk, mv, args, grid, st);
 }
 
 int tgpk_attn_paged_wait_test(unsigned long long limit_ns, int withhold_step) {
