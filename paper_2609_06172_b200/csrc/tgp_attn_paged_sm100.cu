@@ -36,6 +36,17 @@ __device__ __forceinline__ void tma_load_3d(void *dst, const CUtensorMap *map, i
                  ::"r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+                   "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]),
+                 "r"(r[15]) : "memory");
+}
+
 struct ManyArgs { TgpPagedAttn a; uint32_t *counter; uint32_t tokens, piece; int none; bool wide; };        // tiles begun beyond the CTAs' first ones, 0 at the start; tokens of a tile, rows of a piece, a row outside the maps; output on 32 bytes
 
 // what a CTA works on: `tokens` tokens of a sequence and KV head, the first at row `row` and position `pos` (no tokens: the end)
@@ -51,10 +62,9 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     uint8_t *Qs = smem, *Ks = Qs + Q_BYTES, *Vs = Ks + 2 * KV_BYTES;                            // K and V: two stages each
     uint64_t *bar_k = reinterpret_cast<uint64_t *>(Vs + 2 * KV_BYTES);      // [2] K stage landed (of a tile's first block also Q)
     uint64_t *bar_v = bar_k + 2;                                       // [2] V stage landed
-    uint64_t *bar_s = bar_v + 2;                                       // S complete in TMEM (tensor core)
-    uint64_t *bar_sfree = bar_s + 1;                                   // all 128 rows of S are in registers
-    uint64_t *bar_p = bar_sfree + 1;                                   // [2] all 128 rows of P_i (buffer i & 1) written, O rescaled where needed
-    uint64_t *bar_o = bar_p + 2;                                       // [2] P V_i complete (tensor core): P buffer i & 1 and the V stage are free
+    uint64_t *bar_s = bar_v + 2;                                       // [2] S_i complete in TMEM (tensor core), in buffer i & 1
+    uint64_t *bar_p = bar_s + 2;                                       // [2] all 128 rows of P_i written over S_i, O rescaled where needed
+    uint64_t *bar_o = bar_p + 2;                                       // [2] P V_i complete (tensor core): buffer i & 1 and the V stage are free
     uint64_t *bar_kfree = bar_o + 2;                                   // [2] S_i complete: K stage i & 1 is free, and with a tile's last block Q
     uint64_t *bar_ofree = bar_kfree + 2;                               // O of a tile is in registers
     uint64_t *bar_odd = bar_ofree + 1;                                 // `odd` of a tile is what it is going to be
@@ -74,7 +84,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     // Set-up and the TMEM allocation overlap the previous kernel, which wrote what is read below.
     if (warp == 5 && elect_one()) {
         mbar_init(bar_k, 1); mbar_init(bar_k + 1, 1); mbar_init(bar_v, 1); mbar_init(bar_v + 1, 1);
-        mbar_init(bar_s, 1); mbar_init(bar_sfree, 128); mbar_init(bar_p, 128); mbar_init(bar_p + 1, 128); mbar_init(bar_o, 1); mbar_init(bar_o + 1, 1); mbar_init(bar_kfree, 1); mbar_init(bar_kfree + 1, 1);
+        mbar_init(bar_s, 1); mbar_init(bar_s + 1, 1); mbar_init(bar_p, 128); mbar_init(bar_p + 1, 128); mbar_init(bar_o, 1); mbar_init(bar_o + 1, 1); mbar_init(bar_kfree, 1); mbar_init(bar_kfree + 1, 1);
         mbar_init(bar_ofree, 128); mbar_init(bar_odd, 1);
         for (uint32_t i = 0; i < TILES; ++i) { mbar_init(bar_tile + i, 1); mbar_init(bar_tfree + i, 7); }
         failed[0] = 0;
@@ -99,7 +109,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *tmem_slot;
-    const uint32_t tmem_S = tmem_base, tmem_O = tmem_base + 64, tmem_P = tmem_base + 192;     // P: two buffers of 32 columns (bf16 pairs)
+    const uint32_t tmem_S = tmem_base, tmem_O = tmem_base + 2 * BKV;         // S: two buffers of 64 columns; P_i (32 columns of bf16 pairs) takes the first of S_i's
     const uint32_t pieces = BKV / args.piece;
     auto give_up = [&](int code) { if (!*failed) { *failed = 1; atomicCAS(&g_attn_paged_error, 0, code); } };
     auto wait = [&](uint64_t *bar, uint32_t parity, int code) {              // by a warp
@@ -205,6 +215,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
             auto load = [&](Cursor &c, uint8_t *dst, const CUtensorMap *map, uint64_t *bar, uint32_t more_bytes) {
                 if (elect_one()) mbar_expect_tx(bar, KV_BYTES + more_bytes);
                 __syncwarp();
+#pragma unroll 1
                 for (uint32_t i = 0; i < pieces; ++i) {
                     const int y = __shfl_sync(0xffffffffu, c.rows, c.j * pieces + i - c.base);
                     if (elect_one())
@@ -275,8 +286,8 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
             for (uint32_t n = 0, i = 0; ok && tile_at(t, n, ok); ++n) {
                 const uint32_t nblk = keys_of(t).chunks;
                 for (uint32_t jb = 0; jb < nblk; ++jb, ++i) {
-                    if (i >= 1 && !(ok = wait(bar_sfree, (i - 1) & 1, 4))) break;        // S_i-1 is in registers
                     if (!(ok = wait(bar_k + (i & 1), (i >> 1) & 1, 3))) break;           // K_i (and Q with a tile's first) has landed
+                    if (i >= 2 && !(ok = wait(bar_o + (i & 1), (i - 2 >> 1) & 1, 2))) break;         // P V_i-2: the buffer is free
                     if (elect_one()) {
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint8_t *Ki = Ks + (i & 1) * KV_BYTES;
@@ -284,9 +295,9 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
                         for (uint32_t kb = 0; kb < KB; ++kb) {
                             const uint64_t dq = umma_desc(smem_u32(Qs + kb * (BQ * 128))), dk = umma_desc(smem_u32(Ki + kb * (BKV * 128)));
 #pragma unroll
-                            for (uint32_t k = 0; k < 4; ++k) umma(tmem_S, dq + 2 * k, dk + 2 * k, idesc_s, (kb | k) != 0);
+                            for (uint32_t k = 0; k < 4; ++k) umma(tmem_S + (i & 1) * BKV, dq + 2 * k, dk + 2 * k, idesc_s, (kb | k) != 0);
                         }
-                        umma_commit(bar_s);
+                        umma_commit(bar_s + (i & 1));
                         umma_commit(bar_kfree + (i & 1));                            // its completion also frees the K stage
                     }
                     __syncwarp();
@@ -315,10 +326,12 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
                         const uint32_t past = clip(last_pos + 1), from = min(past, clip(keys.low)), head = min(from, clip(a.sinks)), sure = max(from, min(past, clip(t.pos + 1)));
                         const uint32_t near = max(from, min(past, clip(a.sinks))), far = a.window && last_pos >= a.window ? max(near, min(past, clip(last_pos - a.window + 1))) : near;
                         auto rows_of = [&](uint32_t r0, uint32_t r1, auto &&f) {         // f of every 16 bytes of rows [r0, r1)
+#pragma unroll 1
                             for (uint32_t e = lane; e < (r1 - r0) * KB * 8 && r1 > r0; e += 32) f(reinterpret_cast<uint4 *>(Vs + st * KV_BYTES + (e / 8 % KB) * (BKV * 128) + (r0 + e / (KB * 8)) * 128 + e % 8 * 16));
                         };
                         auto zero = [&](uint4 *at) { *at = make_uint4(0u, 0u, 0u, 0u); };
                         steps = 0;
+#pragma unroll 1
                         for (uint32_t k = 0; k < 4; ++k) if (16 * k < head || (16 * k + 16 > from && 16 * k < past)) steps |= 1u << k;
                         // (of steps that are left out nothing is read)
                         rows_of(past, min(BKV, (past + 15) / 16 * 16), zero);
@@ -356,7 +369,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
                         const uint64_t dv = umma_desc_mn(smem_u32(Vs + st * KV_BYTES), BKV * 128);
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k)                             // 16 keys per step: 8 columns of P, 2048 B of V rows
-                            if (steps >> k & 1) umma_ts(tmem_O, tmem_P + st * 32 + 8 * k, dv + 128 * k, idesc_o, jb != 0 || (steps & ((1u << k) - 1)) != 0);
+                            if (steps >> k & 1) umma_ts(tmem_O, tmem_S + st * BKV + 8 * k, dv + 128 * k, idesc_o, jb != 0 || (steps & ((1u << k) - 1)) != 0);
                         umma_commit(bar_o + st);
                     }
                     __syncwarp();
@@ -377,74 +390,86 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
             const uint32_t nblk = keys.chunks, qpos = t.pos + min(tok, t.tokens - 1);    // padding rows take the last token's mask
             float m_ref = -FLT_MAX, lrow = 0.f;                              // exponent reference and running sum of this row
             for (uint32_t jb = 0; jb < nblk; ++jb) {
-                const uint32_t i = i0 + jb, key0 = keys.chunk(jb) * BKV;
-                if (!(ok = wait(bar_s, i & 1, 1))) break;
-                float s[BKV];
+                const uint32_t i = i0 + jb, key0 = keys.chunk(jb) * BKV, buffer = tmem_S + lane_addr + (i & 1) * BKV;
+                if (!(ok = wait(bar_s + (i & 1), (i >> 1) & 1, 1))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                tmem_ld64(tmem_S + lane_addr, s);
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                mbar_arrive(bar_sfree);
+                uint64_t hidden = 0;                                         // a bit per key that is: behind the row, or before its window and none of the first positions, or of no page
                 if (t.missing || !whole(t, key0)) {
-                    // a bit per key that is hidden: behind the row, or before its window and none of the first positions, or of no page
                     auto below = [&](int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; };       // the first n keys of the block
                     const uint32_t low = a.window && qpos >= a.window ? qpos - a.window + 1 : 0;
-                    uint64_t hidden = ~below((int)(qpos - key0) + 1) | (below((int)(low - key0)) & ~below((int)(min(a.sinks, 0x7fffffffu) - key0)));
+                    hidden = ~below((int)(qpos - key0) + 1) | (below((int)(low - key0)) & ~below((int)(min(a.sinks, 0x7fffffffu) - key0)));
                     if (t.missing)
-                        for (uint32_t e = 0; e < 4; ++e) if (page_at(t, key0 + e * 16) >= a.n_pages) hidden |= 0xffffull << e * 16;       // (no page begins inside 16 keys)
-                    const uint32_t h0 = (uint32_t)hidden, h1 = (uint32_t)(hidden >> 32);
-#pragma unroll
-                    for (uint32_t e = 0; e < BKV; ++e)
-                        if ((e < 32 ? h0 : h1) >> (e % 32) & 1) s[e] = -INFINITY;
-                }
-                // The exponent reference m_ref is the row max of the tile's block 0, moved only where a block's sum says that a score lies more than about 2^40 above it (or overflowed).  A row
-                // that sees nothing of block 0 has the lowest finite reference: its sums are 0, and the first finite score moves it.  (Everything stands here once: with the exponentials and
-                // masks unrolled in several places, warps waited for instructions.)
-                uint32_t w[BKV / 2];
-                float lblk;
-                for (bool move = jb == 0;;) {
-                    if (move) {                                              // the row max of the scaled scores (scale > 0: max commutes with it)
-                        float m0 = max3(s[0], s[1], s[2]), m1 = max3(s[3], s[4], s[5]);
-#pragma unroll
-                        for (uint32_t e = 6; e + 3 < BKV; e += 4) { m0 = max3(m0, s[e], s[e + 1]); m1 = max3(m1, s[e + 2], s[e + 3]); }
-                        const float m_new = fmaxf(m_ref, max3(m0, m1, fmaxf(s[BKV - 2], s[BKV - 1])) * a.sl2), alpha = ex2(m_ref - m_new);
-                        m_ref = m_new;
-                        if (jb) {
-                            if (!(ok = wait(bar_o + (i - 1 & 1), (i - 1 >> 1) & 1, 2))) break;       // P V_{i-1}: nothing is accumulating into O
-                            lrow *= alpha;
-                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-                            for (uint32_t h = 0; h < DH / 32; ++h) {
-                                float v[32];
-                                uint32_t u[32];
-                                tmem_ld32(tmem_O + lane_addr + h * 32, v);
+                        for (uint32_t e = 0; e < 4; ++e) if (page_at(t, key0 + e * 16) >= a.n_pages) hidden |= 0xffffull << e * 16;       // (no page begins inside 16 keys)
+                }
+                const bool masked = __any_sync(0xffffffffu, hidden != 0);
+                // Half a block at a time, by the same code: with all of a block unrolled, in several places, warps waited for instructions.
+#pragma unroll 1
+                for (uint32_t half = 0; half < 2; ++half) {
+                    float s[32];
+                    tmem_ld32(buffer + half * 32, s);
+                    if (masked) {
+                        const uint32_t h = half ? (uint32_t)(hidden >> 32) : (uint32_t)hidden;
 #pragma unroll
-                                for (uint32_t e = 0; e < 32; ++e) u[e] = __float_as_uint(v[e] * alpha);
-                                tmem_st32(tmem_O + lane_addr + h * 32, u);
+                        for (uint32_t e = 0; e < 32; ++e) if (h >> e & 1) s[e] = -INFINITY;
+                    }
+                    // The exponent reference m_ref is the row's maximum of the tile's first keys, moved only where a sum says that a score lies more than about 2^40 above it (or overflowed).  A
+                    // row that sees nothing of the first ones has the lowest finite reference: its sums are 0, and the first finite score moves it.
+                    uint32_t w[16];
+                    float sum;
+                    for (bool move = (jb | half) == 0;;) {
+                        if (move) {                                          // the maximum of the scaled scores (scale > 0: it commutes with it)
+                            float m0 = max3(s[0], s[1], s[2]), m1 = max3(s[3], s[4], s[5]);
+#pragma unroll
+                            for (uint32_t e = 6; e + 3 < 32; e += 4) { m0 = max3(m0, s[e], s[e + 1]); m1 = max3(m1, s[e + 2], s[e + 3]); }
+                            const float m_new = fmaxf(m_ref, max3(m0, m1, fmaxf(s[30], s[31])) * a.sl2), alpha = ex2(m_ref - m_new);
+                            m_ref = m_new;
+                            lrow *= alpha;
+                            if (half) {                                      // the first half's weights
+                                uint32_t v[16];
+                                tmem_wait_st();
+                                tmem_ld16(buffer, v);
+#pragma unroll
+                                for (uint32_t e = 0; e < 16; ++e) { const __nv_bfloat162 two = *reinterpret_cast<__nv_bfloat162 *>(&v[e]), x = __floats2bfloat162_rn(__low2float(two) * alpha, __high2float(two) * alpha); v[e] = *reinterpret_cast<const uint32_t *>(&x); }
+                                tmem_st16(buffer, v);
+                            }
+                            if (jb) {
+                                if (!(ok = wait(bar_o + (i - 1 & 1), (i - 1 >> 1) & 1, 2))) break;   // P V_{i-1}: nothing is accumulating into O
+                                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+#pragma unroll 1
+                                for (uint32_t h = 0; h < DH / 32; ++h) {
+                                    float v[32];
+                                    uint32_t u[32];
+                                    tmem_ld32(tmem_O + lane_addr + h * 32, v);
+#pragma unroll
+                                    for (uint32_t e = 0; e < 32; ++e) u[e] = __float_as_uint(v[e] * alpha);
+                                    tmem_st32(tmem_O + lane_addr + h * 32, u);
+                                }
                             }
                         }
-                    }
-                    // w = exp2(S * scale - m) as bf16 pairs, and their fp32 sum
-                    const uint64_t sc2 = pack2(a.sl2, a.sl2), nm2 = pack2(-m_ref, -m_ref);
-                    uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
+                        // w = exp2(S * scale - m) as bf16 pairs, and their fp32 sum
+                        const uint64_t sc2 = pack2(a.sl2, a.sl2), nm2 = pack2(-m_ref, -m_ref);
+                        uint64_t acc0 = pack2(0.f, 0.f), acc1 = acc0;
 #pragma unroll
-                    for (uint32_t e = 0; e < BKV / 2; ++e) {
-                        float x0, x1;
-                        unpack2(fma2(pack2(s[2 * e], s[2 * e + 1]), sc2, nm2), x0, x1);
-                        const float p0 = ex2(x0), p1 = ex2(x1);              // a masked score is -inf: p = 0
-                        if (e & 1) acc1 = add2(acc1, pack2(p0, p1)); else acc0 = add2(acc0, pack2(p0, p1));
-                        __nv_bfloat162 pk = __floats2bfloat162_rn(p0, p1);   // .x = p0 in the lower half
-                        w[e] = *reinterpret_cast<uint32_t *>(&pk);
+                        for (uint32_t e = 0; e < 16; ++e) {
+                            float x0, x1;
+                            unpack2(fma2(pack2(s[2 * e], s[2 * e + 1]), sc2, nm2), x0, x1);
+                            const float p0 = ex2(x0), p1 = ex2(x1);          // a masked score is -inf: p = 0
+                            if (e & 1) acc1 = add2(acc1, pack2(p0, p1)); else acc0 = add2(acc0, pack2(p0, p1));
+                            __nv_bfloat162 pk = __floats2bfloat162_rn(p0, p1);   // .x = p0 in the lower half
+                            w[e] = *reinterpret_cast<uint32_t *>(&pk);
+                        }
+                        float l0, l1;
+                        unpack2(add2(acc0, acc1), l0, l1);
+                        sum = l0 + l1;
+                        if (move || !__any_sync(0xffffffffu, !(sum <= 0x1p40f))) break;
+                        move = true;
                     }
-                    float l0, l1;
-                    unpack2(add2(acc0, acc1), l0, l1);
-                    lblk = l0 + l1;
-                    if (move || !__any_sync(0xffffffffu, !(lblk <= 0x1p40f))) break;
-                    move = true;
+                    if (!ok) break;
+                    lrow += sum;
+                    tmem_st16(buffer + half * 16, w);                        // over scores that have been read
                 }
                 if (!ok) break;
-                lrow += lblk;
-                if (i >= 2 && !(ok = wait(bar_o + (i & 1), (i - 2 >> 1) & 1, 2))) break;      // P V_{i-2}: this P buffer is free
-                tmem_st32(tmem_P + (i & 1) * 32 + lane_addr, w);
                 tmem_wait_st();
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 mbar_arrive(bar_p + (i & 1));
