@@ -503,7 +503,7 @@ extern "C" int tgp_k_attn_paged(const void *qb, const void *k_pages, const void 
     const auto bits = [](auto... p) { return (reinterpret_cast<uintptr_t>(p) | ...); };
     if ((bits(qb, k_pages, v_pages, ob, scratch_dev) & 15u) || (bits(table_dev, start_dev, end_dev) & 3u)) return TGP_E_INVAL;
     if (B > TGP_PAGED_MAX_B || cfg->max_len > 0x7fffffffu || T > 0x7fffffffu || cfg->Hq > (1u << 16) || (uint64_t)n_pages * cfg->TK > 0x7fffffffu ||
-        (uint64_t)n_pages * cfg->TK * cfg->Hkv > 0x7fffff00u || (uint64_t)std::min(B, GROUP) * ((kv_max + 15) / 16) * cfg->Hkv > 0x7fffffffu) return TGP_E_TOO_LARGE;
+        (uint64_t)n_pages * cfg->TK * cfg->Hkv > 0x7fffff00u || (uint64_t)B * ((kv_max + 15) / 16) * cfg->Hkv > 0x7fffffffu) return TGP_E_TOO_LARGE;
     if (!B || !T || !q_max || !kv_max) return TGP_OK;
     q_max = std::min(q_max, T);
     const uint32_t G = cfg->Hq / cfg->Hkv;
