@@ -53,7 +53,8 @@ template <int DH, int MT> __host__ __device__ constexpr uint32_t fixed_smem() { 
 template <int DH, int MT> __host__ __device__ constexpr uint32_t slot_floats() { return MT * 16 * (DH + 2); }
 
 struct FewArgs {
-    TgpPagedAttn a; float *parts; u64 *counters; uint32_t *tiles;           // tiles: the other kernel's counter, which begins at 0
+    TgpPagedAttn a; float *parts; u64 *counters;
+    bool beside;                                                            // launched behind the prompts' kernel of the same call
     uint32_t magic, shift;                                                  // a chunk's page: chunk * magic >> shift (chunks are below 2^27)
     uint32_t per_token;                                                     // a row's token: row * per_token >> 16 (rows are below 32)
     __device__ __forceinline__ uint32_t page_of_chunk(uint32_t chunk) const { return (uint32_t)((u64)chunk * magic >> shift); }
@@ -61,7 +62,11 @@ struct FewArgs {
 
 template <int DH, int MT>
 __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) tgp_attn_paged_few_kernel(const FewArgs f) {
-    pdl_enter();
+    // Beside the prompts' kernel: it is launched once that one has waited for what both read, and their rows are different ones.  Then it waits only before it ends, so that its successor waits for both.
+    // (Between other kernels, one after the other -> beside: eight sequences, two of them chunks of 100 tokens, 38 -> 27 us; twelve, two of 509, 70 -> 71; 96, sixteen of 40, 125 -> 128; prompts alone
+    // 188 -> 189.  From cold caches 46 -> 31, 78 -> 72, 127 -> 120 and 207 -> 201.)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!f.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
     const TgpPagedAttn &a = f.a;
     extern __shared__ __align__(16) uint8_t few_raw[];
     uint8_t *few_sm = few_raw + (-(uint32_t)__cvta_generic_to_shared(few_raw) & 255u);       // stages begin on 256 bytes
@@ -72,7 +77,6 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     uint4 *seqs = reinterpret_cast<uint4 *>(shared_u + 16);                 // [B] first row, rows, length, and chunks of the sequences up to this one, all KV heads
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
 
-    if (blockIdx.x == 0 && tid == 0) *f.tiles = 0;
     // ---- the line of all chunks ----
     {
         uint32_t before = 0;
@@ -100,7 +104,10 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         }
     }
     const uint32_t N = seqs[a.B - 1].w, ctas = min(gridDim.x, (N + MIN_STRETCH - 1) / MIN_STRETCH);
-    if (blockIdx.x >= ctas) return;
+    if (blockIdx.x >= ctas) {
+        if (f.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     const uint32_t each_cta = N / ctas, longer = N - each_cta * ctas;       // the first `longer` stretches have a chunk more
     auto stretch = [&](uint32_t cta) { return cta * each_cta + min(cta, longer); };
     const uint32_t line_lo = stretch(blockIdx.x), line_hi = stretch(blockIdx.x + 1);
@@ -461,6 +468,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         seg_lo = seg_hi;
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (f.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // CTAs that the GPU holds at a time
@@ -474,6 +482,7 @@ int launch_few(FewArgs f, cudaStream_t st) {
         f.a.b0 = b0;
         f.a.B = std::min(GROUP, B - b0);
         if (int rc = launch(tgp_attn_paged_few_kernel<DH, MT>, dim3(few_ctas<DH, MT>()), dim3(WARPS * 32), fixed_smem<DH, MT>() + f.a.B * 16, st, 1, f)) return rc;
+        f.beside = false;                                                   // the next launch takes the same partials
     }
     return TGP_OK;
 }
@@ -518,13 +527,13 @@ extern "C" int tgp_k_attn_paged(const void *qb, const void *k_pages, const void 
     f.magic = (uint32_t)(((1ull << f.shift) + chunks - 1) / chunks);
     f.per_token = (65536 + G - 1) / G;
     f.counters = (u64 *)scratch_dev;
-    f.tiles = (uint32_t *)(f.counters + (uint64_t)B * cfg->Hkv);
     f.parts = (float *)((uint8_t *)scratch_dev + counter_bytes(cfg, B));
     // one tile of 16 rows where all sequences fit it, else two; sequences of more rows are the other kernel's
     const bool one = (uint64_t)q_max * G <= 16;
     f.a.few = one ? 16 : 32;
-    if (int rc = cfg->Dh == 64 ? (one ? launch_few<64, 1>(f, (cudaStream_t)stream) : launch_few<64, 2>(f, (cudaStream_t)stream))
-                               : (one ? launch_few<128, 1>(f, (cudaStream_t)stream) : launch_few<128, 2>(f, (cudaStream_t)stream))) return rc;
-    if ((uint64_t)q_max * G <= f.a.few) return TGP_OK;
-    return tgpk_attn_paged_many(f.a, cfg->Dh, f.tiles, (cudaStream_t)stream);
+    f.beside = (uint64_t)q_max * G > f.a.few;
+    if (f.beside)
+        if (int rc = tgpk_attn_paged_many(f.a, cfg->Dh, f.counters + (uint64_t)B * cfg->Hkv, (cudaStream_t)stream)) return rc;
+    return cfg->Dh == 64 ? (one ? launch_few<64, 1>(f, (cudaStream_t)stream) : launch_few<64, 2>(f, (cudaStream_t)stream))
+                               : (one ? launch_few<128, 1>(f, (cudaStream_t)stream) : launch_few<128, 2>(f, (cudaStream_t)stream));
 }

@@ -65,5 +65,5 @@ __device__ __forceinline__ uint32_t tgp_paged_arrive(unsigned long long *counter
     return (uint32_t)was + 1;
 }
 
-// sequences of more than a.few rows * G, on tcgen05 (tgp_attn_paged_sm100.cu); counter: a word that is 0
-int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, uint32_t *counter, cudaStream_t st);
+// sequences of more than a.few rows * G, on tcgen05 (tgp_attn_paged_sm100.cu); counter: as above, of tiles begun.  Its successor on the stream is launched when what the kernel waits for has completed.
+int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, unsigned long long *counter, cudaStream_t st);

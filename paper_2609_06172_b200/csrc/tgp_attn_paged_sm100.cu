@@ -47,7 +47,7 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
                  "r"(r[15]) : "memory");
 }
 
-struct ManyArgs { TgpPagedAttn a; uint32_t *counter; uint32_t tokens, piece; int none; bool wide; };        // tiles begun beyond the CTAs' first ones, 0 at the start; tokens of a tile, rows of a piece, a row outside the maps; output on 32 bytes
+struct ManyArgs { TgpPagedAttn a; unsigned long long *counter; uint32_t tokens, piece; int none; bool wide; };      // tiles begun beyond the CTAs' first ones; tokens of a tile, rows of a piece, a row outside the maps; output on 32 bytes
 
 // what a CTA works on: `tokens` tokens of a sequence and KV head, the first at row `row` and position `pos` (no tokens: the end)
 struct Tile { uint32_t row, pos, tokens, hk, b, missing; };
@@ -98,7 +98,6 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     if (warp == 4) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(256u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // not before the allocation: see tgp_sm100.cuh
     }
     // rows of Q behind the box's: zeros, so that they do not slow the softmax down
     for (uint32_t i = args.tokens * a.G * KB * 8 + tid; i < BQ * KB * 8; i += THREADS)
@@ -107,6 +106,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");         // not before the TMEM allocation (see tgp_sm100.cuh), nor before the wait: the few-rows kernel relies on it
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t tmem_S = tmem_base, tmem_O = tmem_base + 2 * BKV;         // S: two buffers of 64 columns; P_i (32 columns of bf16 pairs) takes the first of S_i's
@@ -180,13 +180,19 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
                     }
                     t.missing = __any_sync(0xffffffffu, missing);
                 }
-                if (n >= TILES && !(ok = wait(bar_tfree + n % TILES, n / TILES - 1 & 1, 4))) break;
-                if (lane == 0) { tiles[n % TILES] = t; mbar_arrive(bar_tile + n % TILES); }
+                if (n >= TILES) ok = wait(bar_tfree + n % TILES, n / TILES - 1 & 1, 4);
+                if (ok && lane == 0) { tiles[n % TILES] = t; mbar_arrive(bar_tile + n % TILES); }
                 __syncwarp();
                 if (!live) break;
-                uint32_t next = 0;
-                if (lane == 0) next = gridDim.x + atomicAdd(args.counter, 1u);
-                item = __shfl_sync(0xffffffffu, next, 0);
+                // Every item is followed by one number, so the last one is number `items`.  (A CTA that gave up takes numbers all the same, to the end: the counter has to be put back.)
+                do {
+                    uint32_t next = 0;
+                    if (lane == 0) {
+                        next = tgp_paged_arrive(args.counter);
+                        if (next == items) atomicExch(args.counter, 0ull);
+                    }
+                    item = gridDim.x + __shfl_sync(0xffffffffu, next, 0) - 1;
+                } while (!ok && item < items);
             }
         } else if (warp == 5) {
             // ======================= TMA warp =======================
@@ -557,7 +563,7 @@ int launch_many(const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v
 
 }  // namespace
 
-int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, uint32_t *counter, cudaStream_t st) {
+int tgpk_attn_paged_many(const TgpPagedAttn &a, uint32_t Dh, unsigned long long *counter, cudaStream_t st) {
     ManyArgs args{a, counter, BQ / a.G, BKV, 0, reinterpret_cast<uintptr_t>(a.o) % 32 == 0};
     while (a.P % args.piece) args.piece /= 2;                                // (a page holds a multiple of 16 positions)
     const uint64_t rows = (uint64_t)a.n_pages * a.Hkv * a.P;
