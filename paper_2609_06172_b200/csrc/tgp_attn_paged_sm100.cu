@@ -98,6 +98,8 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     if (warp == 4) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(256u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");                  // the few-rows kernel reads, without a wait of its own, what this one waits for
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // not before the allocation: see tgp_sm100.cuh
     }
     // rows of Q behind the box's: zeros, so that they do not slow the softmax down
     for (uint32_t i = args.tokens * a.G * KB * 8 + tid; i < BQ * KB * 8; i += THREADS)
@@ -106,7 +108,6 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");         // not before the TMEM allocation (see tgp_sm100.cuh), nor before the wait: the few-rows kernel relies on it
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t tmem_S = tmem_base, tmem_O = tmem_base + 2 * BKV;         // S: two buffers of 64 columns; P_i (32 columns of bf16 pairs) takes the first of S_i's
