@@ -23,7 +23,7 @@ using namespace tgp_launch;
 using tgp_sm100::cluster_arrive; using tgp_sm100::cluster_sync_all; using tgp_sm100::cluster_wait;
 
 constexpr uint32_t STAT_THREADS = 256, STAT_WARPS = STAT_THREADS / 32, PER_THREAD = 16, PART = STAT_THREADS * PER_THREAD, RING = 3;       // PART: logits of a part of a row
-constexpr uint32_t DRAW_THREADS = 256, NW = DRAW_THREADS / 32, CLUSTER_MAX = 8, BATCH = 8;
+constexpr uint32_t DRAW_THREADS = 256, NW = DRAW_THREADS / 32, CLUSTER_MAX = 8, BATCH = 8, UNITS = 128;        // UNITS: of a warp's segment, at most
 constexpr double LOG2E = 1.4426950408889634074;
 constexpr int OCTAVE = 128, COPIES = 16, TABLE = OCTAVE * COPIES; // entries of the table of powers of two, and copies of it: a lane reads its own, without bank conflicts (with one, these took half of the time)
 
@@ -31,7 +31,7 @@ struct Stat { double sum; float top; uint32_t at; };             // of a part of
 
 struct VerifyArgs {
     const float *x, *y; const int32_t *tokens, *start; const float *u, *u_draw, *temperature; int32_t *out, *n_out;
-    uint32_t B, T, V, parts, per;                                // parts of a row in the first kernel; logits of a CTA in the second
+    uint32_t B, T, V, parts, per, unit;                          // parts of a row in the first kernel; logits of a CTA in the second, and of a unit, 32 * BATCH at a time
     Stat *stats;                                                 // [2][T][parts]: target, draft
     double c[4];                                                 // of Weights
 };
@@ -122,7 +122,21 @@ __device__ __forceinline__ Seq seq_of(const VerifyArgs &a, uint32_t b) {
 }
 
 // The rows that the first kernel adds up, one line of them: of each sequence the target's, then the draft's that something was drawn from - none behind the last row, none where the likeliest token is taken.
-struct LineSeq { Seq s; uint32_t upto; };                        // upto: rows of the sequences up to this one
+// A part costs 1 where the likeliest token is asked for, else 2 (a part of weights took twice as long: with as many parts each, stretches of a mixed batch ended after 17 to 38 us).
+struct LineSeq { Seq s; uint32_t upto, cost; };                  // of the sequences up to this one: rows, and rows times the cost of their parts
+__device__ __forceinline__ uint32_t cost_of(const Seq &s) { return s.rate != 0.0 ? 2 : 1; }
+
+// the first sequence whose value exceeds v
+template <class F> __device__ __forceinline__ uint32_t first_above(uint32_t B, uint32_t v, F &&value) {
+    uint32_t lo = 0, hi = B - 1;
+    while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (value(mid) > v) hi = mid; else lo = mid + 1; }
+    return lo;
+}
+// the first part, in the line of all, that begins at cost c or behind it
+__device__ __forceinline__ uint32_t part_at(const LineSeq *line, uint32_t B, uint32_t parts, uint32_t c) {
+    const uint32_t b = first_above(B, c / parts, [&](uint32_t i) { return line[i].cost; }), w = cost_of(line[b].s), rows = b ? line[b - 1].upto : 0, cost = b ? line[b - 1].cost : 0;
+    return min(line[b].upto * parts, rows * parts + (c - cost * parts + w - 1) / w);
+}
 
 // A place in the line of all parts of these rows: part `part` of row k of sequence b, `left` of them up to a stretch's end.
 struct Place {
@@ -130,10 +144,8 @@ struct Place {
     __device__ __forceinline__ Place(const LineSeq *line, uint32_t B, uint32_t parts, uint32_t step, uint32_t left) : left(left) {
         const uint32_t row = step / parts;
         part = step - row * parts;
-        uint32_t lo = 0, hi = B - 1;                             // the first sequence that ends behind the row
-        while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (line[mid].upto > row) hi = mid; else lo = mid + 1; }
-        b = lo;
-        k = row - (lo ? line[lo - 1].upto : 0);
+        b = first_above(B, row, [&](uint32_t i) { return line[i].upto; });
+        k = row - (b ? line[b - 1].upto : 0);
     }
     __device__ __forceinline__ bool drafts(const LineSeq *line) const { return k >= line[b].s.n; }
     __device__ __forceinline__ uint32_t row(const LineSeq *line) const { const Seq &s = line[b].s; return s.first + (k < s.n ? k : k - s.n); }
@@ -158,41 +170,46 @@ __device__ __forceinline__ void cp_async(uint32_t dst, const float *src, bool wi
 // row's first part in the stretch, the others are empty.  WIDE: rows that begin on 16 bytes, copied 16 at a time, else 4.
 template <bool WIDE>
 __global__ void __launch_bounds__(STAT_THREADS, 3) tgp_verify_stat_kernel(const VerifyArgs a) {
-    pdl_enter();
     __shared__ double table_of_all[TABLE], sh_s[2][STAT_WARPS];
     __shared__ float sh_m[2][STAT_WARPS];
     __shared__ uint32_t sh_i[2][STAT_WARPS];
     extern __shared__ __align__(16) float ring[];                // [RING][PART], then [B] sequences
     LineSeq *line = reinterpret_cast<LineSeq *>(ring + RING * PART);
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    uint32_t rows = 0;
+    const double *table = fill_table(table_of_all);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");          // not before the wait: the draw's kernel reads the call's arguments without one of its own
+    uint32_t rows = 0, cost = 0;
     for (uint32_t b0 = 0; b0 < a.B; b0 += STAT_THREADS) {
         Seq s{0, 0, 0.0, 0.0};
         if (b0 + tid < a.B) s = seq_of(a, b0 + tid);
         uint32_t upto = s.n + (s.n && a.y && s.rate != 0.0 ? s.n - 1 : 0);
+        uint32_t costs = upto * cost_of(s);
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
-        if (lane == 31) sh_i[0][warp] = upto;
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o), c = __shfl_up_sync(0xffffffffu, costs, o); if (lane >= o) { upto += v; costs += c; } }
+        if (lane == 31) { sh_i[0][warp] = upto; sh_i[1][warp] = costs; }
         __syncthreads();
-        uint32_t all = 0;
+        uint32_t all = 0, all_cost = 0;
 #pragma unroll
-        for (uint32_t w = 0; w < STAT_WARPS; ++w) { if (w < warp) upto += sh_i[0][w]; all += sh_i[0][w]; }
-        if (b0 + tid < a.B) line[b0 + tid] = {s, rows + upto};
+        for (uint32_t w = 0; w < STAT_WARPS; ++w) { if (w < warp) { upto += sh_i[0][w]; costs += sh_i[1][w]; } all += sh_i[0][w]; all_cost += sh_i[1][w]; }
+        if (b0 + tid < a.B) line[b0 + tid] = {s, rows + upto, cost + costs};
         rows += all;
+        cost += all_cost;
         __syncthreads();
     }
-    const double *table = fill_table(table_of_all);
-    __syncthreads();
-    const uint32_t steps = rows * a.parts, ctas = min(gridDim.x, steps);
+    const uint32_t costs = cost * a.parts, ctas = min(gridDim.x, (costs + 1) / 2);
     if (blockIdx.x >= ctas) return;
-    const uint32_t each = steps / ctas, longer = steps - each * ctas, lo = blockIdx.x * each + min(blockIdx.x, longer);
+    const uint32_t each = costs / ctas, longer = costs - each * ctas;
+    auto begin_of = [&](uint32_t cta) { return cta == ctas ? rows * a.parts : part_at(line, a.B, a.parts, cta * each + min(cta, longer)); };
+    const uint32_t lo = begin_of(blockIdx.x), steps = begin_of(blockIdx.x + 1) - lo;
+    if (!steps) return;
 
     // element j of this thread: of four neighbours at a time, or of every 256th
     constexpr uint32_t W = WIDE ? 4 : 1;
     const uint32_t mine = tid * W;
     auto offset = [&](uint32_t j) { return j / W * (STAT_THREADS * W) + j % W; };
     const uint32_t ring_u = (uint32_t)__cvta_generic_to_shared(ring) + mine * 4;
-    Place now(line, a.B, a.parts, lo, each + (blockIdx.x < longer)), ahead = now;
+    Place now(line, a.B, a.parts, lo, steps), ahead = now;
     auto logits_of = [&](const Place &p) { return (p.drafts(line) ? a.y : a.x) + (size_t)p.row(line) * a.V + mine; };
     const float *source = logits_of(ahead);
     uint32_t slot = 0;
@@ -361,24 +378,27 @@ __device__ __forceinline__ Found scan_of(const double *v, uint32_t n, double tar
 constexpr uint32_t KEPT = 32;                                    // rows that are judged at a time
 
 __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const VerifyArgs a) {
-    pdl_enter();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ uint32_t sh_refused;                              // first row, counted from the sequence's first, whose token is not taken
     __shared__ Stat kept[2][KEPT];                               // target, draft
     __shared__ Scaled sh_w[2];
     __shared__ double table_of_all[TABLE];
-    __shared__ double seg[CLUSTER_MAX * NW], sub[NW];            // sums of the segments of the vocabulary, one per warp of the cluster, in every CTA; of the parts of one
+    __shared__ double seg[CLUSTER_MAX * NW], sub[NW][UNITS];     // sums of the segments of the vocabulary, one per warp of the cluster, in every CTA; of this CTA's ones' units
     uint32_t rank, ctas;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = blockIdx.x / ctas;
     if (tid < CLUSTER_MAX * NW) seg[tid] = 0.0;
     cluster_arrive();                                            // (the first access to another CTA's memory waits for it to run)
-    const Seq s = seq_of(a, b);
     const double *table = fill_table(table_of_all);
+    // what the sums are not needed for is read while the first kernel, which has waited for it, still runs (no rows: there is none)
+    if (!a.T) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Seq s = seq_of(a, b);
     if (tid == 0) sh_refused = s.n ? s.n - 1 : 0;
     __syncthreads();
     // ---- which rows take their token, every CTA for itself: a warp joins a row of the target or of the draft, then a thread judges a row ----
     uint32_t group = 0;
+    bool waited = false;
     for (; group < s.n; group += KEPT) {
         const uint32_t i = group + tid, r = s.first + i;         // (of the threads that judge)
         const bool judge = tid < KEPT && i + 1 < s.n, drawn = judge && a.y && s.rate != 0.0;
@@ -386,6 +406,7 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
         const bool real = d < a.V && s.rate != 0.0;
         const float x_d = real ? a.x[(size_t)r * a.V + d] : 0.f, y_d = real && drawn ? a.y[(size_t)r * a.V + d] : 0.f;
         const double u = judge ? fmin(fmax((double)a.u[r], 0.0), 1.0) : 0.0;
+        if (!waited) { asm volatile("griddepcontrol.wait;" ::: "memory"); waited = true; }
         for (uint32_t k = warp; k < 2 * KEPT; k += NW) {
             const uint32_t row = group + k / 2, draft = k % 2;
             if (row < s.n && !(draft && (row + 1 == s.n || !a.y || s.rate == 0.0))) {
@@ -407,6 +428,7 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
         __syncthreads();
         if (sh_refused < group + KEPT) break;
     }
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t refused = sh_refused, r = s.first + refused;
     const bool last = refused + 1 == s.n, two = s.n && !last && a.y && s.rate != 0.0;
     const float top_x = s.n ? kept[0][refused - group].top : -INFINITY;
@@ -444,21 +466,28 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
             for (uint32_t j = 0; j < N; ++j) if (i + j * 32 == d) w[j] = 0.0;
         }
     };
-    auto total_of = [&](uint32_t lo, uint32_t hi) {              // by a warp, the next logits on their way while these are weighed
-        double sum = 0.0, w[BATCH];
+    // by a warp, unit by unit, of which each one's sum is kept, the next logits on their way while these are weighed
+    auto total_of = [&](uint32_t lo, uint32_t hi) {
+        double all = 0.0, sum = 0.0, w[BATCH];
         float x[BATCH], y[BATCH], next_x[BATCH], next_y[BATCH];
         fetch(next_x, next_y, lo + lane, hi);
+        uint32_t n = 0, unit = 0;
         for (uint32_t i = lo + lane; i - lane < hi; i += 32 * BATCH) {
 #pragma unroll
             for (uint32_t j = 0; j < BATCH; ++j) { x[j] = next_x[j]; y[j] = next_y[j]; }
             if (i - lane + 32 * BATCH < hi) fetch(next_x, next_y, i + 32 * BATCH, hi);
             rest(x, y, w, i);
+            sum += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+            if (++n < a.unit && i - lane + 32 * BATCH < hi) continue;
 #pragma unroll
-            for (uint32_t j = 0; j < BATCH; ++j) sum += w[j];
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) sub[warp][unit] = sum;
+            all += sum;
+            sum = 0.0;
+            n = 0;
+            ++unit;
         }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        return sum;
+        return all;
     };
     cluster_wait();
     int32_t token = (int32_t)likeliest;                           // the likeliest, or token 0 of a row of nothing but -inf and NaN
@@ -485,31 +514,33 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
         target -= in_row.before;
         mine = found / NW == rank;
         if (!mine) return;
-        // ---- the segment, a sixteenth a warp, then the part that the rest of the target falls into ----
-        const uint32_t lo = min(end, first + found % NW * per_warp), hi = min(end, lo + per_warp), per_part = (hi - lo + NW - 1) / NW;
-        const uint32_t m_lo = min(hi, lo + warp * per_part), m_hi = min(hi, m_lo + per_part);
-        const double w = total_of(m_lo, m_hi);
-        if (lane == 0) sub[warp] = w;
-        __syncthreads();
-        const Found in_segment = scan_of(sub, NW, target);
-        const uint32_t part = in_segment.at;
+        // ---- the segment's warp: the unit, then the token that the rest of the target falls into ----
+        if (found % NW != warp) return;
+        const uint32_t lo = min(end, first + warp * per_warp), hi = min(end, lo + per_warp), tokens = a.unit * 32 * BATCH;
+        const Found in_segment = scan_of(sub[warp], (hi - lo + tokens - 1) / tokens, target);
         target -= in_segment.before;
-        if (part != warp) return;
-        if (!(sub[part] > target)) target = DBL_MAX;             // (rounding: the last token of the part that weighs anything)
+        const uint32_t m_lo = lo + in_segment.at * tokens, m_hi = min(hi, m_lo + tokens);
+        if (!(sub[warp][in_segment.at] > target)) target = DBL_MAX;          // (rounding: the last token of the unit that weighs anything)
         double upto = 0.0;
-        for (uint32_t i0 = m_lo; i0 < m_hi; i0 += 32) {
-            double one[1];
-            float x1[1], y1[1];
-            fetch(x1, y1, i0 + lane, m_hi);
-            rest(x1, y1, one, i0 + lane);
-            double w = one[0];
-            const uint32_t some = __ballot_sync(0xffffffffu, w > 0.0);
+        bool over = false;
+        for (uint32_t i0 = m_lo; i0 < m_hi && !over; i0 += 32 * BATCH) {
+            float x[BATCH], y[BATCH];
+            double w[BATCH];
+            fetch(x, y, i0 + lane, m_hi);
+            rest(x, y, w, i0 + lane);
+#pragma unroll 1
+            for (uint32_t j = 0; j < BATCH && !over; ++j) {
+                double v = w[0];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const double v = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += v; }
-            const uint32_t over = __ballot_sync(0xffffffffu, upto + w > target) & some;
-            if (some) token = (int32_t)(i0 + (over ? __ffs(over) - 1 : 31 - __clz(some)));
-            if (over) break;
-            upto += __shfl_sync(0xffffffffu, w, 31);
+                for (uint32_t k = 0; k + 1 < BATCH; ++k) w[k] = w[k + 1];
+                const uint32_t some = __ballot_sync(0xffffffffu, v > 0.0);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) { const double before = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += before; }
+                const uint32_t above = __ballot_sync(0xffffffffu, upto + v > target) & some;
+                if (some) token = (int32_t)(i0 + j * 32 + (above ? __ffs(above) - 1 : 31 - __clz(some)));
+                over = above != 0;
+                upto += __shfl_sync(0xffffffffu, v, 31);
+            }
         }
     } else if (!mine || warp) return;
     // ---- one warp writes the sequence's tokens ----
@@ -539,7 +570,9 @@ extern "C" int tgp_k_verify(const float *logits, const float *draft_logits, cons
     if (!B) return TGP_OK;
     uint32_t ctas = V > 4096 ? CLUSTER_MAX : 1;
     while (ctas > 1 && B * ctas > 2u * (uint32_t)tgpk_sms()) ctas /= 2;
-    const VerifyArgs a{logits, draft_logits, tokens_dev, start_dev, u_dev, u_draw_dev, temperature_dev, out_dev, n_out_dev, B, T, V, parts_of(V), (V + ctas - 1) / ctas, (Stat *)scratch_dev, {Weights::C0, Weights::C1, Weights::C2, Weights::C3}};
+    VerifyArgs a{logits, draft_logits, tokens_dev, start_dev, u_dev, u_draw_dev, temperature_dev, out_dev, n_out_dev, B, T, V, parts_of(V), (V + ctas - 1) / ctas, 0, (Stat *)scratch_dev, {Weights::C0, Weights::C1, Weights::C2, Weights::C3}};
+    const uint32_t per_warp = (a.per + NW - 1) / NW;
+    a.unit = (per_warp + UNITS * 32 * BATCH - 1) / (UNITS * 32 * BATCH);
     const uint64_t steps = (uint64_t)(draft_logits ? 2 * T : T) * a.parts;
     if (T) {
         const uintptr_t bits = reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(draft_logits) | (uintptr_t)V * 4;
