@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
         if (warp == 7) {
             // ======================= tiles: the first is the CTA's own, further ones are those that nobody has begun =======================
             uint32_t all = 0;                                                // tiles of all sequences
+#pragma unroll 4
             for (uint32_t i0 = 0; i0 < a.B; i0 += 32) {
                 uint32_t mine = 0;
                 if (i0 + lane < a.B) { const TgpPagedSeq s = tgp_paged_seq(a, i0 + lane); if (s.n && !s.idle && s.n * a.G > a.few) mine = (s.n + args.tokens - 1) / args.tokens; }
@@ -146,6 +147,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
             }
             const uint32_t items = all * a.Hkv;
             bool ok = true;
+            uint32_t i0 = 0, before = 0;                                     // 32 sequences, and the tiles before them: a CTA's items ascend, so they do, too
             for (uint32_t n = 0, item = blockIdx.x; ok; ++n) {
                 Tile t{0, 0, 0, 0, 0, 0};
                 const bool live = item < items;
@@ -153,8 +155,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
                     // A sequence's last tile (the longest) comes first, and the KV heads of a tile one after the other.
                     const uint32_t at = item / a.Hkv;
                     t.hk = item - at * a.Hkv;
-                    uint32_t before = 0;
-                    for (uint32_t i0 = 0; i0 < a.B; i0 += 32) {
+                    for (; i0 < a.B; i0 += 32) {
                         TgpPagedSeq s{0, 0, 0, false};
                         uint32_t mine = 0;
                         if (i0 + lane < a.B) { s = tgp_paged_seq(a, i0 + lane); if (s.n && !s.idle && s.n * a.G > a.few) mine = (s.n + args.tokens - 1) / args.tokens; }
