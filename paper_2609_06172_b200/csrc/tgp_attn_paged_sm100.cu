@@ -1,9 +1,11 @@
 // Attention of a ragged batch over a KV cache in pages: prompts, and drafted tokens of many heads, on the 5th-generation tensor cores (sm_100a).
 //
 // A CTA of eight warps owns 128 rows of one (sequence, KV head): neighbouring tokens x the query heads of the group, token by token, so that keys and values are fetched once for the whole
-// group and a few drafted tokens fill a tile.  The roles and their hand-over are those of the prefill over KV tiles (tgp_attn_sm100.cu):
-//   warps 0-3  softmax: thread t is row t and TMEM lane t;
-//   warp 4     issues S_j = Q K_j^T;  warp 6  issues O += P_j V_j;  warp 5  issues every TMA load;  warp 7  idle (completes the second warpgroup for setmaxnreg).
+// group and a few drafted tokens fill a tile.  CTAs stay, two to an SM, and take tiles as they become free:
+//   warps 0-3  softmax: thread t is row t and TMEM lane t;  the store of O;
+//   warp 4     issues S_j = Q K_j^T;  warp 6  issues O += P_j V_j, and sees to the values that not every row sees;  warp 5  issues every TMA load;
+//   warp 7     finds the next tiles, up to four ahead: the first is the CTA's own, further ones are numbered by a counter.
+// S has two buffers of 64 columns, and P_j, in bf16, takes the place of the first half of S_j: so S_j+1 is multiplied while S_j is exponentiated and P_j-1 V_j-1 added up.
 // K and V blocks of 64 keys arrive as pieces of up to 64 rows, none of which crosses a page; one tensor map covers all rows of the key pages and one all of the value pages, and
 // a piece behind the sequence, or of a page that is none, is asked for outside the map, which fills it with zeros.  The table's entries are read 32 pieces at a time, a lane each,
 // ahead of their loads.  Q is one box of [tokens][heads of the group][64].
@@ -12,6 +14,12 @@
 // end to the rows that see it.
 // P is rounded to bf16 for the second product.  Every mbarrier wait is bounded; a wait that runs out sets an error word (tgp_k_attn_status), every role leaves its loop, loads in flight are waited for, TMEM
 // is freed and nothing is stored.
+//
+// What bounds it: a block of 64 keys takes one CTA some 1670 cycles and two on an SM 2400 together, 512 of them the tensor pipe's and as many the exponentials' for each by arithmetic; the rest is their chain within a CTA, and the
+// instruction cache: loops that few rows reach are not unrolled, and a block is exponentiated in halves by the same code (together 207 -> 182 us in the case below).  A tile costs some 7600 cycles besides.  Three prompts of up to 2500 tokens, 64 heads
+// of 128 over 8, a window of 1000: 181 - 190 us behind calls of its own kind, 0.40 of what the products alone take at 1667 TFLOP/s (tensor pipe 37 %, exponentials' 38 % busy).  Not better: blocks of 16 columns of S at a time,
+// exponentials of a quarter or half of the pairs by polynomials (even), eight softmax warps that share rows (198 us), a tile's keys split over several CTAs and joined where there are few tiles (even there, and 1.1 times as
+// long elsewhere by its code alone).
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
 #include <algorithm>

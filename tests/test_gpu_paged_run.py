@@ -202,3 +202,85 @@ def test_requests_that_come_and_go(seed, temperatures):
     graph.replay()
     torch.cuda.synchronize()
     assert int(m.n_free) == N_PAGES and sorted(m.free.cpu().tolist()) == list(range(N_PAGES)) and (m.table == -1).all()
+
+
+def test_nothing_is_read_before_it_is_written():
+    """Append, attention and a product in a row without a pause, over inputs that change from turn to turn: the bits of the same calls with the GPU waited for between them.  (The kernels are launched while those before
+    them run: each has to wait for what it reads, the one for few rows beside the one for prompts, too.)"""
+    rng = np.random.default_rng(8)
+    rows = [(300, 1500), (1, 800), (1, 40), (5, 70), (0, 9), (90, 90)]
+    n, P, T_, W = len(rows), 32, sum(r for r, _ in rows), 47
+    c = tb.ModelCfg(L=1, d=D, Hq=HQ, Hkv=HKV, Dh=DH, F=1, V=1, E=0, topk=0, B=n, max_len=1500, TK=P, rope_base=10000.0, eps=1e-5)
+    order = iter(rng.permutation(100))
+    table = np.full((n, W), -1)
+    for b, (_, e) in enumerate(rows):
+        table[b, :-(-e // P)] = [next(order) for _ in range(-(-e // P))]
+    at = [(b, e - r + i) for b, (r, e) in enumerate(rows) for i in range(r)]
+    slot, pos = ints([table[b, p // P] * P + p % P for b, p in at]), ints([p for _, p in at])
+    start, end = ints(np.concatenate(([0], np.cumsum([r for r, _ in rows])))), ints([e for _, e in rows])
+    cos, sin = (torch.empty(1500, DH // 2, device=DEV) for _ in range(2))
+    tb.k_rope_tables(DH, 1500, 10000.0, cos, sin)
+    sets = [[torch.randn(T_, H * DH, device=DEV) for H in (HQ, HKV, HKV)] for _ in range(3)]
+    tables = [ints(table), ints(np.where(np.arange(W) % 2, table, -1)), ints(table)]
+    weight = bf16(rng.standard_normal((256, HQ * DH)) * 0.05)
+    scratch = torch.empty(tb.k_attn_paged_scratch_bytes(c, n, T_, 300, 1500), dtype=torch.uint8, device=DEV)
+    first = [torch.randn(100, HKV, P, DH, device=DEV).bfloat16() for _ in range(2)]
+
+    def turns(wait):
+        kp, vp = (x.clone() for x in first)
+        q, k, v = (torch.empty_like(x) for x in sets[0])
+        now = torch.empty_like(tables[0])
+        qb, o = (torch.zeros(T_, HQ * DH, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        outs = [torch.empty(T_, 256, device=DEV) for _ in range(12)]
+        torch.cuda.synchronize()
+        for i, out in enumerate(outs):
+            for to, x in zip((q, k, v, now), (*sets[i % 3], tables[i % 3])):
+                to.copy_(x)
+            wait()
+            tb.k_rope_kv_paged(q, k, v, qb, kp, vp, cos, sin, slot, pos, c, T_, 100)
+            wait()
+            tb.k_attn_paged(qb, kp, vp, o, now, start, end, c, n, T_, 300, 1500, 100, (0, 200)[i % 2], 0, scratch)
+            wait()
+            tb.k_gemm(o, weight, out, T_, 256, HQ * DH, 256, 0, False)
+            wait()
+        torch.cuda.synchronize()
+        return outs
+
+    want, got = turns(torch.cuda.synchronize), turns(lambda: None)
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and not torch.equal(want[0], want[1])
+
+
+def test_verification_waits_for_its_logits():
+    """The same of a product, the verification of what it gives and a copy of the answer."""
+    rng = np.random.default_rng(9)
+    n, rows, V_ = 7, 21, 9001
+    hidden = [bf16(rng.standard_normal((rows, D))) for _ in range(6)]
+    weight = bf16(rng.standard_normal((V_, D)) * 0.15)
+    tokens = [ints(rng.integers(0, V_, rows)) for _ in range(3)]
+    starts = [ints([0, 5, 6, 9, 9, 15, 20, 21]), ints([0, 3, 6, 9, 12, 15, 18, 21])]
+    us = [torch.rand(rows, device=DEV) * 0.2 for _ in range(3)]
+    draws, t = torch.rand(n, device=DEV), torch.tensor([1.0, 0.7, 0.0, 1.0, 1.3, 2.0, 0.5], device=DEV)
+    scratch = torch.empty(tb.k_verify_scratch_bytes(rows, V_), dtype=torch.uint8, device=DEV)
+
+    def turns(wait):
+        x, y = (torch.zeros(rows, V_, device=DEV) for _ in range(2))
+        tok, start, u, out, count = torch.zeros_like(tokens[0]), torch.zeros_like(starts[0]), torch.zeros_like(us[0]), torch.zeros(rows, dtype=torch.int32, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV)
+        answers = [(torch.empty_like(out), torch.empty_like(count)) for _ in range(12)]
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(answers):
+            for to, v in ((tok, tokens[i % 3]), (start, starts[i % 2]), (u, us[(i + 1) % 3])):
+                to.copy_(v)
+            wait()
+            tb.k_gemm(hidden[i % 6], weight, x, rows, V_, D, V_, 0, False)
+            tb.k_gemm(hidden[(i + 2) % 6], weight, y, rows, V_, D, V_, 0, False)
+            wait()
+            tb.k_verify(x, y if i % 4 else None, tok, start, u, draws, out, count, n, rows, V_, t, scratch)
+            wait()
+            a.copy_(out)
+            b.copy_(count)
+            wait()
+        torch.cuda.synchronize()
+        return answers
+
+    want, got = turns(torch.cuda.synchronize), turns(lambda: None)
+    assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y)) and len({tuple(a.tolist()) for a, _ in want}) > 3
