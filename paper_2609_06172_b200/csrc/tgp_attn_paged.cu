@@ -79,42 +79,47 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     float *ml = reinterpret_cast<float *>(q_sm + q_bytes<DH, MT>());       // [WARPS][16][2]: maxima and sums of the warps' partials
     uint32_t *shared_u = reinterpret_cast<uint32_t *>(ml + WARPS * 16 * 2);
     uint4 *seqs = reinterpret_cast<uint4 *>(shared_u + 16);                 // [B] first row, rows, length, and chunks of the sequences up to this one, all KV heads
+    uint32_t *upto = reinterpret_cast<uint32_t *>(seqs + a.B);              // [B] stretches of MIN_STRETCH of the sequences up to this one, none of which crosses from one KV head to another
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
 
     // ---- the line of all chunks ----
     {
-        uint32_t before = 0;
+        uint32_t before = 0, before_u = 0;
         for (uint32_t i0 = 0; i0 < a.B; i0 += WARPS * 32) {
             const uint32_t i = i0 + tid;
-            uint32_t mine = 0;
+            uint32_t mine = 0, mine_u = 0;
             TgpPagedSeq s{0, 0, 0, false};
             if (i < a.B) {
                 s = tgp_paged_seq(a, a.b0 + i);
-                if (s.n && !s.idle && s.n * a.G <= a.few) mine = tgp_paged_keys<KEYS>(a, s.end - s.n, s.end - 1).chunks * a.Hkv;
+                if (s.n && !s.idle && s.n * a.G <= a.few) { mine = tgp_paged_keys<KEYS>(a, s.end - s.n, s.end - 1).chunks; mine_u = (mine + MIN_STRETCH - 1) / MIN_STRETCH * a.Hkv; mine *= a.Hkv; }
                 else if (s.n && s.idle)                                     // rows of idle sequences are zero
                     for (u64 e = blockIdx.x; e < (u64)s.n * a.Hq * DH / 8; e += gridDim.x) reinterpret_cast<uint4 *>(a.o + (size_t)s.first * a.Hq * DH)[e] = make_uint4(0, 0, 0, 0);
             }
-            uint32_t x = mine;
+            uint32_t x = mine, x_u = mine_u;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-            if (lane == 31) shared_u[warp] = x;
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o), y_u = __shfl_up_sync(0xffffffffu, x_u, o); if (lane >= o) { x += y; x_u += y_u; } }
+            if (lane == 31) { shared_u[warp] = x; shared_u[WARPS + warp] = x_u; }
             __syncthreads();
-            uint32_t all = 0;
+            uint32_t all = 0, all_u = 0;
 #pragma unroll
-            for (uint32_t w = 0; w < WARPS; ++w) { if (w < warp) x += shared_u[w]; all += shared_u[w]; }
-            if (i < a.B) seqs[i] = make_uint4(s.first, s.n, s.end, before + x);
+            for (uint32_t w = 0; w < WARPS; ++w) { if (w < warp) { x += shared_u[w]; x_u += shared_u[WARPS + w]; } all += shared_u[w]; all_u += shared_u[WARPS + w]; }
+            if (i < a.B) { seqs[i] = make_uint4(s.first, s.n, s.end, before + x); upto[i] = before_u + x_u; }
             before += all;
+            before_u += all_u;
             __syncthreads();
         }
     }
-    const uint32_t N = seqs[a.B - 1].w, ctas = min(gridDim.x, (N + MIN_STRETCH - 1) / MIN_STRETCH);
+    // Where the CTAs suffice for stretches that each lie within an item, they do: one that crosses is two chains of merges one after the other (one sequence of 700 keys, 8 KV heads of 64, 9.4 -> 7.0 us; of 20 keys 7.5 -> 3.5).
+    const uint32_t N = seqs[a.B - 1].w, units = upto[a.B - 1];
+    const bool within = units <= gridDim.x;
+    const uint32_t ctas = within ? units : min(gridDim.x, (N + MIN_STRETCH - 1) / MIN_STRETCH);
     if (blockIdx.x >= ctas) {
         if (f.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
     }
     const uint32_t each_cta = N / ctas, longer = N - each_cta * ctas;       // the first `longer` stretches have a chunk more
     auto stretch = [&](uint32_t cta) { return cta * each_cta + min(cta, longer); };
-    const uint32_t line_lo = stretch(blockIdx.x), line_hi = stretch(blockIdx.x + 1);
+    uint32_t line_lo = stretch(blockIdx.x), line_hi = stretch(blockIdx.x + 1), item_parts = 0, item_part = 0;             // (of stretches within items: how many the item has, and which this is)
 
     // an item: a (sequence, KV head) and its place in the line
     struct Item { uint32_t b, hk, lo, hi; TgpPagedSeq s; TgpPagedKeys k; };
@@ -130,9 +135,18 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     };
     Item ahead, now;
     {
-        uint32_t lo = 0, hi = a.B - 1;                                      // the first sequence that ends behind line_lo
-        while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (seqs[mid].w > line_lo) hi = mid; else lo = mid + 1; }
+        uint32_t lo = 0, hi = a.B - 1;                                      // the first sequence that ends behind line_lo, or this CTA
+        while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (within ? upto[mid] > blockIdx.x : seqs[mid].w > line_lo) hi = mid; else lo = mid + 1; }
         ahead.b = lo;
+        if (within) {
+            const uint32_t seq_lo = lo ? seqs[lo - 1].w : 0, chunks = (seqs[lo].w - seq_lo) / a.Hkv, rel = blockIdx.x - (lo ? upto[lo - 1] : 0);
+            item_parts = (chunks + MIN_STRETCH - 1) / MIN_STRETCH;
+            const uint32_t hk = rel / item_parts;
+            item_part = rel - hk * item_parts;
+            const uint32_t each = chunks / item_parts, more = chunks - each * item_parts;
+            line_lo = seq_lo + hk * chunks + item_part * each + min(item_part, more);
+            line_hi = line_lo + each + (item_part < more);
+        }
     }
     enter(ahead, line_lo);
     now = ahead;
@@ -418,13 +432,13 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             const uint32_t item = (a.b0 + now.b) * a.Hkv + now.hk;
             // CTAs of the item's first and last chunk
             auto cta_of = [&](uint32_t g) { return g < longer * (each_cta + 1) ? g / (each_cta + 1) : longer + (g - longer * (each_cta + 1)) / each_cta; };
-            const uint32_t c0 = cta_of(now.lo), c1 = cta_of(now.hi - 1), parts = c1 - c0 + 1;
+            const uint32_t c0 = within ? blockIdx.x - item_part : cta_of(now.lo), parts = within ? item_parts : cta_of(now.hi - 1) - c0 + 1;
             if (tid == 0) shared_u[8] = tgp_paged_arrive(f.counters + item) == parts;
             __syncthreads();
             if (shared_u[8]) {
                 if (tid == 0) f.counters[item] = TGP_PAGED_COUNTS;
                 // a partial: [rows][DH] outputs, [rows][2] maxima and sums
-                auto part = [&](uint32_t p) { const uint32_t cta = c0 + p; return f.parts + ((size_t)cta * 2 + (stretch(cta) >= now.lo ? 0 : 1)) * slot_floats<DH, MT>(); };
+                auto part = [&](uint32_t p) { const uint32_t cta = c0 + p; return f.parts + ((size_t)cta * 2 + (within || stretch(cta) >= now.lo ? 0 : 1)) * slot_floats<DH, MT>(); };
                 auto ml_of = [&](const float *from, uint32_t row) { return __ldcg(reinterpret_cast<const float2 *>(from + MT * 16 * DH + row * 2)); };
                 auto four_of = [&](const float *from, uint32_t row, uint32_t d) { return __ldcg(reinterpret_cast<const float4 *>(from + row * DH + d)); };
                 constexpr uint32_t SOME = 4, ROWS = DH == 128 ? 3 : 1;     // partials, and pieces of four dimensions, that a thread asks for at a time
@@ -480,12 +494,12 @@ template <int DH, int MT> uint32_t few_ctas() { return (uint32_t)tgpk_sms() * (D
 
 template <int DH, int MT>
 int launch_few(FewArgs f, cudaStream_t st) {
-    if (!tgpk_allow_smem<tgp_attn_paged_few_kernel<DH, MT>>(fixed_smem<DH, MT>() + GROUP * 16, true)) return TGP_E_CUDA;
+    if (!tgpk_allow_smem<tgp_attn_paged_few_kernel<DH, MT>>(fixed_smem<DH, MT>() + GROUP * 20, true)) return TGP_E_CUDA;
     const uint32_t B = f.a.B;
     for (uint32_t b0 = 0; b0 < B; b0 += GROUP) {
         f.a.b0 = b0;
         f.a.B = std::min(GROUP, B - b0);
-        if (int rc = launch(tgp_attn_paged_few_kernel<DH, MT>, dim3(few_ctas<DH, MT>()), dim3(WARPS * 32), fixed_smem<DH, MT>() + f.a.B * 16, st, 1, f)) return rc;
+        if (int rc = launch(tgp_attn_paged_few_kernel<DH, MT>, dim3(few_ctas<DH, MT>()), dim3(WARPS * 32), fixed_smem<DH, MT>() + f.a.B * 20, st, 1, f)) return rc;
         f.beside = false;                                                   // the next launch takes the same partials
     }
     return TGP_OK;
