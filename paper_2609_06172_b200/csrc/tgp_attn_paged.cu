@@ -79,10 +79,11 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     float *ml = reinterpret_cast<float *>(q_sm + q_bytes<DH, MT>());       // [WARPS][16][2]: maxima and sums of the warps' partials
     uint32_t *shared_u = reinterpret_cast<uint32_t *>(ml + WARPS * 16 * 2);
     uint4 *seqs = reinterpret_cast<uint4 *>(shared_u + 16);                 // [B] first row, rows, length, and chunks of the sequences up to this one, all KV heads
-    uint32_t *upto = reinterpret_cast<uint32_t *>(seqs + a.B);              // [B] stretches of MIN_STRETCH of the sequences up to this one, none of which crosses from one KV head to another
+    uint32_t *upto = reinterpret_cast<uint32_t *>(seqs + a.B);              // [B] stretches of up to `unit` chunks of the sequences up to this one, none of which crosses from one KV head to another
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
 
     // ---- the line of all chunks ----
+    uint32_t own = 0;                                                       // chunks of an item of the thread's (last) sequence
     {
         uint32_t before = 0, before_u = 0;
         for (uint32_t i0 = 0; i0 < a.B; i0 += WARPS * 32) {
@@ -91,7 +92,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             TgpPagedSeq s{0, 0, 0, false};
             if (i < a.B) {
                 s = tgp_paged_seq(a, a.b0 + i);
-                if (s.n && !s.idle && s.n * a.G <= a.few) { mine = tgp_paged_keys<KEYS>(a, s.end - s.n, s.end - 1).chunks; mine_u = (mine + MIN_STRETCH - 1) / MIN_STRETCH * a.Hkv; mine *= a.Hkv; }
+                if (s.n && !s.idle && s.n * a.G <= a.few) { own = mine = tgp_paged_keys<KEYS>(a, s.end - s.n, s.end - 1).chunks; mine_u = (mine + MIN_STRETCH - 1) / MIN_STRETCH * a.Hkv; mine *= a.Hkv; }
                 else if (s.n && s.idle)                                     // rows of idle sequences are zero
                     for (u64 e = blockIdx.x; e < (u64)s.n * a.Hq * DH / 8; e += gridDim.x) reinterpret_cast<uint4 *>(a.o + (size_t)s.first * a.Hq * DH)[e] = make_uint4(0, 0, 0, 0);
             }
@@ -110,7 +111,39 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         }
     }
     // Where the CTAs suffice for stretches that each lie within an item, they do: one that crosses is two chains of merges one after the other (one sequence of 700 keys, 8 KV heads of 64, 9.4 -> 7.0 us; of 20 keys 7.5 -> 3.5).
-    const uint32_t N = seqs[a.B - 1].w, units = upto[a.B - 1];
+    // Longer contexts, as long as no stretch is more than eight chunks longer than an equal share (one sequence of 16000 keys 19.7 -> 17.4 us, five drafted tokens over 8000
+    // 29.6 -> 25.4, eight sequences of up to 2000 keys 13.5 -> 10.8; 24 of up to 12000 have too many items and stay as they were).
+    const uint32_t N = seqs[a.B - 1].w;
+    uint32_t units = upto[a.B - 1], unit = MIN_STRETCH;
+    if (units > gridDim.x && a.B <= WARPS * 32 && a.B * a.Hkv <= gridDim.x) {
+        const uint32_t share = max(MIN_STRETCH, (N + gridDim.x - 1) / gridDim.x);
+        auto with = [&](uint32_t u) { return (own + u - 1) / u * a.Hkv; };
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            const uint32_t all = __reduce_add_sync(0xffffffffu, with(share + (1u << k)));
+            if (lane == 0) shared_u[k * WARPS + warp] = all;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 3; k >= 0; --k) {
+            uint32_t all = 0;
+#pragma unroll
+            for (uint32_t w = 0; w < WARPS; ++w) all += shared_u[k * WARPS + w];
+            if (all <= gridDim.x) { units = all; unit = share + (1u << k); }
+        }
+        __syncthreads();
+        if (unit != MIN_STRETCH) {
+            uint32_t x = with(unit);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+            if (lane == 31) shared_u[warp] = x;
+            __syncthreads();
+#pragma unroll
+            for (uint32_t w = 0; w < WARPS; ++w) if (w < warp) x += shared_u[w];
+            if (tid < a.B) upto[tid] = x;
+            __syncthreads();
+        }
+    }
     const bool within = units <= gridDim.x;
     const uint32_t ctas = within ? units : min(gridDim.x, (N + MIN_STRETCH - 1) / MIN_STRETCH);
     if (blockIdx.x >= ctas) {
@@ -140,7 +173,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
         ahead.b = lo;
         if (within) {
             const uint32_t seq_lo = lo ? seqs[lo - 1].w : 0, chunks = (seqs[lo].w - seq_lo) / a.Hkv, rel = blockIdx.x - (lo ? upto[lo - 1] : 0);
-            item_parts = (chunks + MIN_STRETCH - 1) / MIN_STRETCH;
+            item_parts = (chunks + unit - 1) / unit;
             const uint32_t hk = rel / item_parts;
             item_part = rel - hk * item_parts;
             const uint32_t each = chunks / item_parts, more = chunks - each * item_parts;
