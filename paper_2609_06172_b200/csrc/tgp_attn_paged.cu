@@ -5,12 +5,12 @@
 // weights and an unnormalised output in fp32:  p = 2^(s - m),  l += p,  O += p V,  and both times 2^(m - m') where the maximum grows to m'.  Weights are rounded to bf16 for the second
 // product, and those that are summed are the rounded ones, so what is divided by is what the values were multiplied by.
 //
-// Split: all chunks of all sequences and KV heads are one line, of which every CTA takes an equal stretch; lengths are known on the device only, so every CTA adds up the sequences' chunks for
-// itself.  Where a stretch ends inside a (sequence, KV head), its CTA leaves (maximum, sum, output) in the scratch, and the last one to arrive at that pair's counter merges them
+// Split: all chunks of all sequences and KV heads are one line, of which every CTA takes a stretch: an equal one, or where there are CTAs enough one within a (sequence, KV head); lengths are known on the
+// device only, so every CTA adds up the sequences' chunks for itself.  Where a stretch ends inside a (sequence, KV head), its CTA leaves (maximum, sum, output) in the scratch, and the last one to arrive at that pair's counter merges them
 // all in the order of the stretches, so that results do not depend on who was last.
 //
-// What bounds it: HBM where contexts are long (24 of up to 12000 keys, 64 heads of 128 over 8: 106 us, 6.1 TB/s; 61 of up to 2500, 32 over 8: 63 us, 5.2 TB/s), else a fixed 9 us - a launch, the sequences'
-// counts, table, keys, merges in the CTA and across CTAs, each a chain of memory latencies - and with 17 to 32 rows the instructions (32 sequences of five tokens that see 1028 keys: 34 us, 0.57 of HBM's rate).  A chunk's
+// What bounds it: HBM where contexts are long (24 of up to 12000 keys, 64 heads of 128 over 8: 106 us, 6.1 TB/s; 61 of up to 2500, 32 over 8: 63 us, 5.2 TB/s), else a fixed 3.5 us - a launch, the sequences'
+// counts, table, keys, the merge in the CTA - and where CTAs share a context another 3 of their merge, each a chain of memory latencies, and with 17 to 32 rows the instructions (32 sequences of five tokens that see 1028 keys: 34 us, 0.57 of HBM's rate).  A chunk's
 // second tile of rows is multiplied even for sequences that have only one: leaving it out by a test was no faster.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             __syncthreads();
         }
     }
-    // Where the CTAs suffice for stretches that each lie within an item, they do: one that crosses is two chains of merges one after the other (one sequence of 700 keys, 8 KV heads of 64, 9.4 -> 7.0 us; of 20 keys 7.5 -> 3.5).
+    // Where the CTAs suffice for stretches that each lie within an item, they do: one that crosses is two chains of merges one after the other (one sequence of 700 keys, 8 KV heads of 64, 9.4 -> 6.8 us; of 20 keys 7.5 -> 3.5).
     // Longer contexts, as long as no stretch is more than eight chunks longer than an equal share (one sequence of 16000 keys 19.7 -> 17.4 us, five drafted tokens over 8000
     // 29.6 -> 25.4, eight sequences of up to 2000 keys 13.5 -> 10.8; 24 of up to 12000 have too many items and stay as they were).
     const uint32_t N = seqs[a.B - 1].w;
@@ -474,7 +474,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
                 auto part = [&](uint32_t p) { const uint32_t cta = c0 + p; return f.parts + ((size_t)cta * 2 + (within || stretch(cta) >= now.lo ? 0 : 1)) * slot_floats<DH, MT>(); };
                 auto ml_of = [&](const float *from, uint32_t row) { return __ldcg(reinterpret_cast<const float2 *>(from + MT * 16 * DH + row * 2)); };
                 auto four_of = [&](const float *from, uint32_t row, uint32_t d) { return __ldcg(reinterpret_cast<const float4 *>(from + row * DH + d)); };
-                constexpr uint32_t SOME = 4, ROWS = DH == 128 ? 3 : 1;     // partials, and pieces of four dimensions, that a thread asks for at a time
+                constexpr uint32_t SOME = MT == 1 ? 6 : 4, ROWS = DH == 128 ? (MT == 1 ? 2 : 3) : 1;     // partials, and pieces of four dimensions, that a thread asks for at a time
                 for (uint32_t i0 = tid; i0 < rows * DH / 4; i0 += WARPS * 32 * ROWS) {
                     float M[ROWS], sum[ROWS];
                     float4 v[ROWS];
