@@ -243,6 +243,15 @@ def test_contexts_split_over_many(lengths, Hq, Hkv, Dh):
     assert np.array_equal(one, b.run())                    # the same bits, whoever arrives last
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1000, 4)])
+@pytest.mark.parametrize("rows", [[(5, 6000), (1, 3000)], [(5 if b % 3 else 1, 300 + 7 * b) for b in range(40)], [(0, 9), (4, 900), (0, 0), (8, 17)]])
+def test_drafts_over_contexts_split_over_many(rows, window, sinks):
+    """Stretches within a KV head's keys, short and long, and those that cross from one to the next."""
+    b = Batch(32, 8, 128, 16, rows, seed=19)
+    one = b.check(window, sinks, some=7)
+    assert np.array_equal(one, b.run(window, sinks))
+
+
 def test_more_sequences_than_a_launch_takes():
     Batch(4, 1, 64, 16, [(b % 3, 3 + b % 40) for b in range(2500)], seed=6).check(some=5)
 
@@ -406,3 +415,64 @@ def test_a_wait_that_runs_out_ends_the_call():
     got = f64(o).reshape(b.T, 8, 128)
     assert (got[32:, :4] == 7).all() and np.array_equal(got[:32], want[:32]) and np.array_equal(got[32:, 4:], want[32:, 4:])          # (the last tile is the grid's first)
     assert np.array_equal(b.run(dev=d), want)
+
+
+def test_graphs_that_share_a_scratch_and_calls_at_once():
+    """Two captured calls with one scratch replayed in turn, then two streams with a scratch each at the same time."""
+    batches = [Batch(8, 2, 128, 64, [(64, 300), (1, 900), (3, 77), (70, 70)], seed=20), Batch(8, 2, 128, 64, [(1, 700), (2, 90), (0, 5)], seed=21)]
+    want, devs = [b.run(30, 2) for b in batches], [b.device() for b in batches]
+    outs = [torch.zeros(b.T, 1024, dtype=torch.bfloat16, device=DEV) for b in batches]
+    shared = max((b.scratch()[0] for b in batches), key=len)
+
+    def call(i, scratch, stream):
+        b, d = batches[i], devs[i]
+        tb.k_attn_paged(d["q"], d["k"], d["v"], outs[i], d["table"], d["start"], d["end"], b.c, b.B, b.T, b.q_max, b.kv_max, b.n_pages, 30, 2, scratch, stream)
+
+    def right():
+        torch.cuda.synchronize()
+        ok = [np.array_equal(f64(o).reshape(w.shape), w) for o, w in zip(outs, want)]
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        return ok
+
+    graphs, stream = [], torch.cuda.Stream()
+    for i in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i], stream=stream):
+            call(i, shared, stream)
+    for order in ((0, 1), (1, 0), (0, 0, 1, 1)):
+        for i in order:
+            graphs[i].replay()
+        assert right() == [True, True]
+    scratches, streams = [b.scratch()[0] for b in batches], [torch.cuda.Stream() for _ in batches]
+    torch.cuda.synchronize()
+    for turn in range(5):
+        for _ in range(8):
+            for i in (turn % 2, 1 - turn % 2):
+                call(i, scratches[i], streams[i])
+        assert right() == [True, True]
+    assert tb.k_attn_status() == 0
+
+
+@pytest.mark.parametrize("rows", [[(64, 300)], [(1300, 1300), (1, 40)]])
+def test_a_scratch_is_good_for_the_next_call_when_a_wait_ran_out(rows):
+    """Fewer tiles than the GPU takes at a time, and more: those that a CTA leaves when it gives up are counted all the same."""
+    b = Batch(32, 8, 64, 64, rows, seed=22)
+    d, (scratch, _) = b.device(), b.scratch()
+    want, o = b.run(dev=d), torch.zeros(b.T, 2048, dtype=torch.bfloat16, device=DEV)
+    call = lambda: tb.k_attn_paged(d["q"], d["k"], d["v"], o, d["table"], d["start"], d["end"], b.c, b.B, b.T, b.q_max, b.kv_max, b.n_pages, 0, 0, scratch)          # noqa: E731
+    for withheld in (0, 1, 3):
+        tb.k_wait_test(2_000_000, withheld)
+        try:
+            call()
+            torch.cuda.synchronize()
+            assert tb.k_attn_status() in (1, 2, 3, 4)             # (4: the warp that finds tiles waited for room for the next)
+        finally:
+            tb.k_wait_test(0, 0)
+            tb.k_status_clear()
+        for _ in range(2):
+            o.zero_()
+            call()
+            torch.cuda.synchronize()
+            assert tb.k_attn_status() == 0 and np.array_equal(f64(o).reshape(want.shape), want)
