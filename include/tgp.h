@@ -380,8 +380,8 @@ int  tgp_k_attn_select(int impl);
  * batch's context adds up to less than 256 chunks it multiplies what that leaves over with V too, all 24 bits of P.  Process-wide. */
 int  tgp_k_attn_decode_select(int impl);
 /* Error word of the tcgen05 attention kernels (over KV tiles and over pages): 0, or which bounded wait ran out first (1 for S, 2 for P V, 3 for a K/V
- * load, 4 for the hand-over between the softmax warps and the MMA warp), or 5 if shared memory was not 1024-byte
- * aligned.  A CTA that gives up stores nothing.  Synchronous. */
+ * load, 4 for the hand-over between the softmax warps and the MMA warp, over pages also of tiles), or 5 if shared memory was not 1024-byte
+ * aligned.  A CTA that gives up stores nothing (over pages: of the tile that it is at, and of those it has taken for later).  Synchronous. */
 int  tgp_k_attn_status(int *error_code);
 /* Error word of the tensor-core GEMM: 0, or (role << 8 | stage) of the first bounded wait that ran out
  * (role 1 TMA producer, 2 MMA issuer, 3 epilogue).  Synchronous. */
