@@ -66,6 +66,16 @@ def attention(q, K, V, first, window=0, sinks=0, there=None):
     return out, mean, most
 
 
+def rows(start, T):
+    """(first row, rows) of each sequence of a verification: none where they do not lie in [0, T), or begin before the start of a sequence before it (of those in [0, T])."""
+    out, highest = [], 0
+    for s, e in zip(start, start[1:]):
+        out.append((int(s), int(e - s) if highest <= s < e <= T else 0))
+        if 0 <= s <= T:
+            highest = max(highest, s)
+    return out
+
+
 def softmax(x, t):
     """Of logits at a temperature; those of -inf and NaN are 0, and all are where there are no others."""
     x = np.asarray(x, np.float64)

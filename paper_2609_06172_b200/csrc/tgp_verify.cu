@@ -123,6 +123,11 @@ __device__ __forceinline__ Seq seq_of(const VerifyArgs &a, uint32_t b) {
     const float t = a.temperature ? a.temperature[b] : 1.f;
     return {(uint32_t)s0, s0 < 0 || s1 <= s0 || (uint32_t)s1 > a.T ? 0u : (uint32_t)(s1 - s0), t > 0.f ? fmax(OCTAVE * LOG2E / (double)t, 1e-300) : 0.0, (double)t * (1000.0 / LOG2E)};
 }
+// A sequence has rows only from the highest start before its own on (of those in [0, T]).  So a row belongs to one sequence at most, whatever the device holds, and the line of all rows below has 2 T at most: its
+// numbers of parts and costs, products in 32 bits, are bounded by the sizes that the call was checked with.
+__device__ __forceinline__ uint32_t start_in(const VerifyArgs &a, uint32_t start) { return start > a.T ? 0u : start; }
+constexpr uint32_t T_MAX = 32767, PARTS_MAX = (TGP_SAMPLE_MAX_V + PART - 1) / PART;
+static_assert(2ull * 2 * T_MAX * PARTS_MAX < 1u << 31, "all parts' costs");
 
 // The rows that the first kernel adds up, one line of them: of each sequence the target's, then the draft's that something was drawn from - none behind the last row, none where the likeliest token is taken.
 // A part costs 1 where the likeliest token is asked for, else 2 (a part of weights took twice as long: with as many parts each, stretches of a mixed batch ended after 17 to 38 us).
@@ -175,17 +180,26 @@ template <bool WIDE>
 __global__ void __launch_bounds__(STAT_THREADS, 3) tgp_verify_stat_kernel(const VerifyArgs a) {
     __shared__ double table_of_all[TABLE], sh_s[2][STAT_WARPS];
     __shared__ float sh_m[2][STAT_WARPS];
-    __shared__ uint32_t sh_i[2][STAT_WARPS];
+    __shared__ uint32_t sh_i[2][STAT_WARPS], sh_start[STAT_WARPS];
     extern __shared__ __align__(16) float ring[];                // [RING][PART], then [B] sequences
     LineSeq *line = reinterpret_cast<LineSeq *>(ring + RING * PART);
     const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const double *table = fill_table(table_of_all);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");          // not before the wait: the draw's kernel reads the call's arguments without one of its own
-    uint32_t rows = 0, cost = 0;
+    uint32_t rows = 0, cost = 0, highest = 0;
     for (uint32_t b0 = 0; b0 < a.B; b0 += STAT_THREADS) {
         Seq s{0, 0, 0.0, 0.0};
-        if (b0 + tid < a.B) s = seq_of(a, b0 + tid);
+        uint32_t from = 0;
+        if (b0 + tid < a.B) { s = seq_of(a, b0 + tid); from = start_in(a, s.first); }
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, from, o); if (lane >= o) from = max(from, v); }
+        if (lane == 31) sh_start[warp] = from;
+        __syncthreads();
+        from = max(from, highest);
+#pragma unroll
+        for (uint32_t w = 0; w < STAT_WARPS; ++w) { if (w < warp) from = max(from, sh_start[w]); highest = max(highest, sh_start[w]); }
+        if (s.first < from) s.n = 0;
         uint32_t upto = s.n + (s.n && a.y && s.rate != 0.0 ? s.n - 1 : 0);
         uint32_t costs = upto * cost_of(s);
 #pragma unroll
@@ -333,7 +347,7 @@ __device__ __forceinline__ Stat join(const Parts &p, double rate, double span, c
 #pragma unroll
     for (int o = 16; o; o >>= 1) { const float om = __shfl_xor_sync(0xffffffffu, all.top, o); const uint32_t oi = __shfl_xor_sync(0xffffffffu, all.at, o); merge(all, om, oi); }
     all.sum = 0.0;
-    if (all.top == -INFINITY) { all.at = 0; return all; }
+    if (__all_sync(0xffffffffu, all.top == -INFINITY)) { all.at = 0; return all; }                // (by all lanes: the shuffles below are of all, whatever a scratch that is not this call's alone may hold)
     if (rate != 0.0) {
         const Weights weight(all.top, rate, span);
 #pragma unroll
@@ -382,6 +396,8 @@ constexpr uint32_t KEPT = 32;                                    // rows that ar
 
 __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const VerifyArgs a) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    __shared__ bool sh_none[NW];                                 // (a warp each) a sequence before this one starts behind its first row
+    __shared__ uint32_t sh_first, sh_n;                          // first row and rows, for the end
     __shared__ uint32_t sh_refused;                              // first row, counted from the sequence's first, whose token is not taken
     __shared__ Stat kept[2][KEPT];                               // target, draft
     __shared__ Scaled sh_w[2];
@@ -397,8 +413,19 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
     // what the sums are not needed for is read while the first kernel, which has waited for it, still runs (no rows: there is none)
     if (!a.T) asm volatile("griddepcontrol.wait;" ::: "memory");
     const Seq s = seq_of(a, b);
-    if (tid == 0) sh_refused = s.n ? s.n - 1 : 0;
+    if (tid == 0) { sh_refused = s.n ? s.n - 1 : 0; sh_first = s.first; sh_n = s.n; }
+    // Does it begin before the start of one before it?  Then the first kernel has left its rows out, and nothing of their parts may be read.
+    bool none = false;
+    for (uint32_t i = tid; i < b; i += DRAW_THREADS) none |= start_in(a, (uint32_t)a.start[i]) > s.first;
+    none = __any_sync(0xffffffffu, none);
+    if (lane == 0) sh_none[warp] = none;
     __syncthreads();
+    if (__any_sync(0xffffffffu, lane < NW && sh_none[lane])) {                  // (the same in every CTA of the cluster)
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        cluster_wait();
+        if (rank == 0 && tid == 0) a.n_out[b] = 0;
+        return;
+    }
     // ---- which rows take their token, every CTA for itself: a warp joins a row of the target or of the draft, then a thread judges a row ----
     uint32_t group = 0;
     bool waited = false;
@@ -547,18 +574,19 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
         }
     } else if (!mine || warp) return;
     // ---- one warp writes the sequence's tokens ----
-    for (uint32_t i = lane; i < s.n; i += 32) a.out[s.first + i] = i < refused ? a.tokens[s.first + i + 1] : i == refused ? token : -1;
-    if (lane == 0) a.n_out[b] = s.n ? (int32_t)(refused + 1) : 0;
+    const uint32_t out = sh_first, n = sh_n, taken = sh_refused;
+    for (uint32_t i = lane; i < n; i += 32) a.out[out + i] = i < taken ? a.tokens[out + i + 1] : i == taken ? token : -1;
+    if (lane == 0) a.n_out[b] = n ? (int32_t)(taken + 1) : 0;
 }
 
 uint32_t parts_of(uint32_t V) { return (V + PART - 1) / PART; }
-static_assert((TGP_SAMPLE_MAX_V + PART - 1) / PART <= 128, "a warp joins a row's parts");
+static_assert(PARTS_MAX <= 128, "a warp joins a row's parts");
 
 }  // namespace
 
 extern "C" int tgp_k_verify_scratch_bytes(uint32_t T, uint32_t V, uint64_t *bytes) {
     if (!bytes || !V) return TGP_E_INVAL;
-    if (V > TGP_SAMPLE_MAX_V || T > 32767) return TGP_E_TOO_LARGE;
+    if (V > TGP_SAMPLE_MAX_V || T > T_MAX) return TGP_E_TOO_LARGE;
     *bytes = std::max<uint64_t>(16, (uint64_t)2 * T * parts_of(V) * sizeof(Stat));
     return TGP_OK;
 }
@@ -569,7 +597,7 @@ extern "C" int tgp_k_verify(const float *logits, const float *draft_logits, cons
     if (((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(draft_logits) | reinterpret_cast<uintptr_t>(tokens_dev) | reinterpret_cast<uintptr_t>(start_dev) |
           reinterpret_cast<uintptr_t>(u_dev) | reinterpret_cast<uintptr_t>(u_draw_dev) | reinterpret_cast<uintptr_t>(out_dev) | reinterpret_cast<uintptr_t>(n_out_dev) |
           reinterpret_cast<uintptr_t>(temperature_dev)) & 3u) || (reinterpret_cast<uintptr_t>(scratch_dev) & 15u)) return TGP_E_INVAL;
-    if (V > TGP_SAMPLE_MAX_V || T > 32767 || B > TGP_PAGED_MAX_B) return TGP_E_TOO_LARGE;
+    if (V > TGP_SAMPLE_MAX_V || T > T_MAX || B > TGP_PAGED_MAX_B) return TGP_E_TOO_LARGE;
     if (!B) return TGP_OK;
     uint32_t ctas = V > 4096 ? CLUSTER_MAX : 1;
     while (ctas > 1 && B * ctas > 2u * (uint32_t)tgpk_sms()) ctas /= 2;

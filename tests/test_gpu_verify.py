@@ -196,3 +196,40 @@ def test_a_captured_call():
             lo, hi = first[b], first[b + 1]
             want = paged.verify(x[lo:hi], y[lo:hi], tokens[lo + 1:hi], u[lo:hi], v[b], temp) if n[b] else []
             assert list(got[lo:hi]) == want + [-1] * (n[b] - len(want)) and counts[b] == len(want)
+
+
+@pytest.mark.parametrize("start", [[0, 9, 0, 9, 0, 9], [0, 5, 2, 7, 6, 9], [3, 6, 0, 3, 6, 9], [0, 50, 2, 7, 7, 9], [0, 9, 9, 1, 4, 9], [-5, 4, 1, 8, 8, 8], [2, 2, 5, 4, 4, 9], [0, 3, 9, -1, 3, 9]])
+def test_rows_that_several_sequences_claim(start):
+    """They are the first one's: a sequence that begins before the start of one before it has none."""
+    rng = np.random.default_rng(12)
+    x, y, tokens = drafts(rng, [9], 5000)
+    u, v, t = rng.random(9).astype(np.float32), rng.random(5).astype(np.float32), np.array([1.0, 0.0, 0.8, 1.0, 1.5], np.float32)
+    for draft in (y, None):
+        out, n_out = run(x, draft, tokens, start, u, v, t)
+        left = np.full(9, -7)
+        for b, (lo, n) in enumerate(paged.rows(start, 9)):
+            rows = slice(lo, lo + n)
+            want = paged.verify(x[rows], None if draft is None else y[rows], tokens[lo + 1:lo + n], u[rows], v[b], float(t[b])) if n else []
+            left[lo:lo + n] = want + [-1] * (n - len(want))
+            assert n_out[b] == len(want)
+        assert list(out) == list(left)
+
+
+@pytest.mark.parametrize("B", [255, 256, 257, 700, 2000])
+def test_many_sequences_with_starts_that_fall(B):
+    """Beyond one turn of the counts: sequences behind one that claims the rows to the end, or that begin before others."""
+    rng = np.random.default_rng(B)
+    T, V = 600, 33
+    x, y, tokens = drafts(rng, [T], V)
+    u, v = rng.random(T).astype(np.float32), rng.random(B).astype(np.float32)
+    start = np.minimum(np.arange(B + 1) * 2 // 5, T)
+    start[rng.integers(0, B, B // 9)] -= rng.integers(1, 40, B // 9)
+    for start in (start, np.tile([0, T], B // 2 + 1)[:B + 1], np.where(np.arange(B + 1) == 200, T, start)):
+        out, n_out = run(x, y, tokens, start, u, v)
+        left = np.full(T, -7)
+        for b, (lo, n) in enumerate(paged.rows(start, T)):
+            rows = slice(lo, lo + n)
+            want = paged.verify(x[rows], y[rows], tokens[lo + 1:lo + n], u[rows], v[b]) if n else []
+            left[lo:lo + n] = want + [-1] * (n - len(want))
+            assert n_out[b] == len(want)
+        assert list(out) == list(left)

@@ -189,3 +189,24 @@ def test_oracle_verification_gives_the_targets_distribution():
     assert paged.verify(x, y, [0], [0, 0], 0.9, temperature=0.0) == [0, 0] and paged.verify(x, y, [1], [0, 0], 0.9, temperature=0.0) == [0]
     x[:, 3] = -np.inf
     assert paged.verify(x, x, [3], [0.5, 0], 0.9) == [2]   # nothing is left of p - p: a token of p
+
+
+def test_a_row_is_one_sequences_at_most():
+    """Starts of any numbers: no row is claimed twice, so no line of rows is longer than the arrays; and starts that ascend are taken as they are."""
+    rng = np.random.default_rng(2)
+    for T in (1, 7, 100, 32767):
+        for B in (1, 2, 5, 400):
+            for wild in (False, True):
+                for _ in range(20):
+                    start = rng.integers(0, T + 1, B + 1)
+                    if wild:
+                        start = np.where(rng.random(B + 1) < 0.2, rng.choice([-1, T + 1, 2 ** 31 - 1, -2 ** 31], B + 1), start)
+                    used = np.zeros(T, int)
+                    for first, n in paged.rows(start, T):
+                        used[first:first + n] += 1
+                        assert n >= 0 and (n == 0 or 0 <= first < first + n <= T)
+                    assert used.max() <= 1
+                    start = np.sort(rng.integers(0, T + 1, B + 1))
+                    assert paged.rows(start, T) == [(s, e - s) for s, e in zip(start, start[1:])]
+    assert paged.rows([0, 9, 0, 9, 0, 9], 9) == [(0, 9), (9, 0), (0, 0), (9, 0), (0, 0)]
+    assert paged.rows([0, 5, 2, 7, 6, 9], 9) == [(0, 5), (5, 0), (2, 0), (7, 0), (6, 0)] and paged.rows([0, 50, 2, 7], 9) == [(0, 0), (50, 0), (2, 5)]
