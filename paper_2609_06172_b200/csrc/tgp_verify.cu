@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(STAT_THREADS, 3) tgp_verify_stat_kernel(const 
                 sums[1] = 0.0;
                 weight = higher;
                 plain = !higher.sharp && higher.low > -FLT_MAX;
-                limit = higher.sharp ? m : (float)((double)m + 0.4 * of_rate);
+                limit = higher.sharp ? m : fminf((float)((double)m + 0.4 * of_rate), FLT_MAX);      // (an infinite one is above any)
             }
             top = m;
         }

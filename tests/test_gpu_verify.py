@@ -233,3 +233,20 @@ def test_many_sequences_with_starts_that_fall(B):
             left[lo:lo + n] = want + [-1] * (n - len(want))
             assert n_out[b] == len(want)
         assert list(out) == list(left)
+
+
+@pytest.mark.parametrize("t", [1e37, np.inf])
+def test_an_infinite_logit_late_in_a_row_of_a_high_temperature(t):
+    """More parts of rows than CTAs, so that threads meet the infinite logit behind others of its row, where a temperature's span is beyond the largest number."""
+    rng = np.random.default_rng(10)
+    V, n = 128256, [5] * 12
+    x, y = (rng.standard_normal((60, V)).astype(np.float32) for _ in range(2))
+    tokens = rng.integers(0, V, 60)
+    for r in range(60):
+        x[r, 4096 * (1 + 7 * r % 31) + 5 + r] = np.inf
+        if r % 3 == 0:
+            y[r, 4096 * (1 + 5 * r % 31) + 77] = np.inf
+    tokens[1::4] = [int(np.argmax(x[r])) for r in range(0, 60, 4)]                 # some are the only ones that the target has
+    got = check(x, y, tokens, n, rng.random(60), rng.random(12), np.full(12, t))
+    assert (got > 1).any()
+    check(x, None, tokens, n, rng.random(60), rng.random(12), np.full(12, t))
