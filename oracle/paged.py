@@ -105,7 +105,7 @@ def verify(x, y, drafted, u, u_draw, temperature=1.0):
         last = i == n - 1
         if not temperature > 0:
             out.append(likeliest(x[i]))
-            if last or drafted[i] != out[-1]:
+            if last or drafted[i] != out[-1] or not (np.asarray(x[i]) > -np.inf).any():             # (a row of nothing takes no token)
                 return out
             continue
         p = softmax(x[i], temperature)

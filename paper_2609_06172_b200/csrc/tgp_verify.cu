@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(DRAW_THREADS, 2) tgp_verify_draw_kernel(const 
         __syncthreads();
         if (judge) {
             const Stat x = kept[0][tid], y = drawn ? kept[1][tid] : Stat{1.0, 0.f, 0};
-            bool taken = d == x.at;                              // (the likeliest)
+            bool taken = d == x.at && x.top > -INFINITY;         // (the likeliest; a row of nothing takes none)
             if (s.rate != 0.0) {
                 const double p = real && x.top > -INFINITY ? Weights(x.top, s.rate, s.span)(x_d, table) : 0.0;
                 const double q = !drawn ? 1.0 : real && y.top > -INFINITY ? Weights(y.top, s.rate, s.span)(y_d, table) : 0.0;

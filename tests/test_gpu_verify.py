@@ -250,3 +250,18 @@ def test_an_infinite_logit_late_in_a_row_of_a_high_temperature(t):
     got = check(x, y, tokens, n, rng.random(60), rng.random(12), np.full(12, t))
     assert (got > 1).any()
     check(x, None, tokens, n, rng.random(60), rng.random(12), np.full(12, t))
+
+
+@pytest.mark.parametrize("t", [0.0, -1.0, np.nan, 1.0])
+@pytest.mark.parametrize("V", [700, 9000])
+def test_a_row_of_nothing_takes_no_token(V, t):
+    """Not token 0 either, which is what it gives."""
+    rng = np.random.default_rng(11)
+    x, y, tokens = drafts(rng, [4] * 4, V)
+    x[0], x[5], x[10], x[15] = -np.inf, np.nan, np.where(np.arange(V) % 2, np.nan, -np.inf), -np.inf
+    for r in (0, 4, 5, 8, 9, 10):
+        tokens[r + 1] = 0                                        # also behind rows that have other tokens
+    x[[4, 8, 9], 0] = 50.0                                       # there it is the likeliest
+    for draft in (y, None):
+        got = check(x, draft, tokens, [4] * 4, np.zeros(16), rng.random(4), np.full(4, t))
+        assert list(got[:3]) == [1, 2, 3]

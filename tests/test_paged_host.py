@@ -210,3 +210,11 @@ def test_a_row_is_one_sequences_at_most():
                     assert paged.rows(start, T) == [(s, e - s) for s, e in zip(start, start[1:])]
     assert paged.rows([0, 9, 0, 9, 0, 9], 9) == [(0, 9), (9, 0), (0, 0), (9, 0), (0, 0)]
     assert paged.rows([0, 5, 2, 7, 6, 9], 9) == [(0, 5), (5, 0), (2, 0), (7, 0), (6, 0)] and paged.rows([0, 50, 2, 7], 9) == [(0, 0), (50, 0), (2, 5)]
+
+
+def test_oracle_a_row_of_nothing_takes_no_token():
+    x = np.full((3, 5), -np.inf)
+    x[1] = np.nan
+    for t in (0.0, -1.0, np.nan, 1.0):
+        for r in (0, 1):
+            assert paged.verify(x[[r, 2]], None, [0], [0.0, 0.0], 0.5, t) == [0]
