@@ -265,3 +265,20 @@ def test_a_row_of_nothing_takes_no_token(V, t):
     for draft in (y, None):
         got = check(x, draft, tokens, [4] * 4, np.zeros(16), rng.random(4), np.full(4, t))
         assert list(got[:3]) == [1, 2, 3]
+
+
+@pytest.mark.parametrize("V", [300, 5000])
+@pytest.mark.parametrize("t", [1.0, 0.0])
+def test_long_drafts(V, t):
+    """Rows are judged 32 at a time: first refusals in the first, second and third turn, at their ends, and none."""
+    rng = np.random.default_rng(13)
+    stop = {70: 64, 40: 35, 33: None, 32: 30, 31: None, 34: 32, 65: None, 100: 31, 97: 95, 64: 63}
+    n = list(stop)
+    x, _, tokens = drafts(rng, n, V, away=0.0, temperature=np.full(len(n), t))
+    y, start = x.copy(), np.concatenate(([0], np.cumsum(n)))
+    for lo, (rows, i) in zip(start, stop.items()):
+        if i is not None and i + 1 < rows:
+            x[lo + i, tokens[lo + i + 1]] = -np.inf
+    for draft in (y, None) if t == 0 else (y,):
+        got = check(x, draft, tokens, n, np.full(len(x), 0.9), rng.random(len(n)), np.full(len(n), t))
+        assert list(got) == [rows if i is None or i + 1 == rows else i + 1 for rows, i in stop.items()]
