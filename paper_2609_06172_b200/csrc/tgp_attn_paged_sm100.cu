@@ -405,6 +405,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
         for (uint32_t n = 0, i0 = 0; ok && tile_at(t, n, ok); ++n) {
             const TgpPagedKeys keys = keys_of(t);
             const uint32_t nblk = keys.chunks, qpos = t.pos + min(tok, t.tokens - 1);    // padding rows take the last token's mask
+            const bool row_ok = tid < t.tokens * a.G;
             float m_ref = -FLT_MAX, lrow = 0.f;                              // exponent reference and running sum of this row
             for (uint32_t jb = 0; jb < nblk; ++jb) {
                 const uint32_t i = i0 + jb, key0 = keys.chunk(jb) * BKV, buffer = tmem_S + lane_addr + (i & 1) * BKV;
@@ -430,16 +431,17 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
 #pragma unroll
                         for (uint32_t e = 0; e < 32; ++e) if (h >> e & 1) s[e] = -INFINITY;
                     }
-                    // The exponent reference m_ref is the row's maximum of the tile's first keys, moved only where a sum says that a score lies more than about 2^40 above it (or overflowed).  A
+                    // The exponent reference m_ref is the row's maximum of the tile's first keys, moved only where its own sum says that a score lies more than about 2^40 above it (or overflowed):
+                    // the others of the warp keep theirs, so that a row's bits do not depend on its neighbours, and rows that nobody has (the next sequence's queries) do not ask.  A
                     // row that sees nothing of the first ones has the lowest finite reference: its sums are 0, and the first finite score moves it.
                     uint32_t w[16];
                     float sum;
-                    for (bool move = (jb | half) == 0;;) {
+                    for (bool move = (jb | half) == 0, own = move;;) {
                         if (move) {                                          // the maximum of the scaled scores (scale > 0: it commutes with it)
                             float m0 = max3(s[0], s[1], s[2]), m1 = max3(s[3], s[4], s[5]);
 #pragma unroll
                             for (uint32_t e = 6; e + 3 < 32; e += 4) { m0 = max3(m0, s[e], s[e + 1]); m1 = max3(m1, s[e + 2], s[e + 3]); }
-                            const float m_new = fmaxf(m_ref, max3(m0, m1, fmaxf(s[30], s[31])) * a.sl2), alpha = ex2(m_ref - m_new);
+                            const float m_new = own ? fmaxf(m_ref, max3(m0, m1, fmaxf(s[30], s[31])) * a.sl2) : m_ref, alpha = ex2(m_ref - m_new);
                             m_ref = m_new;
                             lrow *= alpha;
                             if (half) {                                      // the first half's weights
@@ -479,7 +481,8 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
                         float l0, l1;
                         unpack2(add2(acc0, acc1), l0, l1);
                         sum = l0 + l1;
-                        if (move || !__any_sync(0xffffffffu, !(sum <= 0x1p40f))) break;
+                        own = sum > 0x1p40f && row_ok;                       // (a NaN is one with any reference)
+                        if (move || !__any_sync(0xffffffffu, own)) break;
                         move = true;
                     }
                     if (!ok) break;
@@ -496,7 +499,7 @@ __global__ void __launch_bounds__(THREADS, 2) tgp_attn_paged_many_kernel(const _
             ok = ok && wait(bar_o + (i0 - 1 & 1), (i0 - 1 >> 1) & 1, 2) && wait(bar_odd, n & 1, 2);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const bool empty = lrow == 0.f, row_ok = tid < t.tokens * a.G;   // a row that sees nothing is zero
+            const bool empty = lrow == 0.f;                                  // a row that sees nothing is zero
             const float inv = 1.0f / lrow;
             bf16 *dst = a.o + ((size_t)(t.row + tok) * a.Hq + t.hk * a.G + (tid - tok * a.G)) * DH;
 #pragma unroll 1

@@ -476,3 +476,29 @@ def test_a_scratch_is_good_for_the_next_call_when_a_wait_ran_out(rows):
             call()
             torch.cuda.synchronize()
             assert tb.k_attn_status() == 0 and np.array_equal(f64(o).reshape(want.shape), want)
+
+
+def assert_bits(got, want, rows):
+    """Equal bits (in 64 bits, so NaN as NaN) of these rows, which are numbers."""
+    rows = np.asarray(rows)
+    assert np.isfinite(want[rows]).all() and np.array_equal(got[rows], want[rows]), np.argwhere(got[rows] != want[rows])[:5]
+
+
+OF_ITS_OWN = [[(33, 300), (50, 420), (1, 200), (41, 41)], [(4, 300), (3, 170), (1, 200), (2, 900)], [(2, 40), (60, 700), (4, 90), (5, 333)], [(1, 500), (1, 90), (1, 700)]]
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 4)])
+@pytest.mark.parametrize("rows", OF_ITS_OWN)
+def test_a_rows_bits_do_not_depend_on_what_other_sequences_hold(rows, window, sinks):
+    """Queries and values of one sequence made large or no numbers: the others, of the same lengths, keep their bits."""
+    for Dh in (64, 128):
+        b = Batch(8, 2, Dh, 16, rows, seed=23, std=2.0)
+        want = b.run(window, sinks)
+        for change in range(len(rows)):
+            others = [t for i in range(len(rows)) if i != change for t in range(b.start[i], b.start[i + 1])]
+            for value in (1e3, np.nan, np.inf):
+                o = Batch(8, 2, Dh, 16, rows, seed=23, std=2.0)
+                o.q[o.start[change]:o.start[change + 1]] *= value
+                pages = o.table[change][o.table[change] >= 0]
+                o.v[pages] *= value
+                assert_bits(o.run(window, sinks), want, others)
