@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
             __syncthreads();
         }
         // The reference m of a row's exponents follows its maximum where that is more than 2^LIFT above it: weights and sums are floating point, and are as exact anywhere.  So a chunk
-        // asks one question of all rows, and O is hardly ever multiplied.  (It starts from the least number, not from -inf: scores of -inf weigh nothing then, in whichever chunk they are met.)
+        // asks one question of all rows, those for which it is true move, and O is hardly ever multiplied.  (It starts from the least number, not from -inf: scores of -inf weigh nothing then, in whichever chunk they are met.)
         float o[MT][DH / 8][4], m[MT][2], l[MT][4];                         // l: the sums of the rounded weights, of rows r (0) and r + 8 (2), by a product with ones
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
@@ -344,8 +344,9 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
                     for (int e = 0; e < 2; ++e) {
                         float best = fmaxf(fmaxf(s[t][0][2 * e], s[t][0][2 * e + 1]), fmaxf(s[t][1][2 * e], s[t][1][2 * e + 1]));
                         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
-                        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2)) * a.sl2;
-                        if (!(best > m[t][e])) best = m[t][e];
+                        best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 2));
+                        // only a row that asked itself (its largest exponent, by the same operation): its bits do not depend on the others
+                        best = fmaf(best, a.sl2, -m[t][e]) > LIFT ? best * a.sl2 : m[t][e];
                         const float alpha = ex2(m[t][e] - best);             // (the first time: of zeros)
                         m[t][e] = best;
                         l[t][2 * e] *= alpha;

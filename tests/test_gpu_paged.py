@@ -502,3 +502,19 @@ def test_a_rows_bits_do_not_depend_on_what_other_sequences_hold(rows, window, si
                 pages = o.table[change][o.table[change] >= 0]
                 o.v[pages] *= value
                 assert_bits(o.run(window, sinks), want, others)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (60, 4)])
+@pytest.mark.parametrize("rows", OF_ITS_OWN)
+def test_a_rows_bits_do_not_depend_on_other_queries(rows, window, sinks):
+    """Of the same sequence: another token's, another head's."""
+    for Dh in (64, 128):
+        b = Batch(8, 2, Dh, 16, rows, seed=24, std=2.0)
+        q, want = b.q.copy(), b.run(window, sinks)
+        for value in (1e3, np.nan):
+            b.q = q.copy()
+            b.q[1::3] *= value
+            assert_bits(b.run(window, sinks), want, [t for t in range(b.T) if t % 3 != 1])
+            b.q = q.copy()
+            b.q[:, 1::3] *= value
+            assert_bits(b.run(window, sinks)[:, [0, 2, 3, 5, 6]], want[:, [0, 2, 3, 5, 6]], range(b.T))
