@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
                 mma_bf16(l[t], pa[t][0], pa[t][1], pa[t][2], pa[t][3], ONES, ONES);
             }
             // ---- O += P V ----
-            // Where some rows see a key and others do not, a value that is no number must not reach the others as 0 x inf: then each row adds up what it sees.
+            // Where some rows see a key and others do not, a value that is no number must not reach the others as 0 x inf: it is added to the rows that see it, and zero in the product, which is the same
+            // operations for the others as with any number there.
             bool each = false;
             if (!whole && now.s.n > 1) {
                 for (uint32_t i = lane; i < KEYS * CPR; i += 32) {
@@ -375,18 +376,7 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
                 }
                 each = __any_sync(0xffffffffu, each);
             }
-            if (!each) {
-#pragma unroll
-                for (int jp = 0; jp < DH / 16; ++jp) {
-                    uint32_t v0, v1, v2, v3;
-                    ldsm_x4_t(at + v_get ^ jp << 5, v0, v1, v2, v3);
-#pragma unroll
-                    for (int t = 0; t < MT; ++t) {
-                        mma_bf16(o[t][2 * jp], pa[t][0], pa[t][1], pa[t][2], pa[t][3], v0, v1);
-                        mma_bf16(o[t][2 * jp + 1], pa[t][0], pa[t][1], pa[t][2], pa[t][3], v2, v3);
-                    }
-                }
-            } else {
+            if (each) {
 #pragma unroll 1
                 for (uint32_t key = 0; key < KEYS; ++key) {
                     const int from = (lane & ~3) | (key % 8 / 2);           // the lane of this row that has the key's weight
@@ -401,9 +391,30 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
                             for (int j = 0; j < DH / 8; ++j) {
                                 uint32_t v;
                                 asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at + KV_BYTES + key * ROW + ((j ^ (key & 7)) << 4) + 4 * c));
-                                if (sees) { o[t][j][2 * e] += w * __uint_as_float(v << 16); o[t][j][2 * e + 1] += w * __uint_as_float(v & 0xffff0000u); }
+                                const float v0 = __uint_as_float(v << 16), v1 = __uint_as_float(v & 0xffff0000u);
+                                if (sees && !(fabsf(v0) < INFINITY)) o[t][j][2 * e] += w * v0;
+                                if (sees && !(fabsf(v1) < INFINITY)) o[t][j][2 * e + 1] += w * v1;
                             }
                         }
+                }
+                __syncwarp();
+                for (uint32_t i = lane; i < KEYS * CPR * 4; i += 32) {
+                    uint32_t v;
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at + KV_BYTES + i * 4));
+                    if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+                    if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+                    asm volatile("st.shared.b32 [%0], %1;" ::"r"(at + KV_BYTES + i * 4), "r"(v) : "memory");
+                }
+                __syncwarp();
+            }
+#pragma unroll
+            for (int jp = 0; jp < DH / 16; ++jp) {
+                uint32_t v0, v1, v2, v3;
+                ldsm_x4_t(at + v_get ^ jp << 5, v0, v1, v2, v3);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    mma_bf16(o[t][2 * jp], pa[t][0], pa[t][1], pa[t][2], pa[t][3], v0, v1);
+                    mma_bf16(o[t][2 * jp + 1], pa[t][0], pa[t][1], pa[t][2], pa[t][3], v2, v3);
                 }
             }
             __syncwarp();                                                   // the stage may be refilled

@@ -518,3 +518,27 @@ def test_a_rows_bits_do_not_depend_on_other_queries(rows, window, sinks):
             b.q = q.copy()
             b.q[:, 1::3] *= value
             assert_bits(b.run(window, sinks)[:, [0, 2, 3, 5, 6]], want[:, [0, 2, 3, 5, 6]], range(b.T))
+
+
+@pytest.mark.parametrize("value", [np.nan, np.inf])
+@pytest.mark.parametrize("rows", OF_ITS_OWN)
+def test_a_rows_bits_do_not_depend_on_values_that_it_does_not_see(rows, value):
+    """Keys and values behind a row, or before its window, that other rows of the sequence see."""
+    for Dh in (64, 128):
+        b = Batch(8, 2, Dh, 16, rows, seed=25, std=2.0)
+        for window, sinks in ((0, 0), (60, 4)):
+            want = b.run(window, sinks)
+            for back in (0, 1):                                  # what the last row alone sees; with a window, what the first row alone sees
+                o = Batch(8, 2, Dh, 16, rows, seed=25, std=2.0)
+                keep = []
+                for i, (n, e) in enumerate(rows):
+                    first = e - n
+                    p = first - window + 1 if back else e - 1
+                    if n < 2 or (back and (not window or p < sinks)):
+                        keep += range(b.start[i], b.start[i + 1])
+                        continue
+                    page = o.table[i, p // 16]
+                    o.v[page, :, p % 16, 3::5] = value
+                    o.k[page, :, p % 16, 7] = np.nan
+                    keep += range(b.start[i] + 1, b.start[i + 1]) if back else range(b.start[i], b.start[i + 1] - 1)
+                assert_bits(o.run(window, sinks), want, keep)
