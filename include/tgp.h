@@ -502,11 +502,14 @@ int  tgp_k_rope_kv_paged(const float *q32, const float *k32, const float *v32, v
                          const int32_t *pos_dev, const tgp_model_cfg *cfg, uint32_t T, uint32_t n_pages, void *stream);
 /* Attention of a step's rows over the pages: single tokens, drafted tokens and prompts in one call.  The row at position p sees the positions j <= p - with window > 0 those of them with
  * j > p - window or j < sinks -: o = softmax(q K^T / sqrt(Dh)) V, bf16 [T, Hq*Dh].  q_max and kv_max are bounds of the rows of a sequence and of end[b]; a sequence beyond them, or with end[b] less
- * than its rows, is idle: its rows of o are zero.  Rows of no sequence keep what they hold, and with start outside [0, T] or falling a sequence has no rows.  A position whose table entry lies outside [0, n_pages)
+ * than its rows, is idle: its rows of o are zero.  With B, T, q_max or kv_max 0 the call does nothing: o keeps what it holds.  Rows of no sequence keep what they hold, and with start outside [0, T] or falling a sequence
+ * has no rows; a row that several sequences claim holds anything.  A position whose table entry lies outside [0, n_pages)
  * is not seen; a row that sees nothing is zero.  Entries of positions that no row sees (before a window, behind the sequence) are not read as pages.  What the pages hold in positions that a row does not
  * see does not reach it, NaN or not.  Dh is 64 or 128, TK a multiple of 16, at most 128 query heads share a KV head; kv_max <= max_len.
- * Softmax weights are rounded to bf16 (half a step is 2^-8 of a weight), sums are fp32.  Sequences of up to 16 rows * query heads per KV head (32 where q_max has more than 16) are split
- * over the GPU by their lengths, prompts go to the tcgen05 kernel; a row's bits may depend on the lengths of the other sequences (how a context is split), and not on anything else.
+ * Softmax weights are rounded to bf16 (half a step is 2^-8 of a weight; tgp_k_attn() keeps more of them in short contexts), sums are fp32.  A reference is subtracted from the scores
+ * that is not always the largest: a weight may reach 2^16, those of 32 keys of a prompt together 2^40, before another one is taken.  So values with |v| * kv_max < 2^88 cannot overflow in the sums; larger ones may, though their
+ * mean is finite.  Sequences of up to 16 rows * query heads per KV head (32 where q_max has more than 16) are split over the GPU by their lengths, prompts go to the tcgen05 kernel; besides on what it sees a row's bits may depend on B, on q_max and on the lengths of the other sequences (which kernel, and how a context is split), but not on
+ * what other rows or unseen positions hold.
  * scratch_dev: tgp_k_attn_paged_scratch_bytes() for at least these arguments, of any contents, not shared with a call that may run at the same time; between two calls that share it other use is fine.
  * B * Hkv * ceil(kv_max / 16) and n_pages * TK * Hkv have to stay below 2^31 (TGP_E_TOO_LARGE). */
 int  tgp_k_attn_paged(const void *qb, const void *k_pages, const void *v_pages, void *ob, const int32_t *table_dev, const int32_t *start_dev, const int32_t *end_dev, const tgp_model_cfg *cfg,
@@ -538,7 +541,7 @@ int  tgp_k_sample(const float *logits, const float *u_dev, int32_t *out, uint32_
  * out [T]: in the rows of a sequence the tokens that it goes on with - those taken and the one drawn -, then -1; n_out [B]: how many (0 for a sequence without rows, whose rows do not lie in [0, T), or that begins before
  * the start of a sequence before it, where that is in [0, T]: a row is one sequence's at most).  Rows of no sequence keep what they hold.  What stays in the cache are the rows fed with tokens that hold: length before the step + n_out.
  * temperature fp32 [B] or NULL (1); a row's 0, negative or NaN: d is taken if it is the row's likeliest token (the lowest of equals), which also is the token that follows.  Logits of -inf and NaN
- * weigh nothing (so filters may be applied to both by -inf); a row of nothing else takes no token and gives token 0.  A drafted token outside [0, V) is not taken.  u and u_draw are limited to [0, 1].  Weights and sums are in 64 bits, weights
+ * weigh nothing (so filters may be applied to both by -inf); a row of nothing else takes no token and gives token 0.  A drafted token outside [0, V) is not taken.  u and u_draw are limited to [0, 1].  Weights and sums are in 64 bits, a weight right to 2^-41 of itself, weights
  * of less than 2^-1000 of a row's largest are 0.  draft_logits of a sequence's last row are not read.  scratch_dev: tgp_k_verify_scratch_bytes(), not shared with a call that may run at the same time.  T <= 32767, V <= TGP_SAMPLE_MAX_V. */
 int  tgp_k_verify(const float *logits, const float *draft_logits, const int32_t *tokens_dev, const int32_t *start_dev, const float *u_dev, const float *u_draw_dev, int32_t *out_dev, int32_t *n_out_dev,
                   uint32_t B, uint32_t T, uint32_t V, const float *temperature_dev, void *scratch_dev, void *stream);

@@ -542,3 +542,27 @@ def test_a_rows_bits_do_not_depend_on_values_that_it_does_not_see(rows, value):
                     o.k[page, :, p % 16, 7] = np.nan
                     keep += range(b.start[i] + 1, b.start[i + 1]) if back else range(b.start[i], b.start[i + 1] - 1)
                 assert_bits(o.run(window, sinks), want, keep)
+
+
+def test_large_values():
+    """|V| * kv_max up to 2^88 stays finite, with scores that grow as far as they can without another reference: V times a power of two is the result times it."""
+    for rise in (0.0, 10.5, 24.0):                               # times log2(e): 15.1 and 34.6; weights of 2^16 (few rows) and, over 32 keys, 2^40 (prompts) move the reference
+        b = Batch(4, 2, 64, 16, [(1, 400), (3, 350), (90, 400), (1, 8)], seed=26)
+        b.q[:, :, 1:] *= 0.01
+        b.q[:, :, 0] = 8.0
+        for i, (n, e) in enumerate(b.rows):
+            for p in range(e):
+                b.k[b.table[i, p // 16], :, p % 16, 0] = 0.0 if p < 64 else rise
+        b.check(some=11)
+        d = b.device()
+        d["v"] = d["v"] * 2.0 ** 76                              # of |V| up to some 4.5 * 2^76, by 400 keys
+        assert d["v"].nan_to_num(0.0).abs().max().item() * 400 <= 2.0 ** 88
+        b.check(got=b.run(dev=d) * 2.0 ** -76, some=11)
+
+
+@pytest.mark.parametrize("bounds", [dict(q_max=0), dict(kv_max=0), dict(q_max=0, kv_max=0)])
+def test_bounds_of_nothing_leave_the_rows_as_they_are(bounds):
+    b = Batch(8, 2, 64, 16, [(1, 40), (2, 60)], seed=27)
+    for name, value in bounds.items():
+        setattr(b, name, value)
+    assert (b.run() == 7).all()
