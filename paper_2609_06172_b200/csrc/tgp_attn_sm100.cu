@@ -464,8 +464,10 @@ int tgpk_attn_wait_test(unsigned long long limit_ns, int withhold_step) {
 
 int tgpk_attn_status_clear() { const int z = 0; return cudaMemcpyToSymbol(g_attn_tc_error, &z, sizeof(z)) == cudaSuccess ? TGP_OK : TGP_E_CUDA; }
 
+int tgpk_attn_status(int *code) { return cudaMemcpyFromSymbol(code, g_attn_tc_error, sizeof(int)) == cudaSuccess ? TGP_OK : TGP_E_CUDA; }
+
 extern "C" int tgp_k_attn_status(int *error_code) {
     if (!error_code) return TGP_E_INVAL;
-    if (cudaMemcpyFromSymbol(error_code, g_attn_tc_error, sizeof(int)) != cudaSuccess) return TGP_E_CUDA;
+    if (int rc = tgpk_attn_status(error_code)) return rc;
     return *error_code ? TGP_OK : tgpk_attn_paged_status(error_code);
 }

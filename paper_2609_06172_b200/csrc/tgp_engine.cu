@@ -1030,7 +1030,7 @@ extern "C" int tgp_step(tgp_ctx *ctx, uint32_t step_kind, const int32_t *tokens_
         // the step has been waited for: a tensor-core kernel whose bounded wait ran out has left its mark
         int gemm_err = 0, attn_err = 0, bad_tok = 0;
         uint32_t bad_row = 0; int32_t bad_id = 0;
-        if (tgp_k_gemm_status(&gemm_err) == TGP_OK && tgp_k_attn_status(&attn_err) == TGP_OK && (gemm_err || attn_err))
+        if (tgp_k_gemm_status(&gemm_err) == TGP_OK && tgpk_attn_status(&attn_err) == TGP_OK && (gemm_err || attn_err))
             return tgp_fail(ctx, TGP_E_CUDA, "a tensor-core kernel gave up on a bounded wait (GEMM code " + std::to_string(gemm_err) + ", attention code " + std::to_string(attn_err) + "): results of this step are incomplete");
         if (tgp_k_embed_status(&bad_tok, &bad_row, &bad_id) == TGP_OK && bad_tok)
             return tgp_fail(ctx, TGP_E_CUDA, "the embedding gather met token id " + std::to_string(bad_id) + " (row " + std::to_string(bad_row) + "), outside the vocabulary: that row was computed from zeros");

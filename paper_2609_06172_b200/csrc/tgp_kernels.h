@@ -98,6 +98,7 @@ int tgp_rope_tables_upload(uint32_t Dh, uint32_t max_len, float base, float *cos
 // reset of the tensor-core kernels' error words (tgp_gemm_sm100.cu, tgp_attn_sm100.cu)
 int tgpk_gemm_status_clear();
 int tgpk_attn_status_clear();
+int tgpk_attn_status(int *error_code);       // of the attention over KV tiles alone, which a step of the engine uses
 // the same of the attention over pages (tgp_attn_paged_sm100.cu), and its error word
 int tgpk_attn_paged_status_clear();
 int tgpk_attn_paged_status(int *error_code);

@@ -544,6 +544,37 @@ def test_a_rows_bits_do_not_depend_on_values_that_it_does_not_see(rows, value):
                 assert_bits(o.run(window, sinks), want, keep)
 
 
+def test_a_step_of_the_engine_is_not_told_of_a_wait_over_pages():
+    """A wait of the attention over pages that ran out is its caller's to see (tgp_k_attn_status): a planned pass, which has no pages, goes on."""
+    import seeded_inputs as si
+    from conftest import MACHINE
+    from paper_2609_06172_b200.runner import Runner, pinned_pool
+    from paper_2609_06172_b200.session import Session
+    b = Batch(8, 2, 128, 64, [(64, 300)], seed=28)
+    d, (scratch, _) = b.device(), b.scratch()
+    o = torch.zeros(b.T, 1024, dtype=torch.bfloat16, device=DEV)
+    tb.k_wait_test(2_000_000, 1)
+    try:
+        tb.k_attn_paged(d["q"], d["k"], d["v"], o, d["table"], d["start"], d["end"], b.c, 1, b.T, b.q_max, b.kv_max, b.n_pages, 0, 0, scratch)
+        torch.cuda.synchronize()
+    finally:
+        tb.k_wait_test(0, 0)
+    try:
+        assert tb.k_attn_status() in (1, 2, 3)
+        cfg = si.CONFIGS[1]
+        lay = si.build_layout(cfg)
+        pool = pinned_pool(lay.pool_bytes)
+        si.fill_pool(lay, pool.numpy())
+        s = Session(lay, MACHINE, pool_base=pool.data_ptr(), pool_flags=tb.POOL_PINNED)
+        s.plan(T=1)
+        r = Runner(s, cfg.B * cfg.S)
+        assert r.step(tb.PREFILL, si.prompt_tokens(cfg), cfg.S, want_stats=True).n_launches > 0
+        s.close()
+        assert tb.k_attn_status() in (1, 2, 3)
+    finally:
+        tb.k_status_clear()
+
+
 def test_large_values():
     """|V| * kv_max up to 2^88 stays finite, with scores that grow as far as they can without another reference: V times a power of two is the result times it."""
     for rise in (0.0, 10.5, 24.0):                               # times log2(e): 15.1 and 34.6; weights of 2^16 (few rows) and, over 32 keys, 2^40 (prompts) move the reference
