@@ -9,8 +9,8 @@
 // device only, so every CTA adds up the sequences' chunks for itself.  Where a stretch ends inside a (sequence, KV head), its CTA leaves (maximum, sum, output) in the scratch, and the last one to arrive at that pair's counter merges them
 // all in the order of the stretches, so that results do not depend on who was last.
 //
-// What bounds it: HBM where contexts are long (24 of up to 12000 keys, 64 heads of 128 over 8: 106 us, 6.1 TB/s; 61 of up to 2500, 32 over 8: 63 us, 5.2 TB/s), else a fixed 3.5 us - a launch, the sequences'
-// counts, table, keys, the merge in the CTA - and where CTAs share a context another 3 of their merge, each a chain of memory latencies, and with 17 to 32 rows the instructions (32 sequences of five tokens that see 1028 keys: 34 us, 0.57 of HBM's rate).  A chunk's
+// What bounds it: HBM where contexts are long (24 of up to 12000 keys, 64 heads of 128 over 8: 106 us, 6.1 TB/s; 61 of up to 2500, 32 over 8: 63 us, 5.3 TB/s), else a fixed 3.5 us - a launch, the sequences'
+// counts, table, keys, the merge in the CTA - and where CTAs share a context another 3 of their merge, each a chain of memory latencies, and with 17 to 32 rows the instructions (32 sequences of five tokens that see 1028 keys: 35 us, 0.56 of HBM's rate; 2500 keys without a window 51.6, 0.54).  A chunk's
 // second tile of rows is multiplied even for sequences that have only one: leaving it out by a test was no faster.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
@@ -534,7 +534,9 @@ __global__ void __launch_bounds__(WARPS * 32, DH == 128 ? 2 : MT == 1 ? 4 : 3) t
     if (f.beside) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// CTAs that the GPU holds at a time
+// CTAs that the GPU holds at a time, of launches of up to some 360 sequences.  Above, their 20 bytes each in shared memory leave three CTAs an SM instead of four (heads of 64, one tile of rows: from 369 sequences on), or
+// one instead of two (heads of 128, two tiles: from 420 on), and the grid's stretches take two turns: 368 -> 384 single tokens over up to 600 keys, 8 heads of 64 over 2, 19.2 -> 29.8 us; 416 -> 432 of up to five drafted
+// tokens, heads of 128, 45.0 -> 73.5.
 template <int DH, int MT> uint32_t few_ctas() { return (uint32_t)tgpk_sms() * (DH == 128 ? 2u : MT == 1 ? 4u : 3u); }
 
 template <int DH, int MT>

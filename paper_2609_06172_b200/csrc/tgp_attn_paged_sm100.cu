@@ -16,8 +16,8 @@
 // is freed and nothing is stored.
 //
 // What bounds it: a block of 64 keys takes one CTA some 1670 cycles and two on an SM 2400 together, 512 of them the tensor pipe's and as many the exponentials' for each by arithmetic; the rest is their chain within a CTA, and the
-// instruction cache: loops that few rows reach are not unrolled, and a block is exponentiated in halves by the same code (together 207 -> 182 us in the case below).  A tile costs some 7600 cycles besides.  Three prompts of up to 2500 tokens, 64 heads
-// of 128 over 8, a window of 1000: 181 - 190 us behind calls of its own kind, 0.40 of what the products alone take at 1667 TFLOP/s (tensor pipe 37 %, exponentials' 38 % busy).  No step bounds it by itself: copies without exponentials, most of
+// instruction cache: loops that few rows reach are not unrolled, and a block is exponentiated in halves by the same code (together 207 -> 181 us in the case below, in turn).  A tile costs some 7600 cycles besides.  Three prompts of up to 2500 tokens, 64 heads
+// of 128 over 8, a window of 1000: 189 - 196 us behind calls of its own kind, 189 - 190 between appends, 0.39 to 0.40 of what the products alone take at 1667 TFLOP/s (tensor pipe 37 %, exponentials' 38 % busy).  Without the window 218 - 237, 0.44 to 0.48.  No step bounds it by itself: copies without exponentials, most of
 // S, most of P V or the loads took 2 to 6 % less, one without the softmax 12 %.  Not better: blocks of 128 keys, those shared by two tiles in one CTA an SM, all of a block's scores at a time, 16 columns of S at a time,
 // exponentials of a quarter or half of the pairs by polynomials (even), eight softmax warps that share rows (198 us), a tile's keys split over several CTAs and joined where there are few tiles (even there, and 1.1 times as
 // long elsewhere by its code alone).

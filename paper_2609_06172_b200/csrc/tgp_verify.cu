@@ -7,7 +7,8 @@
 // first row that refuses, adds up what may be drawn there by segments of the vocabulary and their units, and goes through the one unit that the random number falls into.
 // The first kernel takes instructions and HBM in about equal parts: 32 sequences of up to five rows of 128256 logits with a draft's, 134 MB, some 38 us (HBM: 20; more than half of the issue slots).  Three operations
 // in 64 bits and ten in 32 per weight instead of seven in 64 took as long, two CTAs of 384 threads an SM too; four of 256 took 2 % longer.  The second one takes 20 us of it, a chain: rows judged, one row of each sequence weighed from L2 or
-// HBM, sums over the cluster, the token found.  Both 63 us; one sequence, 32000 logits, 14 us.
+// HBM, sums over the cluster, the token found.  Both 63.5 us (42.8 where the draft has no distribution, 16.6 where the likeliest tokens are asked for); one sequence, 32000 logits, 14.6 us.
+// Of more than some 340 sequences the first kernel's 32 bytes each in shared memory leave two CTAs an SM instead of three, on the same grid: 336 -> 352 of up to two rows of 16000 logits with a draft's 47.6 -> 60.4 us.
 // Weights and sums are in 64 bits: a draw is decided by sums over the vocabulary, and with 2^-24 in each weight one draw in some hundred thousand of flat rows would be another token than
 // exact sums give.  All sums are in an order that depends on sizes alone.
 #include <cuda_runtime.h>
