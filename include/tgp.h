@@ -541,7 +541,7 @@ int  tgp_k_sample(const float *logits, const float *u_dev, int32_t *out, uint32_
  * out [T]: in the rows of a sequence the tokens that it goes on with - those taken and the one drawn -, then -1; n_out [B]: how many (0 for a sequence without rows, whose rows do not lie in [0, T), or that begins before
  * the start of a sequence before it, where that is in [0, T]: a row is one sequence's at most).  Rows of no sequence keep what they hold.  What stays in the cache are the rows fed with tokens that hold: length before the step + n_out.
  * temperature fp32 [B] or NULL (1); a row's 0, negative or NaN: d is taken if it is the row's likeliest token (the lowest of equals), which also is the token that follows.  Logits of -inf and NaN
- * weigh nothing (so filters may be applied to both by -inf); a row of nothing else takes no token and gives token 0.  A drafted token outside [0, V) is not taken.  u and u_draw are limited to [0, 1].  Weights and sums are in 64 bits, a weight right to 2^-41 of itself, weights
+ * weigh nothing (so filters may be applied to both by -inf); a row of nothing else takes no token and gives token 0.  A drafted token outside [0, V) is not taken.  u and u_draw are limited to [0, 1].  Weights and sums are in 64 bits, a weight right to 2^-41 of itself, so p - q to some 2^-40 of p, weights
  * of less than 2^-1000 of a row's largest are 0.  draft_logits of a sequence's last row are not read.  scratch_dev: tgp_k_verify_scratch_bytes(), not shared with a call that may run at the same time.  T <= 32767, V <= TGP_SAMPLE_MAX_V. */
 int  tgp_k_verify(const float *logits, const float *draft_logits, const int32_t *tokens_dev, const int32_t *start_dev, const float *u_dev, const float *u_draw_dev, int32_t *out_dev, int32_t *n_out_dev,
                   uint32_t B, uint32_t T, uint32_t V, const float *temperature_dev, void *scratch_dev, void *stream);
